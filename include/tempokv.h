@@ -23,6 +23,10 @@
  *   kv_validate_jobs(_device)  race check of a job batch (duplicate
  *                         destinations, out-of-range ids), on host copies or
  *                         on the device
+ *   kv_rope_append / kv_paged_attention / kv_attention_weights / kv_evict_*
+ *                         what a serving step does with the retrieved KV: new
+ *                         tokens' rotated keys and values beside it, attention
+ *                         over both, and eviction by accumulated weight
  *
  * Conventions shared by every call
  * --------------------------------
@@ -60,7 +64,7 @@ typedef enum kv_status {
     KV_ENOSPC = -4,  /* no free staging slot for a miss, or the index is full */
     KV_EHIP = -5,    /* a HIP runtime call or kernel launch failed */
     KV_EDUP = -6,    /* two jobs of one batch write the same block (scatter) or slot (gather) */
-    KV_ELIMIT = -7   /* request larger than a fixed capacity (kv_index_insert_static) */
+    KV_ELIMIT = -7   /* request larger than a fixed capacity (kv_index_insert_static, the cache operators) */
 } kv_status;
 
 /* Shapes and strides of the two KV layouts.
@@ -364,6 +368,180 @@ int kv_validate_jobs(const kv_layout *layout, const int32_t *h_block_tables, int
 int kv_validate_jobs_device(const kv_layout *layout, const int32_t *d_block_tables, int32_t bt_stride,
                             int32_t num_reqs, const kv_job *d_jobs, int32_t num_jobs, int is_store,
                             int32_t *d_marks, int32_t *d_status, void *stream);
+
+/* ----------------------------------------------------------------------- */
+/* Operators over the paged cache                                           */
+/* ----------------------------------------------------------------------- */
+
+/* What a serving step does with the KV that a retrieve left in the paged
+ * blocks: put the keys and values of new tokens beside it
+ * (kv_rope_append), attend to both (kv_paged_attention), and, to hold fewer
+ * protected bytes, keep only the tokens that attention uses
+ * (kv_attention_weights, kv_evict_select, kv_evict_compact).  They read and
+ * write one layer's paged tensor (d_layer, as layer_ptrs[l] of the copies)
+ * through the same layout and block tables.
+ *
+ * Element types.  Queries, new keys and values, and outputs are KV_BF16 or
+ * KV_F16.  The cache holds the same type (elem_bytes 2) or KV_F8E4M3
+ * (elem_bytes 1; sign, 4 exponent bits, 3 mantissa bits, largest value 448,
+ * no infinities).  An 8-bit cache may have a positive scale per KV head for
+ * each plane (d_k_scale, d_v_scale: float32 [kv_heads], NULL = 1): an element
+ * stands for its value times the scale.  Sums, softmax statistics and angles
+ * are held in 32 bits or more. */
+typedef enum kv_dtype { KV_BF16 = 0, KV_F16 = 1, KV_F8E4M3 = 2 } kv_dtype;
+
+/* Rows [num_q][heads][head_dim] of new tokens in device memory: element x of
+ * head h of token t is at element t*token_stride + h*head_stride + x.
+ * d_data and both strides in bytes must be multiples of 16, so that q, k and
+ * v may lie side by side as one projection leaves them. */
+typedef struct kv_rows {
+    const void *d_data;
+    int64_t token_stride, head_stride;   /* elements */
+    int32_t heads;
+    int32_t dtype;                       /* KV_BF16 or KV_F16 */
+} kv_rows;
+
+/* A ragged batch of new tokens and the cache they belong to.  Request r has
+ * the rows d_q_off[r] .. d_q_off[r+1] (n_r of them) and, these included,
+ * d_kv_len[r] tokens in the cache: new token i has cache index
+ * d_kv_len[r] - n_r + i, and cache index t lies at row t % B of the block
+ * d_block_tables[r*bt_stride + t / B].  A block id outside [0, num_blocks) is
+ * a missing block, and indices past the table are missing too: nothing is
+ * written there, and attention does not see them.  n_r may be 0, 1 or
+ * thousands in one batch.  max_q_len and max_kv_len are the largest n_r and
+ * d_kv_len[r] as far as the host knows: they choose launch shapes, results do
+ * not depend on them.  The struct lives in host memory and is read during the
+ * call. */
+typedef struct kv_batch {
+    int32_t num_reqs;
+    int32_t bt_stride;
+    int64_t num_q;                   /* rows in all: d_q_off[num_reqs] */
+    int32_t max_q_len, max_kv_len;
+    const int64_t *d_q_off;          /* [num_reqs+1], non-decreasing */
+    const int32_t *d_kv_len;         /* [num_reqs] */
+    const int32_t *d_block_tables;   /* [num_reqs][bt_stride] */
+} kv_batch;
+
+/* Ways of scaling rotary frequencies for contexts longer than the original. */
+typedef enum kv_rope_scaling {
+    KV_ROPE_PLAIN = 0,    /* f_i = base^(-2i/rot_dim) */
+    KV_ROPE_LINEAR = 1,   /* f_i / factor (positions interpolated; Chen et al. 2023, arXiv 2306.15595) */
+    KV_ROPE_BASE = 2,     /* base replaced by base * factor^(rot_dim/(rot_dim-2)); rot_dim > 2 */
+    KV_ROPE_RAMP = 3      /* by turns in the original context (Peng et al. 2023, arXiv 2309.00071): with
+                             t_i = context * f_i / (2 pi) and g_i = clamp((t_i - low)/(high - low), 0, 1), the
+                             frequency is f_i * (g_i + (1 - g_i)/factor), and rotated values are multiplied by
+                             magnitude = 0.1 ln(factor) + 1 */
+} kv_rope_scaling;
+
+/* Frequencies (radians per position, float64) of the rot_dim/2 rotated pairs,
+ * in host memory, and the factor on rotated values (1 except for
+ * KV_ROPE_RAMP).  `context`, `low` and `high` are read by KV_ROPE_RAMP alone,
+ * `factor` (>= 1) by every scaling but KV_ROPE_PLAIN.  Errors: KV_EINVAL. */
+int kv_rope_frequencies(int32_t rot_dim, double base, int32_t scaling, double factor, double context, double low,
+                        double high, double *h_freqs, float *magnitude);
+
+/* How kv_rope_append pairs elements and turns them (flags, or'ed). */
+enum { KV_ROPE_HALF = 0,          /* element i with i + rot_dim/2 */
+       KV_ROPE_INTERLEAVED = 1,   /* element 2i with 2i + 1 */
+       KV_ROPE_INVERSE = 2 };     /* turn backwards: undoes a rotation (at magnitude 1), and is its gradient */
+
+/* Rotary positions, and the append to the paged cache.  A row at position p
+ * has its pair (a, b) of index i < rot_dim/2 replaced by
+ *     (a cos u - b sin u, a sin u + b cos u) * magnitude,  u = p * d_freqs[i],
+ * the angle formed and reduced in 64 bits; elements from rot_dim on stay.
+ * p is d_positions[row], or the row's cache index when d_positions is NULL.
+ *   q, q_out   rows to rotate and where the result goes (the same rows for
+ *              in place; partial overlap is not allowed); both NULL: none
+ *   k, v       new keys and values with kv_heads heads: k rotated, v as it
+ *              is, both written to the cache at the row's cache index in
+ *              cache_dtype (KV_F8E4M3: divided by the scale, rounded to
+ *              nearest even, values beyond 448 become 448 with their sign,
+ *              NaN stays); both NULL: the cache is not touched, and d_layer
+ *              may be NULL
+ * d_freqs float64 [rot_dim/2] in device memory; rot_dim even, 0 <= rot_dim <=
+ * head_dim; head_dim a multiple of 8 (16 for an 8-bit cache) up to 256.
+ * Cache indices of one batch must name distinct rows.  One launch; num_q == 0
+ * enqueues nothing.  Errors: KV_EINVAL, KV_EALIGN, KV_ELIMIT (head_dim, or
+ * blocks that span 64 GiB or more of one layer), KV_EHIP. */
+int kv_rope_append(const kv_layout *layout, void *d_layer, const kv_batch *batch, const kv_rows *q,
+                   const kv_rows *q_out, const kv_rows *k, const kv_rows *v, const double *d_freqs, int32_t rot_dim,
+                   int32_t flags, float magnitude, const int32_t *d_positions, int32_t cache_dtype,
+                   const float *d_k_scale, const float *d_v_scale, void *stream);
+
+/* Bytes of device scratch that kv_paged_attention needs for a batch (0 when
+ * it splits no request's keys): depends on the shapes and the host's hints
+ * alone, so a program can keep one buffer of the largest.  Errors: KV_EINVAL,
+ * KV_EALIGN, KV_ELIMIT. */
+int kv_paged_attention_workspace(const kv_layout *layout, const kv_batch *batch, int32_t q_heads, int32_t window,
+                                 int64_t *bytes);
+
+/* Attention of a batch's new tokens over the paged cache, the new tokens'
+ * own keys included (kv_rope_append put them there).  Query head g reads KV
+ * head g / (q_heads / kv_heads).  Row i at cache index p_i sees key j when
+ * j < d_kv_len[r], j's block is not missing, j <= p_i if `causal`, and
+ * j > p_i - window if window > 0 (0 = no window):
+ *     s_ij = scale * q_i . k_j,   lse_i = log sum_j exp(s_ij),
+ *     out_i = sum_j exp(s_ij - lse_i) v_j   over the keys it sees.
+ * A row that sees no key gets out 0 and lse -infinity; keys that a row does
+ * not see do not reach it, whatever they hold.
+ *   q, out     rows of one dtype and head count, a multiple of kv_heads
+ *   scale      positive and finite
+ *   d_lse      float32 [num_q][q_heads], or NULL
+ *   d_workspace  at least kv_paged_attention_workspace bytes, 16-byte
+ *              aligned, overwritten (NULL when that is 0)
+ * Deterministic.  At most two launches; num_q == 0 enqueues nothing.
+ * Errors: KV_EINVAL, KV_EALIGN, KV_ELIMIT (as kv_rope_append, and more than
+ * 2^31 row tiles or a workspace too small), KV_EHIP. */
+int kv_paged_attention(const kv_layout *layout, const void *d_layer, const kv_batch *batch, const kv_rows *q,
+                       const kv_rows *out, float scale, int32_t causal, int32_t window, int32_t cache_dtype,
+                       const float *d_k_scale, const float *d_v_scale, float *d_lse, void *d_workspace,
+                       int64_t workspace_bytes, void *stream);
+
+/* Attention weight that each cached token received from the batch's new
+ * tokens, accumulated over calls: for request r, KV head h and cache index
+ * j < d_kv_len[r],
+ *     d_weights[r][h][j] = decay * d_weights[r][h][j]
+ *                          + sum over rows i and the query heads g of h that see j of exp(s_igj - lse_ig)
+ * with s and the rule of what a row sees as in kv_paged_attention, which
+ * gives d_lse.  A key that no row sees, or in a missing block, gets 0 added;
+ * rows with lse -infinity add nothing.  decay 0 overwrites without reading
+ * what was there.  d_weights float32 [num_reqs][kv_heads][weight_stride];
+ * indices from weight_stride on, and from d_kv_len[r] on, are left alone.
+ * One launch, deterministic.  Errors: those of kv_paged_attention. */
+int kv_attention_weights(const kv_layout *layout, const void *d_layer, const kv_batch *batch, const kv_rows *q,
+                         const float *d_lse, float scale, int32_t causal, int32_t window, int32_t cache_dtype,
+                         const float *d_k_scale, float decay, float *d_weights, int64_t weight_stride, void *stream);
+
+/* Which cached tokens to keep, for every layer, request and head of
+ * accumulated weights float32 [num_layers][num_reqs][heads][weight_stride]
+ * (heads = kv_heads, or 1 for one choice that all heads share).  Of a request
+ * with n = min(d_len[r], weight_stride) tokens, m = min(n, budget) are kept:
+ * all if n <= budget, else the first `sink`, the last `recent` and, of those
+ * between, the ones of largest weight (a tie goes to the lower index; NaN is
+ * below every number, and -0 equals +0).
+ *   d_keep     int32 [num_layers][num_reqs][heads][budget]: the kept indices
+ *              in ascending order, then -1
+ *   d_new_len  int32 [num_reqs]: m
+ * sink, recent >= 0, sink + recent <= budget, budget > 0.  One launch.
+ * Errors: KV_EINVAL, KV_EHIP. */
+int kv_evict_select(const float *d_weights, int64_t weight_stride, const int32_t *d_len, int32_t num_layers,
+                    int32_t num_reqs, int32_t heads, int32_t budget, int32_t sink, int32_t recent, int32_t *d_keep,
+                    int32_t *d_new_len, void *stream);
+
+/* Move the kept tokens to the front of their request's blocks, in place and
+ * in order: for every layer l, request r, head and i < d_new_len[r], the K
+ * and V rows at cache index d_keep[l][r][head][i] go to cache index i (and,
+ * with d_weights, their weights likewise).  heads is kv_heads or 1 as in
+ * kv_evict_select; d_keep must be ascending within each head, as that call
+ * leaves it.  Rows stay as they are: keys keep the rotation of the position
+ * they were computed at.  Blocks past ceil(d_new_len[r] / B) are free
+ * afterwards.  A move whose source or destination block is missing or past
+ * the table is skipped.  Requests must not share blocks that move.  head_dim *
+ * elem_bytes must be a multiple of 16.  One launch.  Errors: KV_EINVAL,
+ * KV_EALIGN, KV_ELIMIT (blocks that span 64 GiB or more), KV_EHIP. */
+int kv_evict_compact(const kv_layout *layout, void *const *h_layer_ptrs, const int32_t *d_block_tables,
+                     int32_t bt_stride, int32_t num_reqs, int32_t heads, const int32_t *d_keep, int32_t budget,
+                     const int32_t *d_new_len, float *d_weights, int64_t weight_stride, void *stream);
 
 /* ----------------------------------------------------------------------- */
 /* Commitment rule (host)                                                   */

@@ -28,6 +28,9 @@ RETRIEVE_KIND_NAMES = {KV_RETRIEVE_UNIT: "unit", KV_RETRIEVE_PAIR: "pair", KV_RE
                        KV_RETRIEVE_QUAD: "quad"}
 SIM_TRACE_KINDS = ["arrive", "admit", "commit", "ordinary", "ready", "stageready", "transfer", "fetch", "release",
                    "done", "evict"]
+KV_BF16, KV_F16, KV_F8E4M3 = range(3)
+KV_ROPE_PLAIN, KV_ROPE_LINEAR, KV_ROPE_BASE, KV_ROPE_RAMP = range(4)
+KV_ROPE_HALF, KV_ROPE_INTERLEAVED, KV_ROPE_INVERSE = 0, 1, 2
 KV_MAX_LAYERS = 128
 HASH_BLOCK_TOKENS = 16
 
@@ -40,11 +43,13 @@ EXPORTS = ["kv_hash_prefix", "kv_index_create", "kv_index_destroy", "kv_index_in
            "kv_host_device_pointer", "kv_version", "kv_sim_run", "kv_stage_in", "kv_stage_out",
            "kv_pipeline_create", "kv_pipeline_destroy", "kv_retrieve_pipelined", "kv_decide_claims",
            "kv_build_jobs_routed", "kv_ttr_static", "kv_ttr_state_aware", "kv_chunk_keys", "kv_validate_jobs_device",
-           "kv_probe_mixed_traffic"]
+           "kv_probe_mixed_traffic", "kv_rope_frequencies", "kv_rope_append", "kv_paged_attention_workspace",
+           "kv_paged_attention", "kv_attention_weights", "kv_evict_select", "kv_evict_compact"]
 # the calls that run on the host only (host.cpp, controller.cpp)
 HOST_CALLS = ["kv_build_jobs", "kv_build_jobs_routed", "kv_decide_claims", "kv_group_jobs_by_slot",
               "kv_validate_jobs", "kv_commit_should_stage", "kv_commit_should_stage_n", "kv_retrieve_plan",
-              "kv_strerror", "kv_version", "kv_sim_run", "kv_ttr_static", "kv_ttr_state_aware", "kv_chunk_keys"]
+              "kv_strerror", "kv_version", "kv_sim_run", "kv_ttr_static", "kv_ttr_state_aware", "kv_chunk_keys",
+              "kv_rope_frequencies", "kv_paged_attention_workspace"]
 
 
 class KvError(RuntimeError):
@@ -77,11 +82,24 @@ class KvSimEvent(ct.Structure):
     _fields_ = [("t", ct.c_double), ("kind", ct.c_int32), ("id", ct.c_int32)]
 
 
+class KvRows(ct.Structure):
+    _fields_ = [("d_data", ct.c_void_p), ("token_stride", ct.c_int64), ("head_stride", ct.c_int64),
+                ("heads", ct.c_int32), ("dtype", ct.c_int32)]
+
+
+class KvBatch(ct.Structure):
+    """A ragged batch of new tokens (make_batch).  Keeps its tensors alive."""
+    _fields_ = [("num_reqs", ct.c_int32), ("bt_stride", ct.c_int32), ("num_q", ct.c_int64),
+                ("max_q_len", ct.c_int32), ("max_kv_len", ct.c_int32), ("d_q_off", ct.c_void_p),
+                ("d_kv_len", ct.c_void_p), ("d_block_tables", ct.c_void_p)]
+
+
 _lib: Optional[ct.CDLL] = None
 # Tests only: a separately built copy of the host-only calls (HOST_CALLS) from the same sources, e.g. a
 # sanitizer build, used by the host-call wrappers in place of libtempokv.so.
 _host_override: Optional[ct.CDLL] = None
 _vp, _i32, _i64, _u32, _u64, _dbl = ct.c_void_p, ct.c_int32, ct.c_int64, ct.c_uint32, ct.c_uint64, ct.c_double
+_flt = ct.c_float
 
 SIGNATURES = {
     "kv_hash_prefix": [_vp, _vp, _i32, _u64, _vp, _vp, _vp],
@@ -122,6 +140,13 @@ SIGNATURES = {
     "kv_pipeline_destroy": [_vp],
     "kv_retrieve_pipelined": [_vp, ct.POINTER(KvLayout), _vp, _vp, _vp, _vp, _i32, _i32, _vp, _vp, _i32, _i32,
                               _vp, _vp],
+    "kv_rope_frequencies": [_i32, _dbl, _i32, _dbl, _dbl, _dbl, _dbl, _vp, ct.POINTER(_flt)],
+    "kv_rope_append": [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i32, _i32, _flt, _vp, _i32, _vp, _vp, _vp],
+    "kv_paged_attention_workspace": [ct.POINTER(KvLayout), ct.POINTER(KvBatch), _i32, _i32, ct.POINTER(_i64)],
+    "kv_paged_attention": [_vp, _vp, _vp, _vp, _vp, _flt, _i32, _i32, _i32, _vp, _vp, _vp, _vp, _i64, _vp],
+    "kv_attention_weights": [_vp, _vp, _vp, _vp, _vp, _flt, _i32, _i32, _i32, _vp, _flt, _vp, _i64, _vp],
+    "kv_evict_select": [_vp, _i64, _vp, _i32, _i32, _i32, _i32, _i32, _i32, _vp, _vp, _vp],
+    "kv_evict_compact": [_vp, _vp, _vp, _i32, _i32, _i32, _vp, _i32, _vp, _vp, _i64, _vp],
 }
 
 
@@ -651,6 +676,181 @@ def kv_validate_jobs_device(layout: KvLayout, d_block_tables, bt_stride: int, nu
                                          1 if is_store else 0, _dptr(d_marks, torch.int32, "marks"),
                                          _dptr(d_status, torch.int32, "status"), _stream(stream)),
            "kv_validate_jobs_device")
+
+
+# ---------------------------------------------------------------------------
+# operators over the paged cache
+# ---------------------------------------------------------------------------
+
+def make_batch(d_q_off, d_kv_len, d_block_tables, num_q: int, max_q_len: int, max_kv_len: int) -> KvBatch:
+    """A ragged batch of new tokens for the operators over the paged cache: int64 offsets [R+1] of each request's
+    rows, int32 tokens in the cache [R] (new ones included), int32 block tables [R, n], the rows in all, and the
+    largest of both lengths as far as the host knows (launch shapes only).  Made once a step, used for every
+    layer."""
+    torch = _torch()
+    R = d_kv_len.numel()
+    if d_q_off.numel() != R + 1 or d_block_tables.dim() != 2 or d_block_tables.shape[0] != R:
+        raise ValueError("q_off must hold one offset more than kv_len, and block_tables one row per request")
+    b = KvBatch(R, max(1, d_block_tables.shape[1]), num_q, max_q_len, max_kv_len,
+                _dptr(d_q_off, torch.int64, "q_off"), _dptr(d_kv_len, torch.int32, "kv_len"),
+                _dptr(d_block_tables, torch.int32, "block_tables"))
+    b.tensors = (d_q_off, d_kv_len, d_block_tables)
+    return b
+
+
+def _dtypes():
+    """Element types of the operators: torch dtype -> kv_dtype."""
+    global _dtype_codes
+    if _dtype_codes is None:
+        torch = _torch()
+        _dtype_codes = {torch.bfloat16: KV_BF16, torch.float16: KV_F16, torch.float8_e4m3fn: KV_F8E4M3}
+    return _dtype_codes
+
+
+_dtype_codes = None
+
+
+def _rows(t, batch: KvBatch, layout: KvLayout, what: str) -> KvRows:
+    """Rows [num_q, heads, head_dim] of a device tensor whose last dimension is dense."""
+    if not t.is_cuda:
+        raise ValueError(f"{what} must be a device tensor")
+    shape, (ts, hs, es) = t.shape, t.stride() if t.dim() == 3 else (0, 0, 0)
+    if t.dim() != 3 or shape[0] != batch.num_q or shape[2] != layout.head_dim or (es != 1 and shape[2] > 1):
+        raise ValueError(f"{what} must be [{batch.num_q}, heads, {layout.head_dim}] with dense rows, got "
+                         f"{tuple(t.shape)} with strides {t.stride()}")
+    code = _dtypes().get(t.dtype)
+    if code is None:
+        raise ValueError(f"{what} must be bfloat16 or float16, got {t.dtype}")
+    return KvRows(t.data_ptr(), ts, hs, shape[1], code)
+
+
+def _cache_code(cache_dtype, layout: KvLayout, dtype: int) -> int:
+    """Element type of the cache: given, or float8_e4m3fn for one byte and the queries' type for two."""
+    if cache_dtype is None:
+        return KV_F8E4M3 if layout.elem_bytes == 1 else dtype
+    code = _dtypes().get(cache_dtype)
+    if code is None:
+        raise ValueError(f"the cache must be bfloat16, float16 or float8_e4m3fn, got {cache_dtype}")
+    return code
+
+
+def _scale_ptr(t, layout: KvLayout, what: str):
+    if t is None:
+        return None
+    if not isinstance(t, int) and t.numel() != layout.kv_heads:
+        raise ValueError(f"{what} must hold one scale per KV head")
+    return _dptr(t, _torch().float32, what)
+
+
+def kv_rope_frequencies(rot_dim: int, base: float = 10000.0, scaling: int = KV_ROPE_PLAIN, factor: float = 1.0,
+                        context: float = 0.0, low: float = 1.0, high: float = 32.0):
+    """Returns (frequencies float64 [rot_dim/2], magnitude) for kv_rope_append."""
+    out = np.zeros(max(rot_dim // 2, 0), np.float64)
+    mag = _flt(1.0)
+    _check(host_lib().kv_rope_frequencies(rot_dim, base, scaling, factor, context, low, high, out.ctypes.data,
+                                          ct.byref(mag)), "kv_rope_frequencies")
+    return out, mag.value
+
+
+def kv_rope_append(layout: KvLayout, layer, batch: KvBatch, q, k, v, d_freqs, *, q_out=None,
+                   interleaved: bool = False, inverse: bool = False, magnitude: float = 1.0, positions=None,
+                   k_scale=None, v_scale=None, cache_dtype=None, stream=None) -> None:
+    """Rotate q into q_out (default: in place) and append rotated k, and v, to the cache.  q, or both k and v, may be
+    None; layer may be None without k and v."""
+    torch = _torch()
+    if q is None and k is None:
+        raise ValueError("nothing to do: q and k are both None")
+    if (k is None) != (v is None):
+        raise ValueError("k and v go together")
+    refs = [None if t is None else _rows(t, batch, layout, what)
+            for t, what in ((q, "q"), (q if q_out is None else q_out, "q_out"), (k, "k"), (v, "v"))]
+    code = _cache_code(cache_dtype, layout, (refs[0] or refs[2]).dtype)
+    if positions is not None and not isinstance(positions, int) and positions.numel() != batch.num_q:
+        raise ValueError("positions must hold one position per row")
+    _check(lib().kv_rope_append(ct.addressof(layout), None if layer is None else _dptr(layer, None, "layer"),
+                                ct.addressof(batch), *[None if r is None else ct.addressof(r) for r in refs],
+                                _dptr(d_freqs, torch.float64, "freqs"), 2 * d_freqs.numel(),
+                                KV_ROPE_INTERLEAVED * bool(interleaved) | KV_ROPE_INVERSE * bool(inverse), magnitude,
+                                None if positions is None else _dptr(positions, torch.int32, "positions"), code,
+                                _scale_ptr(k_scale, layout, "k_scale"), _scale_ptr(v_scale, layout, "v_scale"),
+                                _stream(stream)), "kv_rope_append")
+
+
+def kv_paged_attention_workspace(layout: KvLayout, batch: KvBatch, q_heads: int, window: int = 0) -> int:
+    """Bytes of device scratch that kv_paged_attention needs for this batch."""
+    n = _i64(0)
+    _check(host_lib().kv_paged_attention_workspace(ct.byref(layout), ct.byref(batch), q_heads, window, ct.byref(n)),
+           "kv_paged_attention_workspace")
+    return n.value
+
+
+def kv_paged_attention(layout: KvLayout, layer, batch: KvBatch, q, out, scale: float, *, causal: bool = True,
+                       window: int = 0, lse=None, k_scale=None, v_scale=None, cache_dtype=None, workspace=None,
+                       stream=None) -> None:
+    """Attention of the batch's rows over the paged cache, into out (and lse, float32 [num_q, heads])."""
+    rq, ro = _rows(q, batch, layout, "q"), _rows(out, batch, layout, "out")
+    ws, size = (None, 0) if workspace is None else (_dptr(workspace, None, "workspace"), workspace.nbytes)
+    if lse is not None and lse.numel() != batch.num_q * rq.heads:
+        raise ValueError("lse must be [rows, heads]")
+    _check(lib().kv_paged_attention(ct.addressof(layout), _dptr(layer, None, "layer"), ct.addressof(batch),
+                                    ct.addressof(rq), ct.addressof(ro), scale, 1 if causal else 0, window,
+                                    _cache_code(cache_dtype, layout, rq.dtype),
+                                    _scale_ptr(k_scale, layout, "k_scale"), _scale_ptr(v_scale, layout, "v_scale"),
+                                    None if lse is None else _dptr(lse, _torch().float32, "lse"), ws, size,
+                                    _stream(stream)), "kv_paged_attention")
+
+
+def kv_attention_weights(layout: KvLayout, layer, batch: KvBatch, q, lse, weights, scale: float, *,
+                         causal: bool = True, window: int = 0, decay: float = 1.0, k_scale=None, cache_dtype=None,
+                         stream=None) -> None:
+    """weights (float32 [requests, kv_heads, n]) = decay * weights + the attention that each cached token receives
+    from the batch's rows; lse as kv_paged_attention left it."""
+    torch = _torch()
+    rq = _rows(q, batch, layout, "q")
+    if lse.numel() != batch.num_q * rq.heads:
+        raise ValueError("lse must be [rows, heads]")
+    if weights.dim() != 3 or weights.shape[0] != batch.num_reqs or weights.shape[1] != layout.kv_heads:
+        raise ValueError("weights must be [requests, kv_heads, n]")
+    _check(lib().kv_attention_weights(ct.addressof(layout), _dptr(layer, None, "layer"), ct.addressof(batch),
+                                      ct.addressof(rq), _dptr(lse, torch.float32, "lse"), scale, 1 if causal else 0,
+                                      window, _cache_code(cache_dtype, layout, rq.dtype),
+                                      _scale_ptr(k_scale, layout, "k_scale"), decay,
+                                      _dptr(weights, torch.float32, "weights"), weights.shape[2], _stream(stream)),
+           "kv_attention_weights")
+
+
+def kv_evict_select(weights, d_len, budget: int, sink: int, recent: int, d_keep, d_new_len, stream=None) -> None:
+    """Which tokens to keep: weights float32 [layers, requests, heads, n], d_len int32 [requests]; d_keep int32
+    [layers, requests, heads, budget] and d_new_len int32 [requests] receive the choice."""
+    torch = _torch()
+    if weights.dim() != 4 or d_len.numel() != weights.shape[1] or d_new_len.numel() != weights.shape[1]:
+        raise ValueError("weights must be [layers, requests, heads, n], with one length per request")
+    L, R, G, n = weights.shape
+    if tuple(d_keep.shape) != (L, R, G, budget):
+        raise ValueError(f"keep must be {(L, R, G, budget)}")
+    _check(lib().kv_evict_select(_dptr(weights, torch.float32, "weights"), n, _dptr(d_len, torch.int32, "len"), L, R, G,
+                                 budget, sink, recent, _dptr(d_keep, torch.int32, "keep"),
+                                 _dptr(d_new_len, torch.int32, "new_len"), _stream(stream)), "kv_evict_select")
+
+
+def kv_evict_compact(layout: KvLayout, layers: Sequence, d_block_tables, d_keep, d_new_len, weights=None,
+                     stream=None) -> None:
+    """Move the kept rows (and weights) to the front of their request's blocks, in place."""
+    torch = _torch()
+    if len(layers) != layout.num_layers:
+        raise ValueError("one paged tensor per layer is required")
+    if d_keep.dim() != 4 or d_keep.shape[0] != layout.num_layers or d_block_tables.dim() != 2 \
+            or d_block_tables.shape[0] != d_keep.shape[1] or d_new_len.numel() != d_keep.shape[1]:
+        raise ValueError("keep must be [layers, requests, heads, budget], with one block table and length per request")
+    if weights is not None and tuple(weights.shape[:3]) != tuple(d_keep.shape[:3]):
+        raise ValueError("weights must be [layers, requests, heads, n] as keep is")
+    lp = _layer_array(layers)   # alive during the call
+    _check(lib().kv_evict_compact(ct.addressof(layout), lp.buffer_info()[0],
+                                  _dptr(d_block_tables, torch.int32, "block_tables"), d_block_tables.shape[1],
+                                  d_keep.shape[1], d_keep.shape[2], _dptr(d_keep, torch.int32, "keep"),
+                                  d_keep.shape[3], _dptr(d_new_len, torch.int32, "new_len"),
+                                  None if weights is None else _dptr(weights, torch.float32, "weights"),
+                                  0 if weights is None else weights.shape[3], _stream(stream)), "kv_evict_compact")
 
 
 def kv_commit_should_stage(ttu_s: float, ttr_s: float, free_protected_bytes: int, claim_new_bytes: int,

@@ -1,0 +1,387 @@
+// attention.hip -- attention of new tokens over the paged cache.
+//
+// For a row i and the keys j it sees, s_ij = scale q_i.k_j, out_i = sum_j
+// exp(s_ij - lse_i) v_j.  The keys are passed once, with the running maximum
+// m and sum l of a softmax: adding keys with scores s makes
+//     m' = max(m, s),  l' = l 2^(m-m') + sum 2^(s-m'),  o' = o 2^(m-m') + sum 2^(s-m') v
+// (scores in units of log 2), and parts taken over different keys join by the
+// same rule.  A row is a (token, head) pair: the heads that share a KV head
+// are packed into one tile, so that K and V are read once for all of them.
+
+#include <math.h>
+
+#include "mfma.h"
+#include "paged.h"
+
+namespace tkv {
+namespace {
+
+constexpr int kWaves = 4;
+constexpr int kThreads = 64 * kWaves;
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+static_assert(kSplitStep == 32 * kWaves, "a wave takes 32 keys a step");
+
+struct AttentionParams {
+    Paged cache;
+    const char *q;
+    char *out;
+    int64_t q_ts, q_hs, o_ts, o_hs;    // bytes
+    float *lse;
+    float *part_o;                     // [splits][num_q * q_heads][head_dim], then
+    float *part_ml;                    // [splits][num_q * q_heads][2]: maximum (log 2) and sum
+    const float *k_scale, *v_scale;
+    int64_t tiles;
+    float scale;                       // times log2 e
+    int32_t q_heads, kv_heads, group, head_dim;
+    int32_t splits, window;
+    bool causal;
+};
+
+// The request, and the tile within it, of row tile `tile` for tiles of `rows`
+// rows.  Request r starts at tile floor(q_off[r] * group / rows) + r, which
+// leaves it at least ceil(n_r * group / rows) tiles: a map from the offsets
+// alone, with at most one idle tile for each request.
+struct Tile {
+    int32_t req;
+    int64_t first;      // the request's first row of q
+    int64_t row0;       // the tile's first row within the request (token * group + head)
+    int64_t rows;       // rows of the request
+};
+
+__device__ __forceinline__ Tile find_tile(const Paged &c, int64_t tile, int32_t group, int32_t rows) {
+    const int lane = threadIdx.x & 63;
+    int r = 0;
+    for (int base = 0; base < c.num_reqs; base += 64) {
+        const bool at = base + lane < c.num_reqs &&
+                        clamp_row(c, c.q_off[base + lane]) * group / rows + base + lane <= tile;
+        const int n = __popcll(__ballot(at));
+        r += n;
+        if (n < 64) break;
+    }
+    Tile t;
+    t.req = __builtin_amdgcn_readfirstlane(r > 0 ? r - 1 : 0);
+    t.first = clamp_row(c, c.q_off[t.req]);
+    const int64_t n = clamp_row(c, c.q_off[t.req + 1]) - t.first;
+    t.rows = (n < 0 ? 0 : n) * group;
+    t.row0 = (tile - (t.first * group / rows + t.req)) * rows;
+    return t;
+}
+
+__device__ __forceinline__ void store_out(const AttentionParams &p, int64_t row, int head, int d, f32x4 x, bool bf16) {
+    char *to = p.out + row * p.o_ts + head * p.o_hs + d * 2;
+    const u32x2 y = bf16 ? u32x2{pack2<Bf16>(x[0], x[1]), pack2<Bf16>(x[2], x[3])}
+                         : u32x2{pack2<F16>(x[0], x[1]), pack2<F16>(x[2], x[3])};
+    *(u32x2 *)to = y;
+}
+
+// Tiles of 16 rows; the keys of a tile are cut into p.splits parts, one
+// workgroup each, and a part's steps of 32 keys go to its waves in turn.
+// S^T = K Q^T leaves a lane with the scores of one row (lane % 16) for the
+// keys 4 (lane / 16) + i of either half of the step, which is where the
+// second product, O^T = V^T P^T, wants them if V's keys are taken in the same
+// order; so P never leaves its registers.  K is loaded from memory as the
+// matrix operand itself; V goes through LDS, the wave's own, to be read
+// transposed.
+template <class T, bool F8, int DP>
+__global__ __launch_bounds__(kThreads) void attention_split_kernel(AttentionParams p) {
+    constexpr int KS = DP / 32, DT = DP / 16;
+    constexpr int kRow = DP * 2 + 32;          // bytes of an LDS row: 8 rows lie on different banks
+    constexpr int VEC = F8 ? 16 : 8;           // elements of a 16-byte vector of the cache
+    constexpr int VPR = DP / VEC;              // vectors of a row
+    constexpr int VL = 32 * VPR / 64;          // vectors a lane stages
+    __shared__ __align__(16) char lds[kWaves][32 * kRow];
+    __shared__ float part[kWaves][16][2];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, quad = lane >> 4;
+    const int64_t id = blockIdx.x;
+    const int h = (int)(id % p.kv_heads);
+    const int split = (int)(id / p.kv_heads % p.splits);
+    const Tile tile = find_tile(p.cache, id / p.kv_heads / p.splits, p.group, 16);
+    if (tile.row0 >= tile.rows) return;
+
+    // this lane's row
+    const int64_t myrow = tile.row0 + col;
+    const bool have = myrow < tile.rows;
+    const int64_t token = have ? myrow / p.group : 0;
+    const int head = h * p.group + (int)(have ? myrow % p.group : 0);
+    const int32_t len_raw = p.cache.kv_len[tile.req];
+    const int64_t len = min((int64_t)(len_raw < 0 ? 0 : len_raw), (int64_t)p.cache.bt_stride * p.cache.block_size);
+    const int64_t ntok = tile.rows / p.group;
+    const int64_t pos = len_raw - ntok + token;
+    const int64_t pos_first = len_raw - ntok + tile.row0 / p.group;
+    const int64_t last = min(tile.row0 + 15, tile.rows - 1);
+    const int64_t pos_last = len_raw - ntok + last / p.group;
+    // keys this lane's row sees: lo <= j < hi; and those that some or all rows of the tile see
+    const int64_t hi64 = p.causal ? min(len, pos + 1) : len, lo64 = p.window > 0 ? max((int64_t)0, pos - p.window + 1) : 0;
+    const int hi = have ? (int)max((int64_t)0, hi64) : 0, lo = (int)lo64;
+    const int end = (int)max((int64_t)0, p.causal ? min(len, pos_last + 1) : len);
+    const int begin = (int)(p.window > 0 ? max((int64_t)0, pos_first - p.window + 1) : 0) & ~31;
+    const int all_hi = (int)max((int64_t)0, p.causal ? min(len, pos_first + 1) : len);
+    const int all_lo = (int)(p.window > 0 ? max((int64_t)0, pos_last - p.window + 1) : 0);
+    const int steps = end > begin ? (end - begin + 31) / 32 : 0;
+    const int step0 = (int)((int64_t)steps * split / p.splits), step1 = (int)((int64_t)steps * (split + 1) / p.splits);
+
+    u32x4 qf[KS];
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+        // an 8-bit cache is loaded 16 elements at a time, so its lanes hold the head's elements in another order
+        const int d = F8 ? (ks / 2) * 64 + quad * 16 + (ks & 1) * 8 : ks * 32 + quad * 8;
+        qf[ks] = u32x4{0, 0, 0, 0};
+        if (have && d < p.head_dim) qf[ks] = *(const u32x4 *)(p.q + (tile.first + token) * p.q_ts + head * p.q_hs + d * 2);
+    }
+    const float c = p.scale * (F8 && p.k_scale ? p.k_scale[h] : 1.0f);
+    const char *kbase = p.cache.layer + (int64_t)h * p.cache.head_bytes;
+    const char *vbase = kbase + p.cache.kv_stride;
+    char *mine = lds[wave];
+
+    f32x4 o[DT];
+#pragma unroll
+    for (int i = 0; i < DT; ++i) o[i] = f32x4{0, 0, 0, 0};
+    float m = -INFINITY, l = 0.0f;
+
+    for (int step = step0 + wave; step < step1; step += kWaves) {
+        const int t0 = begin + step * 32;
+        // lanes 0..31 look up the step's keys (lanes 32..63 the same ones)
+        const int t = t0 + (lane & 31);
+        uint32_t row = 0;
+        const int32_t blk = t < end ? block_of(p.cache, tile.req, (uint32_t)t, row) : -1;
+        const uint32_t off = blk < 0 ? 0u : (uint32_t)blk * p.cache.block16 + row * p.cache.row16;
+        const uint32_t there = (uint32_t)__ballot(blk >= 0);
+        if (!there) continue;
+        u32x4 kf[2][F8 ? (KS + 1) / 2 : KS];
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            const char *at = kbase + ((int64_t)(uint32_t)__shfl((int)off, x * 16 + col) << 4);
+#pragma unroll
+            for (int ks = 0; ks < (F8 ? (KS + 1) / 2 : KS); ++ks) {
+                const int d = F8 ? ks * 64 + quad * 16 : ks * 32 + quad * 8;
+                kf[x][ks] = d < p.head_dim ? *(const u32x4 *)(at + ks * 64 + quad * 16) : u32x4{0, 0, 0, 0};
+            }
+        }
+        // V, with zeros for missing keys and past the head
+#pragma unroll
+        for (int i = 0; i < VL; ++i) {
+            const int x = i * 64 + lane, r = x / VPR, vec = x % VPR;
+            const char *at = vbase + ((int64_t)(uint32_t)__shfl((int)off, r) << 4);
+            u32x4 y = {0, 0, 0, 0};
+            if (((there >> r) & 1) && vec * VEC < p.head_dim) y = *(const u32x4 *)(at + vec * 16);
+            if constexpr (F8) {
+                *(u32x4 *)(mine + r * kRow + vec * 32) = unpack8<T>(y[0], y[1]);
+                *(u32x4 *)(mine + r * kRow + vec * 32 + 16) = unpack8<T>(y[2], y[3]);
+            } else {
+                *(u32x4 *)(mine + r * kRow + vec * 16) = y;
+            }
+        }
+        f32x4 s[2];
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            s[x] = f32x4{0, 0, 0, 0};
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                if constexpr (F8) s[x] = T::mfma16(unpack8<T>(kf[x][ks / 2][(ks & 1) * 2], kf[x][ks / 2][(ks & 1) * 2 + 1]), qf[ks], s[x]);
+                else s[x] = T::mfma16(kf[x][ks], qf[ks], s[x]);
+            }
+        }
+        const bool whole = there == 0xffffffffu && t0 >= all_lo && t0 + 32 <= all_hi;
+        bool seen[2][4];
+        float top = -INFINITY;
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int k = x * 16 + quad * 4 + i;
+                seen[x][i] = whole || (((there >> k) & 1) && t0 + k >= lo && t0 + k < hi);
+                s[x][i] = seen[x][i] ? s[x][i] * c : -INFINITY;
+                top = fmaxf(top, s[x][i]);
+            }
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        const float m1 = fmaxf(m, top), base = m1 == -INFINITY ? 0.0f : m1;
+        const float fade = exp2_(m - base);
+        m = m1;
+        l *= fade;
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                s[x][i] = exp2_(s[x][i] - base);
+                l += s[x][i];
+            }
+        const u32x4 pf = {pack2<T>(s[0][0], s[0][1]), pack2<T>(s[0][2], s[0][3]), pack2<T>(s[1][0], s[1][1]),
+                          pack2<T>(s[1][2], s[1][3])};
+#pragma unroll
+        for (int i = 0; i < DT; ++i) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[i][e] *= fade;
+        }
+#pragma unroll
+        for (int i = 0; i < DT; ++i) {
+            const char *at = mine + (quad * 4 + (col >> 2)) * kRow + i * 32 + (col & 3) * 8;
+            const u32x2 a = read_transposed(at), b = read_transposed(at + 16 * kRow);
+            u32x4 vf = {a[0], a[1], b[0], b[1]};
+            if (whole) {
+                o[i] = T::mfma16(vf, pf, o[i]);
+                continue;
+            }
+            // A value that is not finite must reach only the rows that see its key: 0 times it is NaN.  Such values
+            // are taken out of the product and put in by counting, for each row, the keys it sees that hold them.
+            u32x4 odd[3];
+            if (T::take_nonfinite(vf, odd)) {
+                const u32x4 one = {T::pair(seen[0][0], seen[0][1]), T::pair(seen[0][2], seen[0][3]),
+                                   T::pair(seen[1][0], seen[1][1]), T::pair(seen[1][2], seen[1][3])};
+#pragma unroll
+                for (int kind = 0; kind < 3; ++kind) {
+                    const f32x4 n = T::mfma16(odd[kind], one, f32x4{0, 0, 0, 0});
+                    const float v = kind == 0 ? INFINITY : (kind == 1 ? -INFINITY : NAN);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[i][e] = n[e] > 0 ? o[i][e] + v : o[i][e];
+                }
+            }
+            o[i] = T::mfma16(vf, pf, o[i]);
+        }
+    }
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
+
+    // join the waves' parts
+    float *po = (float *)mine;                 // [16][DP + 4]
+#pragma unroll
+    for (int i = 0; i < DT; ++i) *(f32x4 *)(po + col * (DP + 4) + i * 16 + quad * 4) = o[i];
+    if (quad == 0) {
+        part[wave][col][0] = m;
+        part[wave][col][1] = l;
+    }
+    __syncthreads();
+    const int64_t all = p.cache.num_q * p.q_heads;
+    for (int x = threadIdx.x; x < 16 * DP / 4; x += kThreads) {
+        const int r = x / (DP / 4), d = x % (DP / 4) * 4;
+        const int64_t row_ = tile.row0 + r;
+        if (row_ >= tile.rows || d >= p.head_dim) continue;
+        const int64_t q = tile.first + row_ / p.group;
+        const int hd = h * p.group + (int)(row_ % p.group);
+        float mm = -INFINITY, ll = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) mm = fmaxf(mm, part[w][r][0]);
+        const float base = mm == -INFINITY ? 0.0f : mm;
+        f32x4 acc = {0, 0, 0, 0};
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            const float by = exp2_(part[w][r][0] - base);
+            ll += part[w][r][1] * by;
+            const f32x4 y = *(const f32x4 *)((const float *)lds[w] + r * (DP + 4) + d);
+            if (by != 0.0f) acc += y * by;     // a part that saw nothing holds zeros
+        }
+        if (p.splits > 1) {
+            *(f32x4 *)(p.part_o + ((int64_t)split * all + q * p.q_heads + hd) * p.head_dim + d) = acc;
+            if (d == 0) {
+                float *ml = p.part_ml + ((int64_t)split * all + q * p.q_heads + hd) * 2;
+                ml[0] = mm;
+                ml[1] = ll;
+            }
+            continue;
+        }
+        const float by = mm == -INFINITY ? 0.0f : (F8 && p.v_scale ? p.v_scale[h] : 1.0f) / ll;
+        store_out(p, q, hd, d, mm == -INFINITY ? f32x4{0, 0, 0, 0} : acc * by, T::kBf16);
+        if (d == 0 && p.lse) p.lse[q * p.q_heads + hd] = mm == -INFINITY ? -INFINITY : (mm + log2_(ll)) * kLn2;
+    }
+}
+
+// Join the parts of each row: one wave a row.
+template <class T>
+__global__ __launch_bounds__(kThreads) void attention_join_kernel(AttentionParams p) {
+    const int lane = threadIdx.x & 63;
+    const int64_t all = p.cache.num_q * p.q_heads, row = (int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6);
+    if (row >= all) return;
+    const int64_t q = row / p.q_heads;
+    const int head = (int)(row % p.q_heads);
+    float m = -INFINITY, l = 0.0f;
+    if (lane < p.splits) {
+        m = p.part_ml[(lane * all + row) * 2];
+        l = p.part_ml[(lane * all + row) * 2 + 1];
+    }
+    float top = m;
+#pragma unroll
+    for (int x = 1; x < 64; x *= 2) top = fmaxf(top, __shfl_xor(top, x));
+    const float by = top == -INFINITY ? 0.0f : exp2_(m - top);
+    l *= by;
+#pragma unroll
+    for (int x = 1; x < 64; x *= 2) l += __shfl_xor(l, x);
+    const float inv = top == -INFINITY ? 0.0f : (p.v_scale ? p.v_scale[head / p.group] : 1.0f) / l;
+    const int d = lane * 4;                // head_dim is at most 256
+    f32x4 acc = {0, 0, 0, 0};
+    for (int s = 0; s < p.splits; ++s) {
+        const float w = __shfl(by, s);
+        if (w != 0.0f && d < p.head_dim) acc += *(const f32x4 *)(p.part_o + (s * all + row) * p.head_dim + d) * w;
+    }
+    if (d < p.head_dim) store_out(p, q, head, d, top == -INFINITY ? acc : acc * inv, T::kBf16);
+    if (lane == 0 && p.lse) p.lse[row] = top == -INFINITY ? -INFINITY : (top + log2_(l)) * kLn2;
+}
+
+template <class T, bool F8> void (*split_kernel(int head_dim))(AttentionParams) {
+    if (head_dim <= 64) return attention_split_kernel<T, F8, 64>;
+    if constexpr (!F8) {
+        if (head_dim <= 96) return attention_split_kernel<T, F8, 96>;
+    }
+    if (head_dim <= 128) return attention_split_kernel<T, F8, 128>;
+    return attention_split_kernel<T, F8, 256>;
+}
+
+}  // namespace
+}  // namespace tkv
+
+extern "C" {
+
+int kv_paged_attention(const kv_layout *layout, const void *d_layer, const kv_batch *batch, const kv_rows *q,
+                       const kv_rows *out, float scale, int32_t causal, int32_t window, int32_t cache_dtype,
+                       const float *d_k_scale, const float *d_v_scale, float *d_lse, void *d_workspace,
+                       int64_t workspace_bytes, void *stream) {
+    int rc = tkv::check_cache(layout, cache_dtype);
+    if (rc == KV_OK) rc = tkv::check_batch(batch);
+    if (rc == KV_OK) rc = tkv::check_rows(q, batch->num_q, layout->head_dim, false);
+    if (rc == KV_OK) rc = tkv::check_rows(out, batch->num_q, layout->head_dim, true);
+    if (rc != KV_OK) return rc;
+    if (!d_layer || out->dtype != q->dtype || out->heads != q->heads) return KV_EINVAL;
+    if (cache_dtype != KV_F8E4M3 && cache_dtype != q->dtype) return KV_EINVAL;
+    if (!(scale > 0.0f) || !isfinite(scale)) return KV_EINVAL;
+    if (((uintptr_t)d_layer & 15u) || ((uintptr_t)d_lse & 3u) || ((uintptr_t)d_workspace & 15u)) return KV_EALIGN;
+    tkv::AttentionPlan plan;
+    rc = tkv::plan_attention(layout, batch, q->heads, window, &plan);
+    if (rc != KV_OK) return rc;
+    if (plan.workspace > 0 && !d_workspace) return KV_EINVAL;
+    if (plan.workspace > workspace_bytes) return KV_ELIMIT;
+    if (batch->num_q == 0) return KV_OK;
+    const int64_t all = batch->num_q * q->heads;
+    tkv::AttentionParams p;
+    p.cache = tkv::make_paged(layout, d_layer, batch);
+    p.q = (const char *)q->d_data;
+    p.out = (char *)const_cast<void *>(out->d_data);
+    p.q_ts = q->token_stride * 2, p.q_hs = q->head_stride * 2;
+    p.o_ts = out->token_stride * 2, p.o_hs = out->head_stride * 2;
+    p.lse = d_lse;
+    p.part_o = (float *)d_workspace;
+    p.part_ml = p.part_o ? p.part_o + (int64_t)plan.splits * all * layout->head_dim : nullptr;
+    p.k_scale = cache_dtype == KV_F8E4M3 ? d_k_scale : nullptr;
+    p.v_scale = cache_dtype == KV_F8E4M3 ? d_v_scale : nullptr;
+    p.tiles = plan.tiles;
+    p.scale = scale * tkv::kLog2e;
+    p.q_heads = q->heads;
+    p.kv_heads = layout->kv_heads;
+    p.group = q->heads / layout->kv_heads;
+    p.head_dim = layout->head_dim;
+    p.splits = plan.splits;
+    p.window = window;
+    p.causal = causal != 0;
+    const bool bf16 = q->dtype == KV_BF16, f8 = cache_dtype == KV_F8E4M3;
+    const int d = layout->head_dim;
+    auto kernel = bf16 ? (f8 ? tkv::split_kernel<tkv::Bf16, true>(d) : tkv::split_kernel<tkv::Bf16, false>(d))
+                       : (f8 ? tkv::split_kernel<tkv::F16, true>(d) : tkv::split_kernel<tkv::F16, false>(d));
+    hipStream_t s = (hipStream_t)stream;
+    (void)hipGetLastError();
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(plan.tiles * p.kv_heads * p.splits)), dim3(tkv::kThreads), 0, s, p);
+    if (p.splits > 1) {
+        auto join = bf16 ? tkv::attention_join_kernel<tkv::Bf16> : tkv::attention_join_kernel<tkv::F16>;
+        hipLaunchKernelGGL(join, dim3((unsigned)((all + tkv::kWaves - 1) / tkv::kWaves)), dim3(tkv::kThreads), 0, s, p);
+    }
+    return hipGetLastError() == hipSuccess ? KV_OK : KV_EHIP;
+}
+
+}  // extern "C"

@@ -1,5 +1,6 @@
 // host.cpp -- the host-only calls of the C ABI: layout checks, the retrieve
-// planner, host job build, job validation and the commitment rule.  Plain
+// planner, host job build, job validation, the commitment rule, and the checks
+// and launch plan of the operators over the paged cache.  Plain
 // C++ with no HIP header, so that it can also be built and tested on its own
 // (for instance under the address and undefined-behaviour sanitizers).
 
@@ -32,11 +33,113 @@ int check_layout(const kv_layout *lo) {
     return KV_OK;
 }
 
+// Checks shared by the operators over the paged cache.  They address rows in
+// 32-bit units of 16 bytes, hence the limit on a layer's span.
+int check_cache(const kv_layout *lo, int32_t cache_dtype) {
+    const int rc = check_layout(lo);
+    if (rc != KV_OK) return rc;
+    if (cache_dtype != KV_BF16 && cache_dtype != KV_F16 && cache_dtype != KV_F8E4M3) return KV_EINVAL;
+    if (lo->elem_bytes != (cache_dtype == KV_F8E4M3 ? 1 : 2)) return KV_EINVAL;
+    if (lo->head_dim > kMaxHeadDim) return KV_ELIMIT;
+    if (lo->head_dim % 8 != 0 || (lo->head_dim * lo->elem_bytes) % 16 != 0) return KV_EALIGN;
+    return check_span(lo);
+}
+
+int check_span(const kv_layout *lo) {
+    return lo->num_blocks > (int64_t(1) << 36) / lo->paged_block_stride ? KV_ELIMIT : KV_OK;
+}
+
+int check_batch(const kv_batch *b) {
+    if (!b || b->num_reqs < 0 || b->bt_stride <= 0 || b->num_q < 0 || b->max_q_len < 0 || b->max_kv_len < 0)
+        return KV_EINVAL;
+    if (b->num_q > 0 && (b->num_reqs == 0 || !b->d_q_off || !b->d_kv_len || !b->d_block_tables)) return KV_EINVAL;
+    if (((uintptr_t)b->d_q_off & 7u) || ((uintptr_t)b->d_kv_len & 3u) || ((uintptr_t)b->d_block_tables & 3u))
+        return KV_EALIGN;
+    return KV_OK;
+}
+
+int check_rows(const kv_rows *x, int64_t num, int32_t head_dim, bool written) {
+    if (!x || x->heads <= 0 || (x->dtype != KV_BF16 && x->dtype != KV_F16)) return KV_EINVAL;
+    if (num > 0 && !x->d_data) return KV_EINVAL;
+    if (x->token_stride < 0 || x->head_stride < 0) return KV_EINVAL;
+    // rows that are written must not lie on one another
+    if (written && ((x->heads > 1 && x->head_stride < head_dim) || (num > 1 && x->token_stride < head_dim)))
+        return KV_EINVAL;
+    if (((uintptr_t)x->d_data & 15u) || x->token_stride % 8 != 0 || x->head_stride % 8 != 0) return KV_EALIGN;
+    return KV_OK;
+}
+
+// Into how many parts each tile's keys are cut: enough for two workgroups on
+// each compute unit, but no part shorter than one step of its four waves.
+int32_t attention_splits(int64_t tiles, int32_t kv_heads, int64_t span, int32_t step) {
+    const int64_t base = tiles * kv_heads, want = 512;
+    if (base <= 0 || base >= want) return 1;
+    int64_t parts = want / base;
+    const int64_t most = (span + step - 1) / step;
+    if (parts > most) parts = most;
+    if (parts > kMaxSplits) parts = kMaxSplits;
+    return parts < 1 ? 1 : (int32_t)parts;
+}
+
+int plan_attention(const kv_layout *lo, const kv_batch *b, int32_t q_heads, int32_t window, AttentionPlan *plan) {
+    if (q_heads <= 0 || q_heads % lo->kv_heads != 0 || window < 0) return KV_EINVAL;
+    const int64_t group = q_heads / lo->kv_heads;
+    if (b->num_q > (int64_t(1) << 40) / q_heads) return KV_ELIMIT;
+    int64_t span = b->max_kv_len;
+    if (window > 0 && span > (int64_t)window + b->max_q_len) span = (int64_t)window + b->max_q_len;
+    plan->tiles = b->num_q * group / kSplitRows + b->num_reqs;
+    plan->splits = attention_splits(plan->tiles, lo->kv_heads, span, kSplitStep);
+    plan->workspace = plan->splits > 1 ? (int64_t)plan->splits * b->num_q * q_heads * (lo->head_dim + 2) * 4 : 0;
+    if (plan->tiles * lo->kv_heads * plan->splits >= (int64_t(1) << 31)) return KV_ELIMIT;
+    return KV_OK;
+}
+
 }  // namespace tkv
 
 using tkv::check_layout;
 
 extern "C" {
+
+int kv_rope_frequencies(int32_t rot_dim, double base, int32_t scaling, double factor, double context, double low,
+                        double high, double *h_freqs, float *magnitude) {
+    if (rot_dim < 0 || rot_dim % 2 != 0 || (rot_dim > 0 && !h_freqs) || !magnitude) return KV_EINVAL;
+    if (!(base > 1.0) || !isfinite(base)) return KV_EINVAL;
+    if (scaling < KV_ROPE_PLAIN || scaling > KV_ROPE_RAMP) return KV_EINVAL;
+    if (scaling != KV_ROPE_PLAIN && (!(factor >= 1.0) || !isfinite(factor))) return KV_EINVAL;
+    if (scaling == KV_ROPE_RAMP && (!(context > 0.0) || !isfinite(context) || !isfinite(low) || !(high > low) ||
+                                    !isfinite(high)))
+        return KV_EINVAL;
+    if (scaling == KV_ROPE_BASE) {
+        if (rot_dim <= 2) return KV_EINVAL;
+        base *= pow(factor, (double)rot_dim / (rot_dim - 2));
+    }
+    const double two_pi = 6.283185307179586476925;
+    for (int32_t i = 0; i < rot_dim / 2; ++i) {
+        double f = pow(base, -2.0 * i / rot_dim);
+        if (scaling == KV_ROPE_LINEAR) f /= factor;
+        if (scaling == KV_ROPE_RAMP) {
+            double keep = (context * f / two_pi - low) / (high - low);
+            keep = keep < 0.0 ? 0.0 : (keep > 1.0 ? 1.0 : keep);
+            f *= keep + (1.0 - keep) / factor;
+        }
+        h_freqs[i] = f;
+    }
+    *magnitude = scaling == KV_ROPE_RAMP ? (float)(0.1 * log(factor) + 1.0) : 1.0f;
+    return KV_OK;
+}
+
+int kv_paged_attention_workspace(const kv_layout *layout, const kv_batch *batch, int32_t q_heads, int32_t window,
+                                 int64_t *bytes) {
+    int rc = check_layout(layout);
+    if (rc == KV_OK) rc = tkv::check_batch(batch);
+    if (rc != KV_OK) return rc;
+    if (!bytes) return KV_EINVAL;
+    tkv::AttentionPlan plan;
+    rc = tkv::plan_attention(layout, batch, q_heads, window, &plan);
+    if (rc != KV_OK) return rc;
+    *bytes = plan.workspace;
+    return KV_OK;
+}
 
 int kv_retrieve_plan(const kv_layout *layout, const kv_job *h_jobs, int32_t num_jobs) {
     const int rc = check_layout(layout);
@@ -280,7 +383,7 @@ const char *kv_strerror(int status) {
     case KV_ENOSPC: return "no free staging slot or index full";
     case KV_EHIP: return "HIP runtime error";
     case KV_EDUP: return "duplicate destination within one batch";
-    case KV_ELIMIT: return "request exceeds a fixed capacity of the allocation-free call";
+    case KV_ELIMIT: return "request exceeds a fixed capacity of the call";
     default: return "unknown status";
     }
 }

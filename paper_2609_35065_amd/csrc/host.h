@@ -12,4 +12,23 @@ namespace tkv {
 // a negative kv_status.
 int check_layout(const kv_layout *lo);
 
+// Operators over the paged cache: checks of their arguments, and the launch
+// plan of the attention.
+constexpr int kMaxHeadDim = 256;
+constexpr int kSplitRows = 16;      // rows (query, head of the group) of an attention tile
+constexpr int kSplitStep = 128;     // keys that the waves of a workgroup take in one step
+constexpr int kMaxSplits = 64;
+
+struct AttentionPlan {
+    int64_t tiles;        // row tiles, each for every KV head
+    int32_t splits;       // parts that a tile's keys are cut into
+    int64_t workspace;    // bytes
+};
+
+int check_cache(const kv_layout *lo, int32_t cache_dtype);
+int check_span(const kv_layout *lo);
+int check_batch(const kv_batch *b);
+int check_rows(const kv_rows *x, int64_t num, int32_t head_dim, bool written);
+int plan_attention(const kv_layout *lo, const kv_batch *b, int32_t q_heads, int32_t window, AttentionPlan *plan);
+
 }  // namespace tkv

@@ -1,0 +1,121 @@
+// mfma.h -- the two 16-bit element types as the matrix units take them.
+#pragma once
+
+#include "paged.h"
+
+namespace tkv {
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+
+__device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ __forceinline__ float log2_(float x) { return __builtin_amdgcn_logf(x); }
+
+// Bits of the non-finite values among a register's two elements, `exponent`
+// being all ones in each: 0xffff for an element that is not finite.
+template <uint32_t kExponent> __device__ __forceinline__ uint32_t nonfinite_mask(uint32_t x) {
+    const uint32_t lo = (x & (kExponent & 0xffffu)) == (kExponent & 0xffffu) ? 0xffffu : 0u;
+    const uint32_t hi = (x & (kExponent & 0xffff0000u)) == (kExponent & 0xffff0000u) ? 0xffff0000u : 0u;
+    return lo | hi;
+}
+
+// Take the non-finite elements out of an operand.  Where there are any in the
+// wave, odd[0..2] hold ones at its +inf, -inf and NaN elements.
+template <uint32_t kExponent, uint32_t kOne>
+__device__ __forceinline__ bool take_nonfinite_(u32x4 &v, u32x4 odd[3]) {
+    u32x4 bad;
+    uint32_t any = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        bad[i] = nonfinite_mask<kExponent>(v[i]);
+        any |= bad[i];
+    }
+    if (!__any(any != 0)) return false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        uint32_t kind[3] = {0, 0, 0};
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const uint32_t at = 0xffffu << (16 * e), x = v[i] & at, one = kOne & at;
+            if (!(bad[i] & at)) continue;
+            const uint32_t inf = kExponent & at, sign = 0x80008000u & at;
+            kind[x == inf ? 0 : (x == (inf | sign) ? 1 : 2)] |= one;
+        }
+        odd[0][i] = kind[0];
+        odd[1][i] = kind[1];
+        odd[2][i] = kind[2];
+        v[i] &= ~bad[i];
+    }
+    return true;
+}
+
+struct Bf16 {
+    static constexpr bool kBf16 = true;
+    static constexpr uint32_t kOne = 0x3f803f80u;
+    static __device__ __forceinline__ f32x4 mfma16(u32x4 a, u32x4 b, f32x4 c) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c,
+                                                       0, 0, 0);
+    }
+    static __device__ __forceinline__ f32x16 mfma32(u32x4 a, u32x4 b, f32x16 c) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c,
+                                                       0, 0, 0);
+    }
+    static __device__ __forceinline__ uint32_t pack(float a, float b) {   // to nearest even
+        const bf16x2 x = {(__bf16)a, (__bf16)b};
+        return __builtin_bit_cast(uint32_t, x);
+    }
+    static __device__ __forceinline__ uint32_t from_f8(uint32_t x, bool high) {   // exact
+        return __builtin_bit_cast(uint32_t, high ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, 1.0f, true)
+                                                 : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, 1.0f, false));
+    }
+    static __device__ __forceinline__ uint32_t pair(bool a, bool b) { return (a ? 0x3f80u : 0u) | (b ? 0x3f800000u : 0u); }
+    static __device__ __forceinline__ bool take_nonfinite(u32x4 &v, u32x4 odd[3]) {
+        return take_nonfinite_<0x7f807f80u, kOne>(v, odd);
+    }
+};
+
+struct F16 {
+    static constexpr bool kBf16 = false;
+    static constexpr uint32_t kOne = 0x3c003c00u;
+    static __device__ __forceinline__ f32x4 mfma16(u32x4 a, u32x4 b, f32x4 c) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0,
+                                                      0, 0);
+    }
+    static __device__ __forceinline__ f32x16 mfma32(u32x4 a, u32x4 b, f32x16 c) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0,
+                                                      0, 0);
+    }
+    static __device__ __forceinline__ uint32_t pack(float a, float b) {   // to nearest even
+        const f16x2 x = {(_Float16)a, (_Float16)b};
+        return __builtin_bit_cast(uint32_t, x);
+    }
+    static __device__ __forceinline__ uint32_t from_f8(uint32_t x, bool high) {   // exact
+        return __builtin_bit_cast(uint32_t, high ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(x, 1.0f, true)
+                                                 : __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(x, 1.0f, false));
+    }
+    static __device__ __forceinline__ uint32_t pair(bool a, bool b) { return (a ? 0x3c00u : 0u) | (b ? 0x3c000000u : 0u); }
+    static __device__ __forceinline__ bool take_nonfinite(u32x4 &v, u32x4 odd[3]) {
+        return take_nonfinite_<0x7c007c00u, kOne>(v, odd);
+    }
+};
+
+template <class T> __device__ __forceinline__ uint32_t pack2(float a, float b) { return T::pack(a, b); }
+
+// Eight elements of the 8-bit type.
+template <class T> __device__ __forceinline__ u32x4 unpack8(uint32_t a, uint32_t b) {
+    return u32x4{T::from_f8(a, false), T::from_f8(a, true), T::from_f8(b, false), T::from_f8(b, true)};
+}
+
+// Transposing read from LDS.  Of each 16 lanes, lane s gives the address of
+// four consecutive 16-bit elements, 4 (s % 4) .. of row s / 4; lane s gets
+// element s of the four rows.
+__device__ __forceinline__ u32x2 read_transposed(const char *at) {
+    const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+        (__attribute__((address_space(3))) s16x4 *)const_cast<char *>(at));
+    return __builtin_bit_cast(u32x2, x);
+}
+
+}  // namespace tkv

@@ -1,0 +1,216 @@
+"""kv_paged_attention against the definition in 64 bits: lengths from none to
+several tiles, odd head sizes and groups, both layouts, missing blocks, rows
+that see nothing, windows, strided queries, and masked places that hold
+infinities and NaN."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paged_ref as ref
+import paper_2609_35065_amd as kv
+
+pytestmark = pytest.mark.gpu
+F8 = torch.float8_e4m3fn
+
+
+def _run(c, new, q, scale, causal=True, window=0, lse=True, max_q=None, max_kv=None, gap=0):
+    c.device()
+    b = c.batch(new, max_q, max_kv)
+    dq = q.cuda() if q.is_contiguous() else torch.empty_strided(q.shape, q.stride(), dtype=q.dtype, device="cuda").copy_(q)
+    wide = torch.full((q.shape[0], q.shape[1] + gap, q.shape[2]), 7.0, dtype=q.dtype, device="cuda")
+    out = wide[:, :q.shape[1]]
+    d_lse = torch.full(q.shape[:2], 7.0, device="cuda") if lse else None
+    size = kv.kv_paged_attention_workspace(c.layout, b, q.shape[1], window)
+    ws = torch.full((size,), 0xff, dtype=torch.uint8, device="cuda") if size else None
+    kv.kv_paged_attention(c.layout, c.d_pool[0], b, dq, out, scale, causal=causal, window=window, lse=d_lse,
+                          k_scale=c.d_scales[0], v_scale=c.d_scales[1], workspace=ws)
+    torch.cuda.synchronize()
+    if gap:
+        assert bool((wide[:, q.shape[1]:] == 7.0).all())
+    return out, d_lse
+
+
+def _check(c, new, q, scale, **kw):
+    out, lse = _run(c, new, q, scale, **kw)
+    want, tol, wl, lt = ref.attention(c, new, q, scale, kw.get("causal", True), kw.get("window", 0))
+    ref.assert_within(out, want, tol, "out")
+    if lse is not None:
+        ref.assert_within(lse, wl, lt, "lse")
+    return out
+
+
+# (lengths in the cache, new tokens)
+BATCHES = {
+    "one": ([1], [1]), "decode": ([1001], [1]), "decode-ragged": ([1, 15, 16, 17, 31, 32, 33, 500], [1] * 8),
+    "none-new": ([40, 0, 33], [0, 0, 5]), "empty-cache": ([0, 20, 0], [3, 2, 1]), "all-new": ([77], [77]),
+    "chunks": ([130, 257, 64], [65, 257, 1]), "more-new-than-cache": ([5], [9]), "mixed": ([300, 90, 600, 31], [1, 40, 200, 31]),
+    "long": ([2500], [130]),
+}
+
+
+@pytest.mark.parametrize("name", sorted(BATCHES))
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16, F8], ids=["bf16", "f16", "f8"])
+def test_batches(name, dtype):
+    lengths, new = BATCHES[name]
+    c = ref.Cache(lengths, heads=2, dim=128, dtype=dtype, seed=len(name))
+    q = ref.rows_of(sum(new), 8, 128, c.q_dtype, c.gen, 1.5)
+    _check(c, new, q, 128 ** -0.5)
+
+
+@pytest.mark.parametrize("dim", [8, 16, 40, 64, 72, 80, 96, 112, 128, 136, 192, 256])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, F8], ids=["bf16", "f8"])
+def test_head_sizes(dim, dtype):
+    if dtype == F8 and dim % 16:
+        pytest.skip("rows of an 8-bit cache are whole 16-byte units")
+    c = ref.Cache([200, 75], heads=2, dim=dim, dtype=dtype, seed=dim, layout="block_first")
+    q = ref.rows_of(80, 4, dim, c.q_dtype, c.gen, 1.5)
+    _check(c, [70, 10], q, dim ** -0.5)
+
+
+@pytest.mark.parametrize("heads,group", [(1, 1), (1, 71), (3, 3), (2, 6), (5, 1), (8, 4), (2, 16), (1, 32)])
+@pytest.mark.parametrize("new", [[1, 1], [50, 3]], ids=["decode", "chunk"])
+def test_groups(heads, group, new):
+    c = ref.Cache([150, 90], heads=heads, dim=64, dtype=torch.float16, seed=heads * 100 + group)
+    q = ref.rows_of(sum(new), heads * group, 64, torch.float16, c.gen, 2.0)
+    _check(c, new, q, 0.125)
+
+
+@pytest.mark.parametrize("block", [1, 3, 16, 20, 32, 128])
+@pytest.mark.parametrize("layout,pad", [("kv_first", 0), ("block_first", 0), ("kv_first", 48), ("block_first", 16)])
+def test_blocks_and_layouts(block, layout, pad):
+    c = ref.Cache([333, 128, 47], heads=2, dim=64, block=block, layout=layout, pad=pad, seed=block, table_pad=2)
+    q = ref.rows_of(60, 4, 64, torch.bfloat16, c.gen)
+    _check(c, [1, 50, 9], q, 0.2)
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("window", [0, 1, 7, 64, 200, 10000])
+def test_windows(causal, window):
+    c = ref.Cache([400, 129, 33], heads=2, dim=64, seed=window)
+    q = ref.rows_of(250, 4, 64, torch.bfloat16, c.gen)
+    _check(c, [220, 1, 29], q, 0.125, causal=causal, window=window)
+
+
+@pytest.mark.parametrize("new", [[1, 1, 1], [60, 90, 5]], ids=["decode", "chunk"])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, F8], ids=["bf16", "f8"])
+def test_missing_blocks(new, dtype):
+    c = ref.Cache([300, 96, 40], heads=2, dim=64, dtype=dtype, seed=5)
+    c.bt[0, 2] = -1
+    c.bt[0, 5:9] = c.num_blocks          # ids out of range, one of them larger than any index
+    c.bt[0, 9] = 2 ** 31 - 1
+    c.bt[1, :] = -7                       # nothing of this request is there
+    c.bt = np.ascontiguousarray(c.bt[:, :17])   # the first request's last blocks lie past the table
+    q = ref.rows_of(sum(new), 4, 64, c.q_dtype, c.gen)
+    out = _check(c, new, q, 0.125)
+    assert bool((out[new[0]:new[0] + new[1]] == 0).all())
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16], ids=["bf16", "f16"])
+@pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan], ids=["inf", "-inf", "nan"])
+@pytest.mark.parametrize("new,window", [([1], 0), ([1], 50), ([64], 0), ([150], 40)])
+def test_what_a_row_does_not_see_does_not_reach_it(dtype, bad, new, window):
+    """K and V of unused blocks, of the block's end past the length, of later tokens and of tokens before the window
+    hold values that are not finite; what rows do see of them, they get."""
+    n, T = new[0], 201
+    c = ref.Cache([T], heads=2, dim=64, dtype=dtype, seed=11)
+    used = set(c.bt[0].tolist())
+    for p in (0, 1):
+        x = c.view(p)
+        for b in range(c.num_blocks):
+            if b not in used:
+                x[b] = bad
+        x[int(c.bt[0, -1]), T % 16:] = bad
+        if window:
+            for t in range(0, T - n - window + 1, 3):
+                x[int(c.bt[0, t // 16]), t % 16] = bad
+    v = c.view(1)
+    if n > 1:
+        for t in (T - n // 2, T - 3, T - 2):   # seen by the rows from t on
+            v[int(c.bt[0, t // 16]), t % 16, 1, 5:9] = bad
+    q = ref.rows_of(n, 4, 64, dtype, c.gen)
+    out = _check(c, new, q, 0.125, window=window)
+    assert bool(out[0].isfinite().all())
+
+
+def test_extreme_scores():
+    """Maxima that grow late and far, and scores that leave one key."""
+    for dtype in (torch.bfloat16, torch.float16):
+        c = ref.Cache([500], heads=1, dim=64, dtype=dtype, seed=3)
+        k = c.view(0)
+        for t in range(0, 500, 50):
+            k[int(c.bt[0, t // 16]), t % 16] *= 1 + t / 25
+        q = ref.rows_of(40, 4, 64, dtype, c.gen, 4.0)
+        _check(c, [40], q, 0.5)
+        _check(c, [40], q * 0 - 3, 0.5)
+
+
+def test_strided_rows_and_optional_lse():
+    c = ref.Cache([90, 40], heads=2, dim=80, seed=9)
+    q = ref.rows_of(31, 4, 80, torch.bfloat16, c.gen, gap=4)
+    out = _check(c, [30, 1], q, 0.1, gap=3)
+    again, lse = _run(c, [30, 1], q.contiguous(), 0.1, lse=False)
+    assert lse is None and torch.equal(out, again)
+    # head-major queries: [heads, n, dim] seen as [n, heads, dim]
+    turned = q.transpose(0, 1).contiguous().transpose(0, 1)
+    again, _ = _run(c, [30, 1], turned, 0.1)
+    assert torch.equal(out, again)
+
+
+@pytest.mark.parametrize("max_q,max_kv", [(0, 0), (1, 1), (1, 1 << 20), (5000, 3), (5000, 1 << 20)])
+def test_hints_do_not_change_results(max_q, max_kv):
+    c = ref.Cache([700, 90, 31], heads=2, dim=64, seed=21)
+    q = ref.rows_of(102, 4, 64, torch.bfloat16, c.gen)
+    _check(c, [1, 90, 11], q, 0.125, max_q=max_q, max_kv=max_kv)
+
+
+def test_split_keys_are_deterministic():
+    c = ref.Cache([4001], heads=2, dim=128, seed=2)
+    q = ref.rows_of(1, 8, 128, torch.bfloat16, c.gen, 1.5)
+    c.device()
+    assert kv.kv_paged_attention_workspace(c.layout, c.batch([1]), 8) > 0
+    first, lse = _run(c, [1], q, 128 ** -0.5)
+    for _ in range(5):
+        again, l2 = _run(c, [1], q, 128 ** -0.5)
+        assert torch.equal(first, again) and torch.equal(lse, l2)
+
+
+def test_no_rows():
+    c = ref.Cache([33], heads=2, dim=64, seed=2)
+    q = ref.rows_of(0, 4, 64, torch.bfloat16, c.gen)
+    _run(c, [0], q, 0.125)
+
+
+def test_many_requests():
+    rng = np.random.default_rng(4)
+    lengths = rng.integers(0, 60, 300)
+    new = np.minimum(rng.integers(0, 4, 300), lengths)
+    c = ref.Cache(lengths, heads=1, dim=64, seed=8)
+    q = ref.rows_of(int(new.sum()), 4, 64, torch.bfloat16, c.gen)
+    _check(c, new.tolist(), q, 0.125)
+
+
+def test_another_stream_and_graph_replays():
+    c = ref.Cache([513, 40], heads=2, dim=128, seed=6)
+    new = [1, 1]
+    q = ref.rows_of(2, 8, 128, torch.bfloat16, c.gen)
+    want, lse = _run(c, new, q, 0.1)
+    b, pool = c.batch(new), c.d_pool[0]   # the graph's own: each eager run has another copy
+    dq, out = q.cuda(), torch.zeros(2, 8, 128, dtype=torch.bfloat16, device="cuda")
+    ws = torch.empty(kv.kv_paged_attention_workspace(c.layout, b, 8), dtype=torch.uint8, device="cuda")
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    kv.kv_paged_attention(c.layout, pool, b, dq, out, 0.1, workspace=ws, stream=side)
+    side.synchronize()
+    assert torch.equal(out, want)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        kv.kv_paged_attention(c.layout, pool, b, dq, out, 0.1, workspace=ws)
+    for x in range(4):
+        dq.copy_((q * (x + 1)).to(dq.dtype))
+        eager, _ = _run(c, new, dq.cpu(), 0.1)
+        out.zero_()
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, eager), x
