@@ -20,6 +20,7 @@ constexpr int kWaves = 4;
 constexpr int kThreads = 64 * kWaves;
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 static_assert(kSplitStep == 32 * kWaves, "a wave takes 32 keys a step");
+static_assert(kTileRows == 32 * kWaves && kTileStep == 64, "four waves of 32 rows");
 
 struct AttentionParams {
     Paged cache;
@@ -74,6 +75,15 @@ __device__ __forceinline__ void store_out(const AttentionParams &p, int64_t row,
     *(u32x2 *)to = y;
 }
 
+// One element of the cache.
+template <class T, bool F8> __device__ __forceinline__ float load_one(const char *row, int d) {
+    if constexpr (F8) return T::to_f32(T::from_f8(*(const uint8_t *)(row + d), false));
+    return T::to_f32(*(const uint16_t *)(row + d * 2));
+}
+
+// Bytes of LDS that a body needs.
+template <int DP> constexpr int kSplitLds = kWaves * 32 * (DP * 2 + 32);
+
 // Tiles of 16 rows; the keys of a tile are cut into p.splits parts, one
 // workgroup each, and a part's steps of 32 keys go to its waves in turn.
 // S^T = K Q^T leaves a lane with the scores of one row (lane % 16) for the
@@ -83,20 +93,14 @@ __device__ __forceinline__ void store_out(const AttentionParams &p, int64_t row,
 // matrix operand itself; V goes through LDS, the wave's own, to be read
 // transposed.
 template <class T, bool F8, int DP>
-__global__ __launch_bounds__(kThreads) void attention_split_kernel(AttentionParams p) {
+__device__ __forceinline__ void few_rows(const AttentionParams &p, const Tile &tile, int h, int split, char *lds,
+                                         float (*part)[16][2]) {
     constexpr int KS = DP / 32, DT = DP / 16;
     constexpr int kRow = DP * 2 + 32;          // bytes of an LDS row: 8 rows lie on different banks
     constexpr int VEC = F8 ? 16 : 8;           // elements of a 16-byte vector of the cache
     constexpr int VPR = DP / VEC;              // vectors of a row
     constexpr int VL = 32 * VPR / 64;          // vectors a lane stages
-    __shared__ __align__(16) char lds[kWaves][32 * kRow];
-    __shared__ float part[kWaves][16][2];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, quad = lane >> 4;
-    const int64_t id = blockIdx.x;
-    const int h = (int)(id % p.kv_heads);
-    const int split = (int)(id / p.kv_heads % p.splits);
-    const Tile tile = find_tile(p.cache, id / p.kv_heads / p.splits, p.group, 16);
-    if (tile.row0 >= tile.rows) return;
 
     // this lane's row
     const int64_t myrow = tile.row0 + col;
@@ -131,7 +135,7 @@ __global__ __launch_bounds__(kThreads) void attention_split_kernel(AttentionPara
     const float c = p.scale * (F8 && p.k_scale ? p.k_scale[h] : 1.0f);
     const char *kbase = p.cache.layer + (int64_t)h * p.cache.head_bytes;
     const char *vbase = kbase + p.cache.kv_stride;
-    char *mine = lds[wave];
+    char *mine = lds + wave * 32 * kRow;
 
     f32x4 o[DT];
 #pragma unroll
@@ -267,7 +271,7 @@ __global__ __launch_bounds__(kThreads) void attention_split_kernel(AttentionPara
         for (int w = 0; w < kWaves; ++w) {
             const float by = exp2_(part[w][r][0] - base);
             ll += part[w][r][1] * by;
-            const f32x4 y = *(const f32x4 *)((const float *)lds[w] + r * (DP + 4) + d);
+            const f32x4 y = *(const f32x4 *)((const float *)(lds + w * 32 * kRow) + r * (DP + 4) + d);
             if (by != 0.0f) acc += y * by;     // a part that saw nothing holds zeros
         }
         if (p.splits > 1) {
@@ -283,6 +287,279 @@ __global__ __launch_bounds__(kThreads) void attention_split_kernel(AttentionPara
         store_out(p, q, hd, d, mm == -INFINITY ? f32x4{0, 0, 0, 0} : acc * by, T::kBf16);
         if (d == 0 && p.lse) p.lse[q * p.q_heads + hd] = mm == -INFINITY ? -INFINITY : (mm + log2_(ll)) * kLn2;
     }
+}
+
+// Tiles of 128 rows, 32 a wave, over steps of 64 keys.  K and V of a step go
+// through LDS for all four waves, one step ahead: loaded into registers while
+// the step before is computed, written to the other buffer, one barrier.
+// Again S^T = K Q^T and O^T = V^T P^T, with 32 x 32 products: a lane holds
+// one row's scores for half of the keys, so that a row's maximum and sum need
+// one exchange between lanes.
+//
+// The running maximum may lag: o and l are only scaled when some row's
+// maximum has grown by more than 2^kLag since it was last taken.  Until then
+// exponentials reach 2^kLag instead of 1, which costs no precision, neither in
+// l and o (32 bits) nor in P (a rounding relative to its size; 2^8 is far
+// below the 16-bit types' ends).
+constexpr float kLag = 8.0f;
+constexpr int kRows = 32 * kWaves, kStep = 64;
+template <int DP> constexpr int kKeyRow = DP * 2 + 16;     // bytes of an LDS row of K: 8 rows on different banks
+template <int DP> constexpr int kValueRow = DP * 2 + (DP * 2 % 128 ? 0 : 64);   // of V: 4 rows, 64 bytes of each
+template <int DP> constexpr int kTileLds = 2 * kStep * (kKeyRow<DP> + kValueRow<DP>);
+
+template <class T, bool F8, int DP>
+__device__ __forceinline__ void many_rows(const AttentionParams &p, const Tile &tile, int h, int split, char *lds,
+                                          int *odd) {
+    constexpr int KS = DP / 16, DT = DP / 32;
+    constexpr int VEC = F8 ? 16 : 8, VPR = DP / VEC, VL = kStep * VPR / kThreads;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 31, half = lane >> 5;
+    char *const kbuf = lds, *const vbuf = lds + 2 * kStep * kKeyRow<DP>;
+
+    const int64_t wrow = tile.row0 + wave * 32, myrow = wrow + col;
+    const bool have = myrow < tile.rows, active = wrow < tile.rows;
+    const int64_t token = have ? myrow / p.group : 0;
+    const int head = h * p.group + (int)(have ? myrow % p.group : 0);
+    const int32_t len_raw = p.cache.kv_len[tile.req];
+    const int64_t len = min((int64_t)(len_raw < 0 ? 0 : len_raw), (int64_t)p.cache.bt_stride * p.cache.block_size);
+    const int64_t ahead = len_raw - tile.rows / p.group;       // cache index of the first token
+    // keys that rows see, lo <= j < hi: this lane's, those that all or any of the wave's rows see, those of the tile
+    const auto hi_of = [&](int64_t tok) { return (int)max((int64_t)0, p.causal ? min(len, ahead + tok + 1) : len); };
+    const auto lo_of = [&](int64_t tok) { return (int)(p.window > 0 ? max((int64_t)0, ahead + tok - p.window + 1) : 0); };
+    const int hi = have ? hi_of(token) : 0, lo = lo_of(token);
+    const int64_t wfirst = wrow / p.group, wlast = min(wrow + 31, tile.rows - 1) / p.group;
+    const int all_hi = hi_of(wfirst), all_lo = lo_of(wlast), any_hi = active ? hi_of(wlast) : 0, any_lo = lo_of(wfirst);
+    const int end = hi_of(min(tile.row0 + kRows - 1, tile.rows - 1) / p.group);
+    const int begin = lo_of(tile.row0 / p.group) & ~(kStep - 1);
+    const int steps = end > begin ? (end - begin + kStep - 1) / kStep : 0;
+    const int step0 = (int)((int64_t)steps * split / p.splits), step1 = (int)((int64_t)steps * (split + 1) / p.splits);
+
+    u32x4 qf[KS];
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+        const int d = ks * 16 + half * 8;
+        qf[ks] = u32x4{0, 0, 0, 0};
+        if (have && d < p.head_dim) qf[ks] = *(const u32x4 *)(p.q + (tile.first + token) * p.q_ts + head * p.q_hs + d * 2);
+    }
+    const float c = p.scale * (F8 && p.k_scale ? p.k_scale[h] : 1.0f);
+    const char *kbase = p.cache.layer + (int64_t)h * p.cache.head_bytes;
+    const char *vbase = kbase + p.cache.kv_stride;
+
+    const int tile_hi = hi_of(tile.row0 / p.group), tile_lo = lo_of(min(tile.row0 + kRows - 1, tile.rows - 1) / p.group);
+    uint64_t there = 0, there_next = 0;        // bit k: key k of the step is in the cache
+    const auto is_mixed = [&](uint64_t there, int t0) { return there != ~uint64_t(0) || t0 < tile_lo || t0 + kStep > tile_hi; };
+    if (tid == 0) *odd = 0;
+    __syncthreads();
+
+    // staging: one lane looks up one key of a step; vectors x = i kThreads + tid
+    u32x4 kreg[VL], vreg[VL];
+    int32_t id = -1;
+    uint32_t id_row = 0;
+    const auto look_up = [&](int step) {
+        const int t = begin + step * kStep + lane;
+        id = step < step1 && t < end ? block_of(p.cache, tile.req, (uint32_t)t, id_row) : -1;
+    };
+    const auto load = [&]() {
+        const uint32_t off = id < 0 ? 0u : (uint32_t)id * p.cache.block16 + id_row * p.cache.row16;
+        there_next = __ballot(id >= 0);
+#pragma unroll
+        for (int i = 0; i < VL; ++i) {
+            const int x = i * kThreads + tid, r = x / VPR, vec = x % VPR;
+            const int64_t at = ((int64_t)(uint32_t)__shfl((int)off, r) << 4) + vec * 16;
+            const bool in = vec * VEC < p.head_dim;
+            kreg[i] = in ? *(const u32x4 *)(kbase + at) : u32x4{0, 0, 0, 0};
+            vreg[i] = in ? *(const u32x4 *)(vbase + at) : u32x4{0, 0, 0, 0};
+        }
+    };
+    // A value that is not finite must reach only the rows that see its key: 0 times it is NaN.  In a step that some
+    // row does not see whole, such values are staged as 0; add_nonfinite adds them to the results that do see them.
+    const auto stage = [&](int buf, int step) {
+        const int t0 = begin + step * kStep;
+        const bool mixed = is_mixed(there_next, t0);
+#pragma unroll
+        for (int i = 0; i < VL; ++i) {
+            const int x = i * kThreads + tid, r = x / VPR, vec = x % VPR;
+            char *k = kbuf + (buf * kStep + r) * kKeyRow<DP> + vec * VEC * 2;
+            char *v = vbuf + (buf * kStep + r) * kValueRow<DP> + vec * VEC * 2;
+            u32x4 y[F8 ? 2 : 1];
+            if constexpr (F8) {
+                *(u32x4 *)k = unpack8<T>(kreg[i][0], kreg[i][1]);
+                *(u32x4 *)(k + 16) = unpack8<T>(kreg[i][2], kreg[i][3]);
+                y[0] = unpack8<T>(vreg[i][0], vreg[i][1]);
+                y[1] = unpack8<T>(vreg[i][2], vreg[i][3]);
+            } else {
+                *(u32x4 *)k = kreg[i];
+                y[0] = vreg[i];
+            }
+#pragma unroll
+            for (int j = 0; j < (F8 ? 2 : 1); ++j) {
+                if (mixed && T::drop_nonfinite(y[j])) *odd = 1;
+                *(u32x4 *)(v + j * 16) = y[j];
+            }
+        }
+    };
+
+    f32x16 o[DT];
+#pragma unroll
+    for (int i = 0; i < DT; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[i][e] = 0.0f;
+    float m = -INFINITY, base = 0.0f, l = 0.0f;
+
+    look_up(step0);
+    if (step0 < step1) load();
+    look_up(step0 + 1);
+    for (int step = step0; step < step1; ++step) {
+        const int buf = (step - step0) & 1;
+        stage(buf, step);
+        there = there_next;
+        __syncthreads();
+        if (step + 1 < step1) load();
+        look_up(step + 2);
+        const int t0 = begin + step * kStep;
+        if (t0 >= any_hi || t0 + kStep <= any_lo || !there) continue;
+
+        f32x16 s[2];
+        const char *kat = kbuf + (buf * kStep + col) * kKeyRow<DP> + half * 16;
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) s[x][e] = 0.0f;
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks)
+                s[x] = T::mfma32(*(const u32x4 *)(kat + x * 32 * kKeyRow<DP> + ks * 32), qf[ks], s[x]);
+        }
+        const bool whole = there == ~uint64_t(0) && t0 >= all_lo && t0 + kStep <= all_hi;
+        if (!whole) {
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int k = x * 32 + 8 * (i / 4) + 4 * half + i % 4;
+                    if (!((there >> k) & 1) || t0 + k < lo || t0 + k >= hi) s[x][i] = -INFINITY;
+                }
+        }
+        float top = s[0][0];
+#pragma unroll
+        for (int i = 1; i < 16; ++i) top = fmaxf(top, s[0][i]);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) top = fmaxf(top, s[1][i]);
+        const f32x2 tops = both_halves(top);
+        top = fmaxf(tops[0], tops[1]) * c;
+        if (__any(top > m + kLag)) {
+            const float m1 = fmaxf(m, top), b1 = m1 == -INFINITY ? 0.0f : m1, fade = exp2_(m - b1);
+            m = m1;
+            base = b1;
+            l *= fade;
+#pragma unroll
+            for (int i = 0; i < DT; ++i)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) o[i][e] *= fade;
+        }
+        u32x4 pf[4];
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+            for (int i = 0; i < 16; i += 2) {
+                const float a = exp2_(__builtin_fmaf(s[x][i], c, -base)), b = exp2_(__builtin_fmaf(s[x][i + 1], c, -base));
+                l += a;
+                l += b;
+                pf[x * 2 + i / 8][i / 2 % 4] = pack2<T>(a, b);
+            }
+        const char *vat = vbuf + (buf * kStep + half * 4 + (lane >> 2 & 3)) * kValueRow<DP> + (lane >> 4 & 1) * 32 + (lane & 3) * 8;
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk)
+#pragma unroll
+            for (int i = 0; i < DT; ++i) {
+                const char *at = vat + kk * 16 * kValueRow<DP> + i * 64;
+                const u32x2 a = read_transposed(at), b = read_transposed(at + 8 * kValueRow<DP>);
+                o[i] = T::mfma32(u32x4{a[0], a[1], b[0], b[1]}, pf[kk], o[i]);
+            }
+    }
+    const f32x2 ls = both_halves(l);
+    l = ls[0] + ls[1];
+
+    const int64_t row = tile.first + token, at = row * p.q_heads + head;
+    float *const to32 = p.part_o + ((int64_t)split * p.cache.num_q * p.q_heads + at) * p.head_dim;
+    char *const to = p.out + row * p.o_ts + head * p.o_hs;
+    if (p.splits > 1) {
+#pragma unroll
+        for (int i = 0; i < DT; ++i)
+#pragma unroll
+            for (int e = 0; e < 16; e += 4) {
+                const int d = i * 32 + e * 2 + half * 4;
+                if (have && d < p.head_dim) *(f32x4 *)(to32 + d) = f32x4{o[i][e], o[i][e + 1], o[i][e + 2], o[i][e + 3]};
+            }
+        if (have && half == 0) {
+            float *ml = p.part_ml + ((int64_t)split * p.cache.num_q * p.q_heads + at) * 2;
+            ml[0] = m;
+            ml[1] = l;
+        }
+    } else {
+        const float by = m == -INFINITY ? 0.0f : (F8 && p.v_scale ? p.v_scale[h] : 1.0f) / l;
+        if (m == -INFINITY)
+#pragma unroll
+            for (int i = 0; i < DT; ++i)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) o[i][e] = 0.0f;
+#pragma unroll
+        for (int i = 0; i < DT; ++i)
+#pragma unroll
+            for (int e = 0; e < 16; e += 8) {
+                // both halves' four elements of one group of eight to one lane
+                const u32x2 a = swap_halves(pack2<T>(o[i][e] * by, o[i][e + 1] * by), pack2<T>(o[i][e + 4] * by, o[i][e + 5] * by));
+                const u32x2 b = swap_halves(pack2<T>(o[i][e + 2] * by, o[i][e + 3] * by), pack2<T>(o[i][e + 6] * by, o[i][e + 7] * by));
+                const int d = i * 32 + e * 2 + half * 8;
+                if (have && d < p.head_dim) *(u32x4 *)(to + d * 2) = u32x4{a[0], b[0], a[1], b[1]};
+            }
+        if (have && half == 0 && p.lse) p.lse[at] = m == -INFINITY ? -INFINITY : (m + log2_(l)) * kLn2;
+    }
+    __syncthreads();
+    if (!*odd) return;
+    // add_nonfinite: the values staged as 0, to the elements just written (each lane to those of one half's, which no
+    // other lane writes: the barrier is behind both halves' stores)
+    for (int step = step0; step < step1; ++step) {
+        const int t0 = begin + step * kStep;
+        look_up(step);
+        const uint32_t off = id < 0 ? 0u : (uint32_t)id * p.cache.block16 + id_row * p.cache.row16;
+        const uint64_t in = __ballot(id >= 0);
+        if (!is_mixed(in, t0)) continue;
+        for (int k = 0; k < kStep; ++k) {
+            const char *v = vbase + ((int64_t)(uint32_t)__shfl((int)off, k) << 4);
+            if (!((in >> k) & 1) || !have || t0 + k < lo || t0 + k >= hi) continue;
+            for (int d = half; d < p.head_dim; d += 2) {
+                const float x = load_one<T, F8>(v, d);
+                if (fabsf(x) < INFINITY) continue;
+                if (p.splits > 1) to32[d] += x;
+                else ((uint16_t *)to)[d] = (uint16_t)pack2<T>(T::to_f32(((const uint16_t *)to)[d]) + x, 0.0f);
+            }
+        }
+    }
+}
+
+// Every request in tiles of 16 rows.
+template <class T, bool F8, int DP>
+__global__ __launch_bounds__(kThreads) void attention_few_kernel(AttentionParams p) {
+    __shared__ __align__(16) char lds[kSplitLds<DP>];
+    __shared__ float part[kWaves][16][2];
+    const int64_t id = blockIdx.x;
+    const int h = (int)(id % p.kv_heads), split = (int)(id / p.kv_heads % p.splits);
+    const Tile tile = find_tile(p.cache, id / p.kv_heads / p.splits, p.group, kSplitRows);
+    if (tile.row0 < tile.rows) few_rows<T, F8, DP>(p, tile, h, split, lds, part);
+}
+
+// Tiles of 128 rows, from the last to the first (a request's last rows see
+// most keys); a request with no more than 16 rows in all takes the other body.
+template <class T, bool F8, int DP>
+__global__ __launch_bounds__(kThreads, DP > 128 ? 1 : 2) void attention_many_kernel(AttentionParams p) {
+    __shared__ __align__(16) char lds[kTileLds<DP> > kSplitLds<DP> ? kTileLds<DP> : kSplitLds<DP>];
+    __shared__ float part[kWaves][16][2];
+    __shared__ int odd;                        // some value that not all rows see is not finite
+    const int64_t id = blockIdx.x;
+    const int h = (int)(id % p.kv_heads), split = (int)(id / p.kv_heads % p.splits);
+    const Tile tile = find_tile(p.cache, p.tiles - 1 - id / p.kv_heads / p.splits, p.group, kRows);
+    if (tile.row0 >= tile.rows) return;
+    if (tile.rows <= kSplitRows) few_rows<T, F8, DP>(p, tile, h, split, lds, part);
+    else many_rows<T, F8, DP>(p, tile, h, split, lds, &odd);
 }
 
 // Join the parts of each row: one wave a row.
@@ -316,13 +593,13 @@ __global__ __launch_bounds__(kThreads) void attention_join_kernel(AttentionParam
     if (lane == 0 && p.lse) p.lse[row] = top == -INFINITY ? -INFINITY : (top + log2_(l)) * kLn2;
 }
 
-template <class T, bool F8> void (*split_kernel(int head_dim))(AttentionParams) {
-    if (head_dim <= 64) return attention_split_kernel<T, F8, 64>;
+template <class T, bool F8> void (*attention_kernel(bool many, int head_dim))(AttentionParams) {
+    if (head_dim <= 64) return many ? attention_many_kernel<T, F8, 64> : attention_few_kernel<T, F8, 64>;
     if constexpr (!F8) {
-        if (head_dim <= 96) return attention_split_kernel<T, F8, 96>;
+        if (head_dim <= 96) return many ? attention_many_kernel<T, F8, 96> : attention_few_kernel<T, F8, 96>;
     }
-    if (head_dim <= 128) return attention_split_kernel<T, F8, 128>;
-    return attention_split_kernel<T, F8, 256>;
+    if (head_dim <= 128) return many ? attention_many_kernel<T, F8, 128> : attention_few_kernel<T, F8, 128>;
+    return many ? attention_many_kernel<T, F8, 256> : attention_few_kernel<T, F8, 256>;
 }
 
 }  // namespace
@@ -372,8 +649,9 @@ int kv_paged_attention(const kv_layout *layout, const void *d_layer, const kv_ba
     p.causal = causal != 0;
     const bool bf16 = q->dtype == KV_BF16, f8 = cache_dtype == KV_F8E4M3;
     const int d = layout->head_dim;
-    auto kernel = bf16 ? (f8 ? tkv::split_kernel<tkv::Bf16, true>(d) : tkv::split_kernel<tkv::Bf16, false>(d))
-                       : (f8 ? tkv::split_kernel<tkv::F16, true>(d) : tkv::split_kernel<tkv::F16, false>(d));
+    const bool many = plan.rows != tkv::kSplitRows;
+    auto kernel = bf16 ? (f8 ? tkv::attention_kernel<tkv::Bf16, true>(many, d) : tkv::attention_kernel<tkv::Bf16, false>(many, d))
+                       : (f8 ? tkv::attention_kernel<tkv::F16, true>(many, d) : tkv::attention_kernel<tkv::F16, false>(many, d));
     hipStream_t s = (hipStream_t)stream;
     (void)hipGetLastError();
     hipLaunchKernelGGL(kernel, dim3((unsigned)(plan.tiles * p.kv_heads * p.splits)), dim3(tkv::kThreads), 0, s, p);

@@ -87,8 +87,9 @@ int plan_attention(const kv_layout *lo, const kv_batch *b, int32_t q_heads, int3
     if (b->num_q > (int64_t(1) << 40) / q_heads) return KV_ELIMIT;
     int64_t span = b->max_kv_len;
     if (window > 0 && span > (int64_t)window + b->max_q_len) span = (int64_t)window + b->max_q_len;
-    plan->tiles = b->num_q * group / kSplitRows + b->num_reqs;
-    plan->splits = attention_splits(plan->tiles, lo->kv_heads, span, kSplitStep);
+    plan->rows = b->max_q_len * group > kSplitRows ? kTileRows : kSplitRows;
+    plan->tiles = b->num_q * group / plan->rows + b->num_reqs;
+    plan->splits = attention_splits(plan->tiles, lo->kv_heads, span, plan->rows == kTileRows ? kTileStep : kSplitStep);
     plan->workspace = plan->splits > 1 ? (int64_t)plan->splits * b->num_q * q_heads * (lo->head_dim + 2) * 4 : 0;
     if (plan->tiles * lo->kv_heads * plan->splits >= (int64_t(1) << 31)) return KV_ELIMIT;
     return KV_OK;

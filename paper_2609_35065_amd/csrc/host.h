@@ -15,11 +15,13 @@ int check_layout(const kv_layout *lo);
 // Operators over the paged cache: checks of their arguments, and the launch
 // plan of the attention.
 constexpr int kMaxHeadDim = 256;
-constexpr int kSplitRows = 16;      // rows (query, head of the group) of an attention tile
-constexpr int kSplitStep = 128;     // keys that the waves of a workgroup take in one step
+constexpr int kSplitRows = 16, kSplitStep = 128;   // rows (query, head of the group) of a small attention tile, and
+                                                   // keys that its workgroup takes in one step
+constexpr int kTileRows = 128, kTileStep = 64;     // the same of a large one
 constexpr int kMaxSplits = 64;
 
 struct AttentionPlan {
+    int32_t rows;         // of a tile: kSplitRows or kTileRows
     int64_t tiles;        // row tiles, each for every KV head
     int32_t splits;       // parts that a tile's keys are cut into
     int64_t workspace;    // bytes

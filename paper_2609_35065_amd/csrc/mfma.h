@@ -22,6 +22,18 @@ template <uint32_t kExponent> __device__ __forceinline__ uint32_t nonfinite_mask
     return lo | hi;
 }
 
+// Set the non-finite elements to 0; whether there were any.
+template <uint32_t kExponent> __device__ __forceinline__ bool drop_nonfinite_(u32x4 &v) {
+    uint32_t any = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t bad = nonfinite_mask<kExponent>(v[i]);
+        v[i] &= ~bad;
+        any |= bad;
+    }
+    return any != 0;
+}
+
 // Take the non-finite elements out of an operand.  Where there are any in the
 // wave, odd[0..2] hold ones at its +inf, -inf and NaN elements.
 template <uint32_t kExponent, uint32_t kOne>
@@ -75,6 +87,8 @@ struct Bf16 {
     static __device__ __forceinline__ bool take_nonfinite(u32x4 &v, u32x4 odd[3]) {
         return take_nonfinite_<0x7f807f80u, kOne>(v, odd);
     }
+    static __device__ __forceinline__ bool drop_nonfinite(u32x4 &v) { return drop_nonfinite_<0x7f807f80u>(v); }
+    static __device__ __forceinline__ float to_f32(uint32_t x) { return __builtin_bit_cast(float, x << 16); }
 };
 
 struct F16 {
@@ -100,6 +114,8 @@ struct F16 {
     static __device__ __forceinline__ bool take_nonfinite(u32x4 &v, u32x4 odd[3]) {
         return take_nonfinite_<0x7c007c00u, kOne>(v, odd);
     }
+    static __device__ __forceinline__ bool drop_nonfinite(u32x4 &v) { return drop_nonfinite_<0x7c007c00u>(v); }
+    static __device__ __forceinline__ float to_f32(uint32_t x) { return (float)__builtin_bit_cast(_Float16, (uint16_t)x); }
 };
 
 template <class T> __device__ __forceinline__ uint32_t pack2(float a, float b) { return T::pack(a, b); }
@@ -107,6 +123,17 @@ template <class T> __device__ __forceinline__ uint32_t pack2(float a, float b) {
 // Eight elements of the 8-bit type.
 template <class T> __device__ __forceinline__ u32x4 unpack8(uint32_t a, uint32_t b) {
     return u32x4{T::from_f8(a, false), T::from_f8(a, true), T::from_f8(b, false), T::from_f8(b, true)};
+}
+
+// A value of both lanes 32 apart: lane i's (y[0]) and lane i + 32's (y[1]).
+__device__ __forceinline__ f32x2 both_halves(float x) {
+    const uint32_t b = __builtin_bit_cast(uint32_t, x);
+    return __builtin_bit_cast(f32x2, __builtin_amdgcn_permlane32_swap(b, b, false, false));
+}
+
+// a with its upper 32 lanes exchanged for the lower 32 of b, and b likewise.
+__device__ __forceinline__ u32x2 swap_halves(uint32_t a, uint32_t b) {
+    return __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(a, b, false, false));
 }
 
 // Transposing read from LDS.  Of each 16 lanes, lane s gives the address of
