@@ -1,10 +1,10 @@
 // weights.hip -- attention weight that cached tokens received, accumulated.
 //
 // W[h][j] = decay W[h][j] + sum over rows i that see j of exp(s_ij - lse_i).
-// With lse known nothing depends on other keys, so a workgroup owns 128 keys
-// of one KV head, holds them as matrix operands in registers (32 keys a wave)
-// and passes the request's rows; a lane's sums stay in its registers and are
-// added across lanes once at the end, in a fixed order, with no atomics.
+// With lse known nothing depends on other keys, so a workgroup owns the sums
+// of some keys of one KV head and passes the request's rows, with no atomics.
+// S = Q K^T leaves a lane with one key (lane % 32) and 16 of 32 rows, so that
+// the sum over rows stays in the lane: one register a key.
 
 #include <math.h>
 
@@ -16,7 +16,7 @@ namespace {
 
 constexpr int kWaves = 4;
 constexpr int kThreads = 64 * kWaves;
-constexpr int kKeys = 32 * kWaves;
+constexpr int kWaveKeys = 64;               // keys of a wave, held as matrix operands in registers
 constexpr float kLog2e = 1.44269504088896340736f;
 
 struct WeightParams {
@@ -33,99 +33,197 @@ struct WeightParams {
     bool causal;
 };
 
-template <class T, bool F8, int DP>
-__global__ __launch_bounds__(kThreads) void attention_weights_kernel(WeightParams p) {
-    constexpr int KS = DP / 16;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 31, half = lane >> 5;
+// What a staged row is to its keys: those it sees, lo <= j < hi, and its
+// lse in units of log 2.
+struct __align__(16) RowInfo {
+    float base[32];
+    int lo[32], hi[32];
+};
+
+template <int DP> constexpr int kQueryRow = DP * 2 + 16;     // bytes of an LDS row: 8 rows on different banks
+
+// The four waves take KW groups of 64 keys and 4 / KW groups of 32 rows at a
+// time; the rows go through LDS, one step ahead, for all of them.
+template <class T, bool F8, int DP, int KW>
+__global__ __launch_bounds__(kThreads, DP > 128 ? 1 : 2) void attention_weights_kernel(WeightParams p) {
+    constexpr int KS = DP / 16, RW = kWaves / KW, kRows = 32 * RW, VPR = DP / 8, VL = kRows * VPR / kThreads;
+    constexpr int kKeys = kWaveKeys * KW;
+    __shared__ __align__(16) char rows[2][kRows * kQueryRow<DP>];
+    __shared__ RowInfo info[2][RW];
+    __shared__ float parts[kWaves][kWaveKeys];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 31, half = lane >> 5;
+    const int kw = wave % KW, rw = wave / KW;
     const int h = (int)(blockIdx.x % p.kv_heads), r = (int)(blockIdx.x / p.kv_heads);
     const int32_t len_raw = p.cache.kv_len[r];
     const int64_t first = clamp_row(p.cache, p.cache.q_off[r]);
-    const int64_t ntok = max((int64_t)0, clamp_row(p.cache, p.cache.q_off[r + 1]) - first), nrows = ntok * p.group;
-    const int64_t len = min((int64_t)(len_raw < 0 ? 0 : len_raw), p.weight_stride);
+    const int64_t ntok = max((int64_t)0, clamp_row(p.cache, p.cache.q_off[r + 1]) - first);
+    const int64_t len = min((int64_t)(len_raw < 0 ? 0 : len_raw), p.weight_stride), ahead = len_raw - ntok;
     const float c = p.scale * (F8 && p.k_scale ? p.k_scale[h] : 1.0f);
     float *out = p.weights + ((int64_t)r * p.kv_heads + h) * p.weight_stride;
 
     for (int64_t tile = blockIdx.y; tile * kKeys < len; tile += gridDim.y) {
-        const int64_t t0 = tile * kKeys + wave * 32;
-        if (t0 >= len) continue;
-        // this lane's key, as an operand row
-        const int64_t t = t0 + col;
-        uint32_t row = 0;
-        const int32_t blk = t < len ? block_of(p.cache, r, (uint32_t)t, row) : -1;
-        const uint32_t there = (uint32_t)__ballot(blk >= 0);
-        const char *at = p.cache.layer + (int64_t)h * p.cache.head_bytes +
-                         ((int64_t)(blk < 0 ? 0u : (uint32_t)blk * p.cache.block16 + row * p.cache.row16) << 4);
-        u32x4 kf[KS];
-        // an 8-bit cache is loaded 16 elements at a time: lanes hold the head's elements in another order
-        if constexpr (F8) {
+        const int64_t tile0 = tile * kKeys, t0 = tile0 + kw * kWaveKeys;
+        // this lane's two keys, as operands; the element order follows the rows'
+        u32x4 kf[2][KS];
+        bool there[2];
+        uint64_t all = ~uint64_t(0);
 #pragma unroll
-            for (int ks = 0; ks < KS; ks += 2) {
-                const int d = ks * 16 + half * 16;
-                const u32x4 y = d < p.head_dim ? *(const u32x4 *)(at + d) : u32x4{0, 0, 0, 0};
-                kf[ks] = unpack8<T>(y[0], y[1]);
-                kf[ks + 1] = unpack8<T>(y[2], y[3]);
-            }
-        } else {
+        for (int x = 0; x < 2; ++x) {
+            const int64_t t = t0 + x * 32 + col;
+            uint32_t row = 0;
+            const int32_t blk = t < len ? block_of(p.cache, r, (uint32_t)t, row) : -1;
+            there[x] = blk >= 0;
+            all &= __ballot(there[x]);
+            const char *at = p.cache.layer + (int64_t)h * p.cache.head_bytes +
+                             ((int64_t)(blk < 0 ? 0u : (uint32_t)blk * p.cache.block16 + row * p.cache.row16) << 4);
+            if constexpr (F8) {
+                // 16 elements at a time: a lane holds other elements than in order, as the rows are read below
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks) {
-                const int d = ks * 16 + half * 8;
-                kf[ks] = d < p.head_dim ? *(const u32x4 *)(at + d * 2) : u32x4{0, 0, 0, 0};
+                for (int ks = 0; ks < KS; ks += 2) {
+                    const int d = ks * 16 + half * 16;
+                    const u32x4 y = d < p.head_dim ? *(const u32x4 *)(at + d) : u32x4{0, 0, 0, 0};
+                    kf[x][ks] = unpack8<T>(y[0], y[1]);
+                    kf[x][ks + 1] = unpack8<T>(y[2], y[3]);
+                }
+            } else {
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks) {
+                    const int d = ks * 16 + half * 8;
+                    kf[x][ks] = d < p.head_dim ? *(const u32x4 *)(at + d * 2) : u32x4{0, 0, 0, 0};
+                }
             }
         }
-        float sum[16];
-#pragma unroll
-        for (int i = 0; i < 16; ++i) sum[i] = 0.0f;
-        // rows that may see one of these keys: from the token at t0 on (causal), to the one whose window ends here
+        // rows that may see a key of the tile: from the token at its first key on (causal), to the one whose window
+        // ends at its last key
         int64_t tok0 = 0, tok1 = ntok;
-        if (p.causal) tok0 = max((int64_t)0, t0 - (len_raw - ntok));
-        if (p.window > 0) tok1 = min(ntok, t0 + 31 + p.window - (len_raw - ntok));
-        for (int64_t row0 = tok0 * p.group; row0 < tok1 * p.group; row0 += 32) {
-            const int64_t myrow = row0 + col;
-            const bool have = myrow < nrows;
-            const int64_t token = have ? myrow / p.group : 0;
-            const int head = h * p.group + (int)(have ? myrow % p.group : 0);
-            const char *qat = p.q + (first + token) * p.q_ts + head * p.q_hs;
-            f32x16 s;
+        if (p.causal) tok0 = max((int64_t)0, tile0 - ahead);
+        if (p.window > 0) tok1 = min(ntok, tile0 + kKeys - 1 + p.window - ahead);
+        const int64_t row_begin = tok0 * p.group, row_end = tok1 * p.group;
+
+        u32x4 qreg[VL];
+        float base = 0.0f;
+        int lo = 0, hi = 0;
+        const auto load = [&](int64_t row0) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) s[i] = 0.0f;
+            for (int i = 0; i < VL; ++i) {
+                const int x = i * kThreads + tid, vec = x % VPR;
+                const int64_t row = row0 + x / VPR;
+                qreg[i] = u32x4{0, 0, 0, 0};
+                if (row < row_end && vec * 8 < p.head_dim) {
+                    const int64_t token = row / p.group;
+                    const int head = h * p.group + (int)(row - token * p.group);
+                    qreg[i] = *(const u32x4 *)(p.q + (first + token) * p.q_ts + head * p.q_hs + vec * 16);
+                }
+            }
+            if (tid < kRows) {
+                const int64_t row = row0 + tid, token = row / p.group;
+                base = lo = hi = 0;
+                if (row < row_end) {
+                    base = p.lse[(first + token) * p.q_heads + h * p.group + (int)(row - token * p.group)];
+                    const int64_t pos = ahead + token;
+                    if (base != -INFINITY) hi = (int)max((int64_t)0, p.causal ? min(len, pos + 1) : len);
+                    else base = 0.0f;
+                    lo = (int)(p.window > 0 ? max((int64_t)0, pos - p.window + 1) : 0);
+                }
+            }
+        };
+        const auto stage = [&](int buf) {
+#pragma unroll
+            for (int i = 0; i < VL; ++i) {
+                const int x = i * kThreads + tid;
+                *(u32x4 *)(rows[buf] + x / VPR * kQueryRow<DP> + x % VPR * 16) = qreg[i];
+            }
+            if (tid < kRows) {
+                info[buf][tid / 32].base[tid % 32] = base * kLog2e;
+                info[buf][tid / 32].lo[tid % 32] = lo;
+                info[buf][tid / 32].hi[tid % 32] = hi;
+            }
+        };
+        float sum[2] = {0.0f, 0.0f};
+        if (row_begin < row_end) load(row_begin);
+        int buf = 0;
+        for (int64_t row0 = row_begin; row0 < row_end; row0 += kRows, buf ^= 1) {
+            stage(buf);
+            __syncthreads();
+            if (row0 + kRows < row_end) load(row0 + kRows);
+            const int64_t wrow = row0 + rw * 32;
+            if (wrow >= row_end) continue;
+            f32x16 s[2];
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) s[x][e] = 0.0f;
+            const char *at = rows[buf] + (rw * 32 + col) * kQueryRow<DP>;
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) {
                 const int d = F8 ? (ks / 2) * 32 + half * 16 + (ks & 1) * 8 : ks * 16 + half * 8;
-                u32x4 qf = {0, 0, 0, 0};
-                if (have && d < p.head_dim) qf = *(const u32x4 *)(qat + d * 2);
-                s = T::mfma32(kf[ks], qf, s);
+                const u32x4 qf = *(const u32x4 *)(at + d * 2);
+                s[0] = T::mfma32(qf, kf[0][ks], s[0]);
+                s[1] = T::mfma32(qf, kf[1][ks], s[1]);
             }
-            const float lse = have ? p.lse[(first + token) * p.q_heads + head] : -INFINITY;
-            const int64_t pos = len_raw - ntok + token;
-            const int64_t hi = !have || lse == -INFINITY ? 0 : (p.causal ? pos + 1 : len);
-            const int64_t lo = p.window > 0 ? pos - p.window + 1 : 0;
-            const float base = lse * kLog2e;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const int k = 8 * (i / 4) + 4 * half + i % 4;
-                const bool seen = ((there >> k) & 1) && t0 + k >= lo && t0 + k < hi;
-                if (seen) sum[i] += exp2_(__builtin_fmaf(s[i], c, -base));
+            const RowInfo &y = info[buf][rw];
+            // whether every row sees every key of the wave
+            bool whole = all == ~uint64_t(0);
+            if (whole) {
+                const bool in = y.lo[col] <= t0 && y.hi[col] >= t0 + kWaveKeys;
+                whole = __ballot(in) == ~uint64_t(0);
             }
+            float part[2] = {0.0f, 0.0f};          // of these rows, so that long sums stay exact
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const f32x4 b = *(const f32x4 *)&y.base[g * 8 + half * 4];
+                if (whole) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+#pragma unroll
+                        for (int x = 0; x < 2; ++x) part[x] += exp2_(__builtin_fmaf(s[x][g * 4 + e], c, -b[e]));
+                } else {
+                    const i32x4 l = *(const i32x4 *)&y.lo[g * 8 + half * 4], u = *(const i32x4 *)&y.hi[g * 8 + half * 4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+#pragma unroll
+                        for (int x = 0; x < 2; ++x) {
+                            const int64_t t = t0 + x * 32 + col;
+                            const bool see = there[x] && t >= l[e] && t < u[e];
+                            part[x] += see ? exp2_(__builtin_fmaf(s[x][g * 4 + e], c, -b[e])) : 0.0f;
+                        }
+                }
+            }
+            sum[0] += part[0];
+            sum[1] += part[1];
         }
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-#pragma unroll
-            for (int x = 1; x < 32; x *= 2) sum[i] += __shfl_xor(sum[i], x);
+        for (int x = 0; x < 2; ++x) {
+            const f32x2 y = both_halves(sum[x]);
+            sum[x] = y[0] + y[1];
         }
-        // lane 32 half + i writes the key of its sum i
+        // lane i has the sum of key 32 x + i % 32 in sum[x]
+        float got = half ? sum[1] : sum[0];
+        if constexpr (RW > 1) {
+            parts[wave][lane] = got;
+            __syncthreads();
+            if (rw == 0)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const int64_t key = t0 + 8 * (i / 4) + 4 * half + i % 4;
-            if (col == i && key < len) out[key] = p.decay == 0.0f ? sum[i] : __builtin_fmaf(p.decay, out[key], sum[i]);
+                for (int i = 1; i < RW; ++i) got += parts[i * KW + kw][lane];
+            __syncthreads();
+        } else {
+            __syncthreads();      // the rows' buffers are free for the next tile
         }
+        const int64_t key = t0 + lane;
+        if (rw == 0 && key < len) out[key] = p.decay == 0.0f ? got : __builtin_fmaf(p.decay, out[key], got);
     }
 }
 
-template <class T, bool F8> void (*weights_kernel(int head_dim))(WeightParams) {
-    if (head_dim <= 64) return attention_weights_kernel<T, F8, 64>;
-    if (head_dim <= 96) return attention_weights_kernel<T, F8, 96>;
-    if (head_dim <= 128) return attention_weights_kernel<T, F8, 128>;
-    return attention_weights_kernel<T, F8, 256>;
+template <class T, bool F8, int KW> void (*weights_kernel(int head_dim))(WeightParams) {
+    if (head_dim <= 64) return attention_weights_kernel<T, F8, 64, KW>;
+    if (head_dim <= 96) return attention_weights_kernel<T, F8, 96, KW>;
+    if (head_dim <= 128) return attention_weights_kernel<T, F8, 128, KW>;
+    return attention_weights_kernel<T, F8, 256, KW>;
+}
+
+template <int KW> auto weights_kernel(bool bf16, bool f8, int d) {
+    return bf16 ? (f8 ? weights_kernel<Bf16, true, KW>(d) : weights_kernel<Bf16, false, KW>(d))
+                : (f8 ? weights_kernel<F16, true, KW>(d) : weights_kernel<F16, false, KW>(d));
 }
 
 }  // namespace
@@ -166,14 +264,17 @@ int kv_attention_weights(const kv_layout *layout, const void *d_layer, const kv_
     p.head_dim = layout->head_dim;
     p.window = window;
     p.causal = causal != 0;
+    // Keys of a workgroup: 256, each wave 64 of its own, or 64, with the waves sharing the rows, where that is needed to
+    // give each compute unit two workgroups and there are rows to share.
+    const int64_t heads = (int64_t)batch->num_reqs * layout->kv_heads;
+    const bool share = heads * ((batch->max_kv_len + 255) / 256) < 512 && (int64_t)batch->max_q_len * p.group > 32;
+    const int keys = share ? 64 : 256, d = layout->head_dim;
     const bool bf16 = q->dtype == KV_BF16, f8 = cache_dtype == KV_F8E4M3;
-    const int d = layout->head_dim;
-    auto kernel = bf16 ? (f8 ? tkv::weights_kernel<tkv::Bf16, true>(d) : tkv::weights_kernel<tkv::Bf16, false>(d))
-                       : (f8 ? tkv::weights_kernel<tkv::F16, true>(d) : tkv::weights_kernel<tkv::F16, false>(d));
-    int64_t tiles = ((int64_t)batch->max_kv_len + tkv::kKeys - 1) / tkv::kKeys;
+    auto kernel = share ? tkv::weights_kernel<1>(bf16, f8, d) : tkv::weights_kernel<4>(bf16, f8, d);
+    int64_t tiles = ((int64_t)batch->max_kv_len + keys - 1) / keys;
     tiles = tiles < 1 ? 1 : (tiles > 65535 ? 65535 : tiles);
     (void)hipGetLastError();
-    hipLaunchKernelGGL(kernel, dim3((unsigned)(batch->num_reqs * layout->kv_heads), (unsigned)tiles),
+    hipLaunchKernelGGL(kernel, dim3((unsigned)heads, (unsigned)tiles),
                        dim3(tkv::kThreads), 0, (hipStream_t)stream, p);
     return hipGetLastError() == hipSuccess ? KV_OK : KV_EHIP;
 }
