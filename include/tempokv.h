@@ -490,8 +490,8 @@ int kv_paged_attention_workspace(const kv_layout *layout, const kv_batch *batch,
  *   d_workspace  at least kv_paged_attention_workspace bytes, 16-byte
  *              aligned, overwritten (NULL when that is 0)
  * Deterministic.  At most two launches; num_q == 0 enqueues nothing.
- * Errors: KV_EINVAL, KV_EALIGN, KV_ELIMIT (as kv_rope_append, and more than
- * 2^31 row tiles or a workspace too small), KV_EHIP. */
+ * Errors: KV_EINVAL, KV_EALIGN, KV_ELIMIT (as kv_rope_append, and 2^30 rows
+ * num_q * q_heads or 2^31 workgroups or more, or a workspace too small), KV_EHIP. */
 int kv_paged_attention(const kv_layout *layout, const void *d_layer, const kv_batch *batch, const kv_rows *q,
                        const kv_rows *out, float scale, int32_t causal, int32_t window, int32_t cache_dtype,
                        const float *d_k_scale, const float *d_v_scale, float *d_lse, void *d_workspace,

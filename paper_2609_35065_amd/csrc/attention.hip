@@ -33,6 +33,7 @@ struct AttentionParams {
     const float *k_scale, *v_scale;
     int64_t tiles;
     float scale;                       // times log2 e
+    Divider by_group;
     int32_t q_heads, kv_heads, group, head_dim;
     int32_t splits, window;
     bool causal;
@@ -45,16 +46,16 @@ struct AttentionParams {
 struct Tile {
     int32_t req;
     int64_t first;      // the request's first row of q
-    int64_t row0;       // the tile's first row within the request (token * group + head)
-    int64_t rows;       // rows of the request
+    int row0;           // the tile's first row within the request (token * group + head)
+    int rows;           // rows of the request
 };
 
-__device__ __forceinline__ Tile find_tile(const Paged &c, int64_t tile, int32_t group, int32_t rows) {
+template <int ROWS> __device__ __forceinline__ Tile find_tile(const Paged &c, int tile, int group) {
     const int lane = threadIdx.x & 63;
     int r = 0;
     for (int base = 0; base < c.num_reqs; base += 64) {
         const bool at = base + lane < c.num_reqs &&
-                        clamp_row(c, c.q_off[base + lane]) * group / rows + base + lane <= tile;
+                        (int)clamp_row(c, c.q_off[base + lane]) * group / ROWS + base + lane <= tile;
         const int n = __popcll(__ballot(at));
         r += n;
         if (n < 64) break;
@@ -62,9 +63,8 @@ __device__ __forceinline__ Tile find_tile(const Paged &c, int64_t tile, int32_t 
     Tile t;
     t.req = __builtin_amdgcn_readfirstlane(r > 0 ? r - 1 : 0);
     t.first = clamp_row(c, c.q_off[t.req]);
-    const int64_t n = clamp_row(c, c.q_off[t.req + 1]) - t.first;
-    t.rows = (n < 0 ? 0 : n) * group;
-    t.row0 = (tile - (t.first * group / rows + t.req)) * rows;
+    t.rows = max(0, (int)(clamp_row(c, c.q_off[t.req + 1]) - t.first)) * group;
+    t.row0 = (tile - ((int)t.first * group / ROWS + t.req)) * ROWS;
     return t;
 }
 
@@ -103,17 +103,15 @@ __device__ __forceinline__ void few_rows(const AttentionParams &p, const Tile &t
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, quad = lane >> 4;
 
     // this lane's row
-    const int64_t myrow = tile.row0 + col;
+    const int myrow = tile.row0 + col;
     const bool have = myrow < tile.rows;
-    const int64_t token = have ? myrow / p.group : 0;
-    const int head = h * p.group + (int)(have ? myrow % p.group : 0);
+    const int token = have ? (int)divide(myrow, p.by_group) : 0;
+    const int head = h * p.group + (have ? myrow - token * p.group : 0);
     const int32_t len_raw = p.cache.kv_len[tile.req];
     const int64_t len = min((int64_t)(len_raw < 0 ? 0 : len_raw), (int64_t)p.cache.bt_stride * p.cache.block_size);
-    const int64_t ntok = tile.rows / p.group;
-    const int64_t pos = len_raw - ntok + token;
-    const int64_t pos_first = len_raw - ntok + tile.row0 / p.group;
-    const int64_t last = min(tile.row0 + 15, tile.rows - 1);
-    const int64_t pos_last = len_raw - ntok + last / p.group;
+    const int64_t ahead = (int64_t)len_raw - divide(tile.rows, p.by_group);    // cache index of the first token
+    const int64_t pos = ahead + token, pos_first = ahead + divide(tile.row0, p.by_group);
+    const int64_t pos_last = ahead + divide(min(tile.row0 + 15, tile.rows - 1), p.by_group);
     // keys this lane's row sees: lo <= j < hi; and those that some or all rows of the tile see
     const int64_t hi64 = p.causal ? min(len, pos + 1) : len, lo64 = p.window > 0 ? max((int64_t)0, pos - p.window + 1) : 0;
     const int hi = have ? (int)max((int64_t)0, hi64) : 0, lo = (int)lo64;
@@ -258,10 +256,10 @@ __device__ __forceinline__ void few_rows(const AttentionParams &p, const Tile &t
     const int64_t all = p.cache.num_q * p.q_heads;
     for (int x = threadIdx.x; x < 16 * DP / 4; x += kThreads) {
         const int r = x / (DP / 4), d = x % (DP / 4) * 4;
-        const int64_t row_ = tile.row0 + r;
-        if (row_ >= tile.rows || d >= p.head_dim) continue;
-        const int64_t q = tile.first + row_ / p.group;
-        const int hd = h * p.group + (int)(row_ % p.group);
+        const int row = tile.row0 + r, tok = (int)divide(row, p.by_group);
+        if (row >= tile.rows || d >= p.head_dim) continue;
+        const int64_t q = tile.first + tok;
+        const int hd = h * p.group + row - tok * p.group;
         float mm = -INFINITY, ll = 0.0f;
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) mm = fmaxf(mm, part[w][r][0]);
@@ -315,21 +313,22 @@ __device__ __forceinline__ void many_rows(const AttentionParams &p, const Tile &
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 31, half = lane >> 5;
     char *const kbuf = lds, *const vbuf = lds + 2 * kStep * kKeyRow<DP>;
 
-    const int64_t wrow = tile.row0 + wave * 32, myrow = wrow + col;
+    const int wrow = tile.row0 + wave * 32, myrow = wrow + col;
     const bool have = myrow < tile.rows, active = wrow < tile.rows;
-    const int64_t token = have ? myrow / p.group : 0;
-    const int head = h * p.group + (int)(have ? myrow % p.group : 0);
+    const int token = have ? (int)divide(myrow, p.by_group) : 0;
+    const int head = h * p.group + (have ? myrow - token * p.group : 0);
     const int32_t len_raw = p.cache.kv_len[tile.req];
     const int64_t len = min((int64_t)(len_raw < 0 ? 0 : len_raw), (int64_t)p.cache.bt_stride * p.cache.block_size);
-    const int64_t ahead = len_raw - tile.rows / p.group;       // cache index of the first token
+    const int64_t ahead = (int64_t)len_raw - divide(tile.rows, p.by_group);    // cache index of the first token
     // keys that rows see, lo <= j < hi: this lane's, those that all or any of the wave's rows see, those of the tile
     const auto hi_of = [&](int64_t tok) { return (int)max((int64_t)0, p.causal ? min(len, ahead + tok + 1) : len); };
     const auto lo_of = [&](int64_t tok) { return (int)(p.window > 0 ? max((int64_t)0, ahead + tok - p.window + 1) : 0); };
     const int hi = have ? hi_of(token) : 0, lo = lo_of(token);
-    const int64_t wfirst = wrow / p.group, wlast = min(wrow + 31, tile.rows - 1) / p.group;
+    const int last_row = tile.rows - 1;
+    const int64_t wfirst = divide(min(wrow, last_row), p.by_group), wlast = divide(min(wrow + 31, last_row), p.by_group);
+    const int64_t first = divide(tile.row0, p.by_group), last = divide(min(tile.row0 + kRows - 1, last_row), p.by_group);
     const int all_hi = hi_of(wfirst), all_lo = lo_of(wlast), any_hi = active ? hi_of(wlast) : 0, any_lo = lo_of(wfirst);
-    const int end = hi_of(min(tile.row0 + kRows - 1, tile.rows - 1) / p.group);
-    const int begin = lo_of(tile.row0 / p.group) & ~(kStep - 1);
+    const int end = hi_of(last), begin = lo_of(first) & ~(kStep - 1);
     const int steps = end > begin ? (end - begin + kStep - 1) / kStep : 0;
     const int step0 = (int)((int64_t)steps * split / p.splits), step1 = (int)((int64_t)steps * (split + 1) / p.splits);
 
@@ -344,7 +343,7 @@ __device__ __forceinline__ void many_rows(const AttentionParams &p, const Tile &
     const char *kbase = p.cache.layer + (int64_t)h * p.cache.head_bytes;
     const char *vbase = kbase + p.cache.kv_stride;
 
-    const int tile_hi = hi_of(tile.row0 / p.group), tile_lo = lo_of(min(tile.row0 + kRows - 1, tile.rows - 1) / p.group);
+    const int tile_hi = hi_of(first), tile_lo = lo_of(last);
     uint64_t there = 0, there_next = 0;        // bit k: key k of the step is in the cache
     const auto is_mixed = [&](uint64_t there, int t0) { return there != ~uint64_t(0) || t0 < tile_lo || t0 + kStep > tile_hi; };
     if (tid == 0) *odd = 0;
@@ -541,9 +540,9 @@ template <class T, bool F8, int DP>
 __global__ __launch_bounds__(kThreads) void attention_few_kernel(AttentionParams p) {
     __shared__ __align__(16) char lds[kSplitLds<DP>];
     __shared__ float part[kWaves][16][2];
-    const int64_t id = blockIdx.x;
+    const unsigned id = blockIdx.x;
     const int h = (int)(id % p.kv_heads), split = (int)(id / p.kv_heads % p.splits);
-    const Tile tile = find_tile(p.cache, id / p.kv_heads / p.splits, p.group, kSplitRows);
+    const Tile tile = find_tile<kSplitRows>(p.cache, (int)(id / p.kv_heads / p.splits), p.group);
     if (tile.row0 < tile.rows) few_rows<T, F8, DP>(p, tile, h, split, lds, part);
 }
 
@@ -554,9 +553,9 @@ __global__ __launch_bounds__(kThreads, DP > 128 ? 1 : 2) void attention_many_ker
     __shared__ __align__(16) char lds[kTileLds<DP> > kSplitLds<DP> ? kTileLds<DP> : kSplitLds<DP>];
     __shared__ float part[kWaves][16][2];
     __shared__ int odd;                        // some value that not all rows see is not finite
-    const int64_t id = blockIdx.x;
+    const unsigned id = blockIdx.x;
     const int h = (int)(id % p.kv_heads), split = (int)(id / p.kv_heads % p.splits);
-    const Tile tile = find_tile(p.cache, p.tiles - 1 - id / p.kv_heads / p.splits, p.group, kRows);
+    const Tile tile = find_tile<kRows>(p.cache, (int)p.tiles - 1 - (int)(id / p.kv_heads / p.splits), p.group);
     if (tile.row0 >= tile.rows) return;
     if (tile.rows <= kSplitRows) few_rows<T, F8, DP>(p, tile, h, split, lds, part);
     else many_rows<T, F8, DP>(p, tile, h, split, lds, &odd);
@@ -643,6 +642,7 @@ int kv_paged_attention(const kv_layout *layout, const void *d_layer, const kv_ba
     p.q_heads = q->heads;
     p.kv_heads = layout->kv_heads;
     p.group = q->heads / layout->kv_heads;
+    p.by_group = tkv::make_divider((uint32_t)p.group);
     p.head_dim = layout->head_dim;
     p.splits = plan.splits;
     p.window = window;

@@ -84,7 +84,7 @@ int32_t attention_splits(int64_t tiles, int32_t kv_heads, int64_t span, int32_t 
 int plan_attention(const kv_layout *lo, const kv_batch *b, int32_t q_heads, int32_t window, AttentionPlan *plan) {
     if (q_heads <= 0 || q_heads % lo->kv_heads != 0 || window < 0) return KV_EINVAL;
     const int64_t group = q_heads / lo->kv_heads;
-    if (b->num_q > (int64_t(1) << 40) / q_heads) return KV_ELIMIT;
+    if (b->num_q >= (int64_t(1) << 30) / q_heads) return KV_ELIMIT;       // rows are counted in 32 bits
     int64_t span = b->max_kv_len;
     if (window > 0 && span > (int64_t)window + b->max_q_len) span = (int64_t)window + b->max_q_len;
     plan->rows = b->max_q_len * group > kSplitRows ? kTileRows : kSplitRows;

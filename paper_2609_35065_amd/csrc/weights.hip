@@ -28,6 +28,7 @@ struct WeightParams {
     float *weights;
     int64_t weight_stride;
     float scale, decay;    // scale times log2 e
+    Divider by_group;
     int32_t q_heads, kv_heads, group, head_dim;
     int32_t window;
     bool causal;
@@ -46,17 +47,17 @@ template <int DP> constexpr int kQueryRow = DP * 2 + 16;     // bytes of an LDS 
 // time; the rows go through LDS, one step ahead, for all of them.
 template <class T, bool F8, int DP, int KW>
 __global__ __launch_bounds__(kThreads, DP > 128 ? 1 : 2) void attention_weights_kernel(WeightParams p) {
-    constexpr int KS = DP / 16, RW = kWaves / KW, kRows = 32 * RW, VPR = DP / 8, VL = kRows * VPR / kThreads;
+    constexpr int KS = DP / 16, RW = kWaves / KW, RT = KW > 1 ? 2 : 1, kRows = 32 * RW * RT, VPR = DP / 8, VL = kRows * VPR / kThreads;
     constexpr int kKeys = kWaveKeys * KW;
     __shared__ __align__(16) char rows[2][kRows * kQueryRow<DP>];
-    __shared__ RowInfo info[2][RW];
+    __shared__ RowInfo info[2][RW * RT];
     __shared__ float parts[kWaves][kWaveKeys];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 31, half = lane >> 5;
     const int kw = wave % KW, rw = wave / KW;
     const int h = (int)(blockIdx.x % p.kv_heads), r = (int)(blockIdx.x / p.kv_heads);
     const int32_t len_raw = p.cache.kv_len[r];
     const int64_t first = clamp_row(p.cache, p.cache.q_off[r]);
-    const int64_t ntok = max((int64_t)0, clamp_row(p.cache, p.cache.q_off[r + 1]) - first);
+    const int ntok = (int)max((int64_t)0, clamp_row(p.cache, p.cache.q_off[r + 1]) - first);
     const int64_t len = min((int64_t)(len_raw < 0 ? 0 : len_raw), p.weight_stride), ahead = len_raw - ntok;
     const float c = p.scale * (F8 && p.k_scale ? p.k_scale[h] : 1.0f);
     float *out = p.weights + ((int64_t)r * p.kv_heads + h) * p.weight_stride;
@@ -95,31 +96,30 @@ __global__ __launch_bounds__(kThreads, DP > 128 ? 1 : 2) void attention_weights_
         }
         // rows that may see a key of the tile: from the token at its first key on (causal), to the one whose window
         // ends at its last key
-        int64_t tok0 = 0, tok1 = ntok;
-        if (p.causal) tok0 = max((int64_t)0, tile0 - ahead);
-        if (p.window > 0) tok1 = min(ntok, tile0 + kKeys - 1 + p.window - ahead);
-        const int64_t row_begin = tok0 * p.group, row_end = tok1 * p.group;
+        int tok0 = 0, tok1 = ntok;
+        if (p.causal) tok0 = (int)min((int64_t)ntok, max((int64_t)0, tile0 - ahead));
+        if (p.window > 0) tok1 = (int)max((int64_t)0, min((int64_t)ntok, tile0 + kKeys - 1 + p.window - ahead));
+        const int row_begin = tok0 * p.group, row_end = tok1 * p.group;
 
         u32x4 qreg[VL];
         float base = 0.0f;
         int lo = 0, hi = 0;
-        const auto load = [&](int64_t row0) {
+        const auto load = [&](int row0) {
 #pragma unroll
             for (int i = 0; i < VL; ++i) {
                 const int x = i * kThreads + tid, vec = x % VPR;
-                const int64_t row = row0 + x / VPR;
+                const int row = row0 + x / VPR;
                 qreg[i] = u32x4{0, 0, 0, 0};
                 if (row < row_end && vec * 8 < p.head_dim) {
-                    const int64_t token = row / p.group;
-                    const int head = h * p.group + (int)(row - token * p.group);
+                    const int token = (int)divide(row, p.by_group), head = h * p.group + row - token * p.group;
                     qreg[i] = *(const u32x4 *)(p.q + (first + token) * p.q_ts + head * p.q_hs + vec * 16);
                 }
             }
             if (tid < kRows) {
-                const int64_t row = row0 + tid, token = row / p.group;
+                const int row = row0 + tid, token = (int)divide(row, p.by_group);
                 base = lo = hi = 0;
                 if (row < row_end) {
-                    base = p.lse[(first + token) * p.q_heads + h * p.group + (int)(row - token * p.group)];
+                    base = p.lse[(first + token) * p.q_heads + h * p.group + row - token * p.group];
                     const int64_t pos = ahead + token;
                     if (base != -INFINITY) hi = (int)max((int64_t)0, p.causal ? min(len, pos + 1) : len);
                     else base = 0.0f;
@@ -142,18 +142,20 @@ __global__ __launch_bounds__(kThreads, DP > 128 ? 1 : 2) void attention_weights_
         float sum[2] = {0.0f, 0.0f};
         if (row_begin < row_end) load(row_begin);
         int buf = 0;
-        for (int64_t row0 = row_begin; row0 < row_end; row0 += kRows, buf ^= 1) {
+        for (int row0 = row_begin; row0 < row_end; row0 += kRows, buf ^= 1) {
             stage(buf);
             __syncthreads();
             if (row0 + kRows < row_end) load(row0 + kRows);
-            const int64_t wrow = row0 + rw * 32;
-            if (wrow >= row_end) continue;
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) {
+            const int rg = rw * RT + rt;
+            if (row0 + rg * 32 >= row_end) continue;
             f32x16 s[2];
 #pragma unroll
             for (int x = 0; x < 2; ++x)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) s[x][e] = 0.0f;
-            const char *at = rows[buf] + (rw * 32 + col) * kQueryRow<DP>;
+            const char *at = rows[buf] + (rg * 32 + col) * kQueryRow<DP>;
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) {
                 const int d = F8 ? (ks / 2) * 32 + half * 16 + (ks & 1) * 8 : ks * 16 + half * 8;
@@ -161,7 +163,7 @@ __global__ __launch_bounds__(kThreads, DP > 128 ? 1 : 2) void attention_weights_
                 s[0] = T::mfma32(qf, kf[0][ks], s[0]);
                 s[1] = T::mfma32(qf, kf[1][ks], s[1]);
             }
-            const RowInfo &y = info[buf][rw];
+            const RowInfo &y = info[buf][rg];
             // whether every row sees every key of the wave
             bool whole = all == ~uint64_t(0);
             if (whole) {
@@ -191,6 +193,7 @@ __global__ __launch_bounds__(kThreads, DP > 128 ? 1 : 2) void attention_weights_
             }
             sum[0] += part[0];
             sum[1] += part[1];
+            }
         }
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
@@ -248,6 +251,7 @@ int kv_attention_weights(const kv_layout *layout, const void *d_layer, const kv_
     if (((uintptr_t)d_layer & 15u) || ((uintptr_t)d_lse & 3u) || ((uintptr_t)d_weights & 3u)) return KV_EALIGN;
     if (batch->num_reqs == 0 || weight_stride == 0) return KV_OK;
     if ((int64_t)batch->num_reqs * layout->kv_heads >= (int64_t(1) << 31)) return KV_ELIMIT;
+    if (batch->num_q >= (int64_t(1) << 30) / q->heads) return KV_ELIMIT;
     tkv::WeightParams p;
     p.cache = tkv::make_paged(layout, d_layer, batch);
     p.q = (const char *)q->d_data;
@@ -261,6 +265,7 @@ int kv_attention_weights(const kv_layout *layout, const void *d_layer, const kv_
     p.q_heads = q->heads;
     p.kv_heads = layout->kv_heads;
     p.group = q->heads / layout->kv_heads;
+    p.by_group = tkv::make_divider((uint32_t)p.group);
     p.head_dim = layout->head_dim;
     p.window = window;
     p.causal = causal != 0;
