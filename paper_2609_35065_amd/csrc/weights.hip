@@ -63,14 +63,14 @@ __global__ __launch_bounds__(kThreads, DP > 128 ? 1 : 2) void attention_weights_
     float *out = p.weights + ((int64_t)r * p.kv_heads + h) * p.weight_stride;
 
     for (int64_t tile = blockIdx.y; tile * kKeys < len; tile += gridDim.y) {
-        const int64_t tile0 = tile * kKeys, t0 = tile0 + kw * kWaveKeys;
+        const int tile0 = (int)tile * kKeys, t0 = tile0 + kw * kWaveKeys;      // t0 + 63 may pass 2^31 - 1: no key is there
         // this lane's two keys, as operands; the element order follows the rows'
         u32x4 kf[2][KS];
         bool there[2];
         uint64_t all = ~uint64_t(0);
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
-            const int64_t t = t0 + x * 32 + col;
+            const int64_t t = (int64_t)t0 + x * 32 + col;
             uint32_t row = 0;
             const int32_t blk = t < len ? block_of(p.cache, r, (uint32_t)t, row) : -1;
             there[x] = blk >= 0;
@@ -97,8 +97,8 @@ __global__ __launch_bounds__(kThreads, DP > 128 ? 1 : 2) void attention_weights_
         // rows that may see a key of the tile: from the token at its first key on (causal), to the one whose window
         // ends at its last key
         int tok0 = 0, tok1 = ntok;
-        if (p.causal) tok0 = (int)min((int64_t)ntok, max((int64_t)0, tile0 - ahead));
-        if (p.window > 0) tok1 = (int)max((int64_t)0, min((int64_t)ntok, tile0 + kKeys - 1 + p.window - ahead));
+        if (p.causal) tok0 = (int)min((int64_t)ntok, max((int64_t)0, (int64_t)tile0 - ahead));
+        if (p.window > 0) tok1 = (int)max((int64_t)0, min((int64_t)ntok, (int64_t)tile0 + kKeys - 1 + p.window - ahead));
         const int row_begin = tok0 * p.group, row_end = tok1 * p.group;
 
         u32x4 qreg[VL];
@@ -148,51 +148,54 @@ __global__ __launch_bounds__(kThreads, DP > 128 ? 1 : 2) void attention_weights_
             if (row0 + kRows < row_end) load(row0 + kRows);
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt) {
-            const int rg = rw * RT + rt;
-            if (row0 + rg * 32 >= row_end) continue;
-            f32x16 s[2];
+                const int rg = rw * RT + rt;
+                if (row0 + rg * 32 >= row_end) continue;
+                const char *at = rows[buf] + (rg * 32 + col) * kQueryRow<DP>;
+                const RowInfo &y = info[buf][rg];
+                u32x4 qf[KS];
+                f32x4 b[4];
 #pragma unroll
-            for (int x = 0; x < 2; ++x)
+                for (int ks = 0; ks < KS; ++ks) {
+                    const int d = F8 ? (ks / 2) * 32 + half * 16 + (ks & 1) * 8 : ks * 16 + half * 8;
+                    qf[ks] = *(const u32x4 *)(at + d * 2);
+                }
 #pragma unroll
-                for (int e = 0; e < 16; ++e) s[x][e] = 0.0f;
-            const char *at = rows[buf] + (rg * 32 + col) * kQueryRow<DP>;
+                for (int g = 0; g < 4; ++g) b[g] = *(const f32x4 *)&y.base[g * 8 + half * 4];
+                // whether every row sees every key of the wave
+                const bool whole = __all(y.lo[col] <= t0 && y.hi[col] >= t0 + kWaveKeys) && all == ~uint64_t(0);
+                __builtin_amdgcn_sched_barrier(0);     // all reads are on their way before the first product waits
+                f32x16 s[2];
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks) {
-                const int d = F8 ? (ks / 2) * 32 + half * 16 + (ks & 1) * 8 : ks * 16 + half * 8;
-                const u32x4 qf = *(const u32x4 *)(at + d * 2);
-                s[0] = T::mfma32(qf, kf[0][ks], s[0]);
-                s[1] = T::mfma32(qf, kf[1][ks], s[1]);
-            }
-            const RowInfo &y = info[buf][rg];
-            // whether every row sees every key of the wave
-            bool whole = all == ~uint64_t(0);
-            if (whole) {
-                const bool in = y.lo[col] <= t0 && y.hi[col] >= t0 + kWaveKeys;
-                whole = __ballot(in) == ~uint64_t(0);
-            }
-            float part[2] = {0.0f, 0.0f};          // of these rows, so that long sums stay exact
+                for (int x = 0; x < 2; ++x)
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const f32x4 b = *(const f32x4 *)&y.base[g * 8 + half * 4];
+                    for (int e = 0; e < 16; ++e) s[x][e] = 0.0f;
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks) {
+                    s[0] = T::mfma32(qf[ks], kf[0][ks], s[0]);
+                    s[1] = T::mfma32(qf[ks], kf[1][ks], s[1]);
+                }
+                float part[2] = {0.0f, 0.0f};          // of these rows, so that long sums stay exact
                 if (whole) {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
+                    for (int g = 0; g < 16; ++g)
 #pragma unroll
-                        for (int x = 0; x < 2; ++x) part[x] += exp2_(__builtin_fmaf(s[x][g * 4 + e], c, -b[e]));
+                        for (int x = 0; x < 2; ++x) part[x] += exp2_(__builtin_fmaf(s[x][g], c, -b[g / 4][g % 4]));
                 } else {
-                    const i32x4 l = *(const i32x4 *)&y.lo[g * 8 + half * 4], u = *(const i32x4 *)&y.hi[g * 8 + half * 4];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
+                    for (int g = 0; g < 16; g += 4) {
+                        const i32x4 l = *(const i32x4 *)&y.lo[g * 2 + half * 4], u = *(const i32x4 *)&y.hi[g * 2 + half * 4];
 #pragma unroll
-                        for (int x = 0; x < 2; ++x) {
-                            const int64_t t = t0 + x * 32 + col;
-                            const bool see = there[x] && t >= l[e] && t < u[e];
-                            part[x] += see ? exp2_(__builtin_fmaf(s[x][g * 4 + e], c, -b[e])) : 0.0f;
-                        }
+                        for (int e = 0; e < 4; ++e)
+#pragma unroll
+                            for (int x = 0; x < 2; ++x) {
+                                const int t = t0 + x * 32 + col;
+                                const float v = exp2_(__builtin_fmaf(s[x][g + e], c, -b[g / 4][e]));
+                                part[x] += there[x] && t >= l[e] && t < u[e] ? v : 0.0f;
+                            }
+                    }
                 }
-            }
-            sum[0] += part[0];
-            sum[1] += part[1];
+                sum[0] += part[0];
+                sum[1] += part[1];
             }
         }
 #pragma unroll
@@ -212,7 +215,7 @@ __global__ __launch_bounds__(kThreads, DP > 128 ? 1 : 2) void attention_weights_
         } else {
             __syncthreads();      // the rows' buffers are free for the next tile
         }
-        const int64_t key = t0 + lane;
+        const int64_t key = (int64_t)t0 + lane;
         if (rw == 0 && key < len) out[key] = p.decay == 0.0f ? got : __builtin_fmaf(p.decay, out[key], got);
     }
 }
