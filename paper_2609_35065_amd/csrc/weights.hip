@@ -220,6 +220,102 @@ __global__ __launch_bounds__(kThreads, DP > 128 ? 1 : 2) void attention_weights_
     }
 }
 
+// Few rows (a decoded token's heads): nothing to share, so that each wave works
+// alone on 64 keys, 16 rows at a time, and all its loads are on their way at
+// once.  K is the 16 x 16 product's operand as it is loaded; a lane has one
+// key (lane % 16) and 4 of 16 rows.
+template <class T, bool F8, int DP>
+__global__ __launch_bounds__(kThreads) void attention_weights_few_kernel(WeightParams p) {
+    constexpr int KS = DP / 32, LD = F8 ? KS / 2 : KS, KT = kWaveKeys / 16;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, quad = lane >> 4;
+    const int h = (int)(blockIdx.x % p.kv_heads), r = (int)(blockIdx.x / p.kv_heads);
+    const int32_t len_raw = p.cache.kv_len[r];
+    const int64_t first = clamp_row(p.cache, p.cache.q_off[r]);
+    const int ntok = (int)max((int64_t)0, clamp_row(p.cache, p.cache.q_off[r + 1]) - first), nrows = ntok * p.group;
+    const int64_t len = min((int64_t)(len_raw < 0 ? 0 : len_raw), p.weight_stride), ahead = len_raw - ntok;
+    const float c = p.scale * (F8 && p.k_scale ? p.k_scale[h] : 1.0f);
+    float *out = p.weights + ((int64_t)r * p.kv_heads + h) * p.weight_stride;
+
+    for (int64_t tile = (int64_t)blockIdx.y * kWaves + wave; tile * kWaveKeys < len; tile += (int64_t)gridDim.y * kWaves) {
+        const int t0 = (int)tile * kWaveKeys;
+        uint32_t row = 0;
+        const int32_t blk = t0 + lane < len ? block_of(p.cache, r, (uint32_t)(t0 + lane), row) : -1;
+        const uint64_t there = __ballot(blk >= 0);
+        const uint32_t off = blk < 0 ? 0u : (uint32_t)blk * p.cache.block16 + row * p.cache.row16;
+        const float old = p.decay != 0.0f && t0 + lane < len ? out[t0 + lane] : 0.0f;
+        u32x4 kf[KT][LD];
+#pragma unroll
+        for (int x = 0; x < KT; ++x) {
+            const char *at = p.cache.layer + (int64_t)h * p.cache.head_bytes +
+                             ((int64_t)(uint32_t)__shfl((int)off, x * 16 + col) << 4) + quad * 16;
+#pragma unroll
+            for (int ks = 0; ks < LD; ++ks)
+                kf[x][ks] = ks * 64 + quad * 16 < p.cache.head_bytes ? *(const u32x4 *)(at + ks * 64) : u32x4{0, 0, 0, 0};
+        }
+        float sum[KT];
+#pragma unroll
+        for (int x = 0; x < KT; ++x) sum[x] = 0.0f;
+        for (int row0 = 0; row0 < nrows; row0 += 16) {
+            const int mine = min(row0 + col, nrows - 1), token = (int)divide(mine, p.by_group);
+            const char *qat = p.q + (first + token) * p.q_ts + (int64_t)(h * p.group + mine - token * p.group) * p.q_hs;
+            u32x4 qf[KS];
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                const int d = F8 ? (ks / 2) * 64 + quad * 16 + (ks & 1) * 8 : ks * 32 + quad * 8;
+                qf[ks] = d < p.head_dim ? *(const u32x4 *)(qat + d * 2) : u32x4{0, 0, 0, 0};
+            }
+            // this lane's four rows of the result
+            float base[4];
+            int lo[4], hi[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int rr = row0 + quad * 4 + i, tok = (int)divide(min(rr, nrows - 1), p.by_group);
+                const float lse = p.lse[(first + tok) * p.q_heads + h * p.group + min(rr, nrows - 1) - tok * p.group];
+                const int64_t pos = ahead + tok;
+                const bool on = rr < nrows && lse != -INFINITY;
+                base[i] = on ? lse * kLog2e : 0.0f;
+                hi[i] = on ? (int)max((int64_t)0, p.causal ? min(len, pos + 1) : len) : 0;
+                lo[i] = (int)(p.window > 0 ? max((int64_t)0, pos - p.window + 1) : 0);
+            }
+#pragma unroll
+            for (int x = 0; x < KT; ++x) {
+                f32x4 s = {0, 0, 0, 0};
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks) {
+                    if constexpr (F8) s = T::mfma16(qf[ks], unpack8<T>(kf[x][ks / 2][ks % 2 * 2], kf[x][ks / 2][ks % 2 * 2 + 1]), s);
+                    else s = T::mfma16(qf[ks], kf[x][ks], s);
+                }
+                const int t = t0 + x * 16 + col;
+                const bool in = (there >> (x * 16 + col)) & 1;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float v = exp2_(__builtin_fmaf(s[i], c, -base[i]));
+                    sum[x] += in && t >= lo[i] && t < hi[i] ? v : 0.0f;
+                }
+            }
+        }
+        // over the four groups of rows; lane i then takes key i
+        float got = 0.0f;
+#pragma unroll
+        for (int x = 0; x < KT; ++x) {
+            float y = sum[x];
+            y += __shfl_xor(y, 16);
+            const f32x2 z = both_halves(y);
+            got = quad == x ? z[0] + z[1] : got;
+        }
+        if (t0 + lane < len) out[t0 + lane] = p.decay == 0.0f ? got : __builtin_fmaf(p.decay, old, got);
+    }
+}
+
+template <class T, bool F8> void (*weights_few_kernel(int head_dim))(WeightParams) {
+    if (head_dim <= 64) return attention_weights_few_kernel<T, F8, 64>;
+    if constexpr (!F8) {
+        if (head_dim <= 96) return attention_weights_few_kernel<T, F8, 96>;
+    }
+    if (head_dim <= 128) return attention_weights_few_kernel<T, F8, 128>;
+    return attention_weights_few_kernel<T, F8, 256>;
+}
+
 template <class T, bool F8, int KW> void (*weights_kernel(int head_dim))(WeightParams) {
     if (head_dim <= 64) return attention_weights_kernel<T, F8, 64, KW>;
     if (head_dim <= 96) return attention_weights_kernel<T, F8, 96, KW>;
@@ -273,12 +369,15 @@ int kv_attention_weights(const kv_layout *layout, const void *d_layer, const kv_
     p.window = window;
     p.causal = causal != 0;
     // Keys of a workgroup: 256, each wave 64 of its own, or 64, with the waves sharing the rows, where that is needed to
-    // give each compute unit two workgroups and there are rows to share.
+    // give each compute unit two workgroups.  Up to 16 rows take a kernel of their own.
     const int64_t heads = (int64_t)batch->num_reqs * layout->kv_heads;
-    const bool share = heads * ((batch->max_kv_len + 255) / 256) < 512 && (int64_t)batch->max_q_len * p.group > 32;
+    const bool few = (int64_t)batch->max_q_len * p.group <= 16;
+    const bool share = !few && heads * ((batch->max_kv_len + 255) / 256) < 512;
     const int keys = share ? 64 : 256, d = layout->head_dim;
     const bool bf16 = q->dtype == KV_BF16, f8 = cache_dtype == KV_F8E4M3;
-    auto kernel = share ? tkv::weights_kernel<1>(bf16, f8, d) : tkv::weights_kernel<4>(bf16, f8, d);
+    auto kernel = few ? (bf16 ? (f8 ? tkv::weights_few_kernel<tkv::Bf16, true>(d) : tkv::weights_few_kernel<tkv::Bf16, false>(d))
+                              : (f8 ? tkv::weights_few_kernel<tkv::F16, true>(d) : tkv::weights_few_kernel<tkv::F16, false>(d)))
+                      : (share ? tkv::weights_kernel<1>(bf16, f8, d) : tkv::weights_kernel<4>(bf16, f8, d));
     int64_t tiles = ((int64_t)batch->max_kv_len + keys - 1) / keys;
     tiles = tiles < 1 ? 1 : (tiles > 65535 ? 65535 : tiles);
     (void)hipGetLastError();
