@@ -48,23 +48,27 @@ struct Tile {
     int64_t first;      // the request's first row of q
     int row0;           // the tile's first row within the request (token * group + head)
     int rows;           // rows of the request
+    int kv_len;
 };
 
 template <int ROWS> __device__ __forceinline__ Tile find_tile(const Paged &c, int tile, int group) {
     const int lane = threadIdx.x & 63;
-    int r = 0;
+    Tile t = {0, 0, 0, 0, 0};
     for (int base = 0; base < c.num_reqs; base += 64) {
-        const bool at = base + lane < c.num_reqs &&
-                        (int)clamp_row(c, c.q_off[base + lane]) * group / ROWS + base + lane <= tile;
-        const int n = __popcll(__ballot(at));
-        r += n;
+        const int r = min(base + lane, c.num_reqs - 1);
+        const int64_t first = clamp_row(c, c.q_off[r]), next = clamp_row(c, c.q_off[r + 1]);
+        const int len = c.kv_len[r], tile0 = (int)first * group / ROWS + base + lane;
+        // the last request that starts at or before the tile
+        const int n = __popcll(__ballot(base + lane < c.num_reqs && tile0 <= tile));
+        if (n == 0) break;
+        const int at = n - 1;
+        t.req = base + at;
+        t.first = (int64_t)__builtin_amdgcn_readlane((int)first, at);    // below 2^30, as all rows together
+        t.rows = max(0, __builtin_amdgcn_readlane((int)(next - first), at)) * group;
+        t.row0 = (tile - __builtin_amdgcn_readlane(tile0, at)) * ROWS;
+        t.kv_len = __builtin_amdgcn_readlane(len, at);
         if (n < 64) break;
     }
-    Tile t;
-    t.req = __builtin_amdgcn_readfirstlane(r > 0 ? r - 1 : 0);
-    t.first = clamp_row(c, c.q_off[t.req]);
-    t.rows = max(0, (int)(clamp_row(c, c.q_off[t.req + 1]) - t.first)) * group;
-    t.row0 = (tile - ((int)t.first * group / ROWS + t.req)) * ROWS;
     return t;
 }
 
@@ -94,8 +98,8 @@ template <int DP> constexpr int kSplitLds = kWaves * 32 * (DP * 2 + 32);
 // transposed.
 template <class T, bool F8, int DP>
 __device__ __forceinline__ void few_rows(const AttentionParams &p, const Tile &tile, int h, int split, char *lds,
-                                         float (*part)[16][2]) {
-    constexpr int KS = DP / 32, DT = DP / 16;
+                                         float (*part)[16][2], int *odd) {
+    constexpr int KS = DP / 32, LD = F8 ? KS / 2 : KS, DT = DP / 16;
     constexpr int kRow = DP * 2 + 32;          // bytes of an LDS row: 8 rows lie on different banks
     constexpr int VEC = F8 ? 16 : 8;           // elements of a 16-byte vector of the cache
     constexpr int VPR = DP / VEC;              // vectors of a row
@@ -107,7 +111,7 @@ __device__ __forceinline__ void few_rows(const AttentionParams &p, const Tile &t
     const bool have = myrow < tile.rows;
     const int token = have ? (int)divide(myrow, p.by_group) : 0;
     const int head = h * p.group + (have ? myrow - token * p.group : 0);
-    const int32_t len_raw = p.cache.kv_len[tile.req];
+    const int32_t len_raw = tile.kv_len;
     const int64_t len = min((int64_t)(len_raw < 0 ? 0 : len_raw), (int64_t)p.cache.bt_stride * p.cache.block_size);
     const int64_t ahead = (int64_t)len_raw - divide(tile.rows, p.by_group);    // cache index of the first token
     const int64_t pos = ahead + token, pos_first = ahead + divide(tile.row0, p.by_group);
@@ -122,6 +126,41 @@ __device__ __forceinline__ void few_rows(const AttentionParams &p, const Tile &t
     const int steps = end > begin ? (end - begin + 31) / 32 : 0;
     const int step0 = (int)((int64_t)steps * split / p.splits), step1 = (int)((int64_t)steps * (split + 1) / p.splits);
 
+    const float c = p.scale * (F8 && p.k_scale ? p.k_scale[h] : 1.0f);
+    const char *kbase = p.cache.layer + (int64_t)h * p.cache.head_bytes;
+    const char *vbase = kbase + p.cache.kv_stride;
+    char *mine = lds + wave * 32 * kRow;
+    const auto is_mixed = [&](uint32_t there, int t0) { return there != 0xffffffffu || t0 < all_lo || t0 + 32 > all_hi; };
+    if (threadIdx.x == 0) *odd = 0;
+    __syncthreads();
+
+    // one step ahead: lanes 0..31 look up the keys (lanes 32..63 the same ones), then all load K and V
+    int32_t id = -1;
+    uint32_t id_row = 0, there_next = 0;
+    u32x4 kreg[2][LD], vreg[VL];
+    const auto look_up = [&](int step) {
+        const int t = begin + step * 32 + (lane & 31);
+        id = step < step1 && t < end ? block_of(p.cache, tile.req, (uint32_t)t, id_row) : -1;
+    };
+    const auto offset = [&]() { return id < 0 ? 0u : (uint32_t)id * p.cache.block16 + id_row * p.cache.row16; };
+    const auto load = [&]() {
+        const uint32_t off = offset();
+        there_next = (uint32_t)__ballot(id >= 0);
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            const char *at = kbase + ((int64_t)(uint32_t)__shfl((int)off, x * 16 + col) << 4) + quad * 16;
+#pragma unroll
+            for (int ks = 0; ks < LD; ++ks)
+                kreg[x][ks] = ks * 64 + quad * 16 < p.cache.head_bytes ? *(const u32x4 *)(at + ks * 64) : u32x4{0, 0, 0, 0};
+        }
+#pragma unroll
+        for (int i = 0; i < VL; ++i) {
+            const int x = i * 64 + lane, r = x / VPR, vec = x % VPR;
+            const char *at = vbase + ((int64_t)(uint32_t)__shfl((int)off, r) << 4);
+            vreg[i] = vec * 16 < p.cache.head_bytes ? *(const u32x4 *)(at + vec * 16) : u32x4{0, 0, 0, 0};
+        }
+    };
+    look_up(step0 + wave);
     u32x4 qf[KS];
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
@@ -130,10 +169,8 @@ __device__ __forceinline__ void few_rows(const AttentionParams &p, const Tile &t
         qf[ks] = u32x4{0, 0, 0, 0};
         if (have && d < p.head_dim) qf[ks] = *(const u32x4 *)(p.q + (tile.first + token) * p.q_ts + head * p.q_hs + d * 2);
     }
-    const float c = p.scale * (F8 && p.k_scale ? p.k_scale[h] : 1.0f);
-    const char *kbase = p.cache.layer + (int64_t)h * p.cache.head_bytes;
-    const char *vbase = kbase + p.cache.kv_stride;
-    char *mine = lds + wave * 32 * kRow;
+    if (step0 + wave < step1) load();
+    look_up(step0 + wave + kWaves);
 
     f32x4 o[DT];
 #pragma unroll
@@ -142,35 +179,24 @@ __device__ __forceinline__ void few_rows(const AttentionParams &p, const Tile &t
 
     for (int step = step0 + wave; step < step1; step += kWaves) {
         const int t0 = begin + step * 32;
-        // lanes 0..31 look up the step's keys (lanes 32..63 the same ones)
-        const int t = t0 + (lane & 31);
-        uint32_t row = 0;
-        const int32_t blk = t < end ? block_of(p.cache, tile.req, (uint32_t)t, row) : -1;
-        const uint32_t off = blk < 0 ? 0u : (uint32_t)blk * p.cache.block16 + row * p.cache.row16;
-        const uint32_t there = (uint32_t)__ballot(blk >= 0);
-        if (!there) continue;
-        u32x4 kf[2][F8 ? (KS + 1) / 2 : KS];
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-            const char *at = kbase + ((int64_t)(uint32_t)__shfl((int)off, x * 16 + col) << 4);
-#pragma unroll
-            for (int ks = 0; ks < (F8 ? (KS + 1) / 2 : KS); ++ks) {
-                const int d = F8 ? ks * 64 + quad * 16 : ks * 32 + quad * 8;
-                kf[x][ks] = d < p.head_dim ? *(const u32x4 *)(at + ks * 64 + quad * 16) : u32x4{0, 0, 0, 0};
-            }
-        }
-        // V, with zeros for missing keys and past the head
+        const uint32_t there = there_next;
+        // A value that is not finite must reach only the rows that see its key: 0 times it is NaN.  In a step that some
+        // row does not see whole, such values are staged as 0, and added below to the results that do see them.
+        const bool mixed = is_mixed(there, t0);
 #pragma unroll
         for (int i = 0; i < VL; ++i) {
             const int x = i * 64 + lane, r = x / VPR, vec = x % VPR;
-            const char *at = vbase + ((int64_t)(uint32_t)__shfl((int)off, r) << 4);
-            u32x4 y = {0, 0, 0, 0};
-            if (((there >> r) & 1) && vec * VEC < p.head_dim) y = *(const u32x4 *)(at + vec * 16);
+            u32x4 y[F8 ? 2 : 1];
             if constexpr (F8) {
-                *(u32x4 *)(mine + r * kRow + vec * 32) = unpack8<T>(y[0], y[1]);
-                *(u32x4 *)(mine + r * kRow + vec * 32 + 16) = unpack8<T>(y[2], y[3]);
+                y[0] = unpack8<T>(vreg[i][0], vreg[i][1]);
+                y[1] = unpack8<T>(vreg[i][2], vreg[i][3]);
             } else {
-                *(u32x4 *)(mine + r * kRow + vec * 16) = y;
+                y[0] = vreg[i];
+            }
+#pragma unroll
+            for (int j = 0; j < (F8 ? 2 : 1); ++j) {
+                if (mixed && T::drop_nonfinite(y[j])) *odd = 1;
+                *(u32x4 *)(mine + r * kRow + vec * VEC * 2 + j * 16) = y[j];
             }
         }
         f32x4 s[2];
@@ -179,25 +205,25 @@ __device__ __forceinline__ void few_rows(const AttentionParams &p, const Tile &t
             s[x] = f32x4{0, 0, 0, 0};
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) {
-                if constexpr (F8) s[x] = T::mfma16(unpack8<T>(kf[x][ks / 2][(ks & 1) * 2], kf[x][ks / 2][(ks & 1) * 2 + 1]), qf[ks], s[x]);
-                else s[x] = T::mfma16(kf[x][ks], qf[ks], s[x]);
+                if constexpr (F8) s[x] = T::mfma16(unpack8<T>(kreg[x][ks / 2][(ks & 1) * 2], kreg[x][ks / 2][(ks & 1) * 2 + 1]), qf[ks], s[x]);
+                else s[x] = T::mfma16(kreg[x][ks], qf[ks], s[x]);
             }
         }
-        const bool whole = there == 0xffffffffu && t0 >= all_lo && t0 + 32 <= all_hi;
-        bool seen[2][4];
+        if (step + kWaves < step1) load();
+        look_up(step + 2 * kWaves);
         float top = -INFINITY;
 #pragma unroll
         for (int x = 0; x < 2; ++x)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int k = x * 16 + quad * 4 + i;
-                seen[x][i] = whole || (((there >> k) & 1) && t0 + k >= lo && t0 + k < hi);
-                s[x][i] = seen[x][i] ? s[x][i] * c : -INFINITY;
+                const bool see = !mixed || (((there >> k) & 1) && t0 + k >= lo && t0 + k < hi);
+                s[x][i] = see ? s[x][i] * c : -INFINITY;
                 top = fmaxf(top, s[x][i]);
             }
         top = fmaxf(top, __shfl_xor(top, 16));
-        top = fmaxf(top, __shfl_xor(top, 32));
-        const float m1 = fmaxf(m, top), base = m1 == -INFINITY ? 0.0f : m1;
+        const f32x2 tops = both_halves(top);
+        const float m1 = fmaxf(m, fmaxf(tops[0], tops[1])), base = m1 == -INFINITY ? 0.0f : m1;
         const float fade = exp2_(m - base);
         m = m1;
         l *= fade;
@@ -212,33 +238,11 @@ __device__ __forceinline__ void few_rows(const AttentionParams &p, const Tile &t
                           pack2<T>(s[1][2], s[1][3])};
 #pragma unroll
         for (int i = 0; i < DT; ++i) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) o[i][e] *= fade;
-        }
-#pragma unroll
-        for (int i = 0; i < DT; ++i) {
             const char *at = mine + (quad * 4 + (col >> 2)) * kRow + i * 32 + (col & 3) * 8;
             const u32x2 a = read_transposed(at), b = read_transposed(at + 16 * kRow);
-            u32x4 vf = {a[0], a[1], b[0], b[1]};
-            if (whole) {
-                o[i] = T::mfma16(vf, pf, o[i]);
-                continue;
-            }
-            // A value that is not finite must reach only the rows that see its key: 0 times it is NaN.  Such values
-            // are taken out of the product and put in by counting, for each row, the keys it sees that hold them.
-            u32x4 odd[3];
-            if (T::take_nonfinite(vf, odd)) {
-                const u32x4 one = {T::pair(seen[0][0], seen[0][1]), T::pair(seen[0][2], seen[0][3]),
-                                   T::pair(seen[1][0], seen[1][1]), T::pair(seen[1][2], seen[1][3])};
 #pragma unroll
-                for (int kind = 0; kind < 3; ++kind) {
-                    const f32x4 n = T::mfma16(odd[kind], one, f32x4{0, 0, 0, 0});
-                    const float v = kind == 0 ? INFINITY : (kind == 1 ? -INFINITY : NAN);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) o[i][e] = n[e] > 0 ? o[i][e] + v : o[i][e];
-                }
-            }
-            o[i] = T::mfma16(vf, pf, o[i]);
+            for (int e = 0; e < 4; ++e) o[i][e] *= fade;
+            o[i] = T::mfma16(u32x4{a[0], a[1], b[0], b[1]}, pf, o[i]);
         }
     }
     l += __shfl_xor(l, 16);
@@ -285,6 +289,34 @@ __device__ __forceinline__ void few_rows(const AttentionParams &p, const Tile &t
         store_out(p, q, hd, d, mm == -INFINITY ? f32x4{0, 0, 0, 0} : acc * by, T::kBf16);
         if (d == 0 && p.lse) p.lse[q * p.q_heads + hd] = mm == -INFINITY ? -INFINITY : (mm + log2_(ll)) * kLn2;
     }
+    if (!*odd) return;
+    __syncthreads();
+    // the values staged as 0, to the elements just written
+    for (int step = step0; step < step1; ++step) {
+        const int t0 = begin + step * 32;
+        look_up(step);
+        const uint32_t off = offset(), in = (uint32_t)__ballot(id >= 0);
+        if (!is_mixed(in, t0)) continue;
+        for (int k = 0; k < 32; ++k) {
+            const char *v = vbase + ((int64_t)(uint32_t)__shfl((int)off, k) << 4);
+            if (!((in >> k) & 1)) continue;
+            for (int x = threadIdx.x; x < 16 * p.head_dim; x += kThreads) {
+                const int r = x / p.head_dim, d = x - r * p.head_dim, row = tile.row0 + r, tok = (int)divide(row, p.by_group);
+                const int64_t at = ahead + tok;
+                if (row >= tile.rows || (p.causal && t0 + k > at) || (p.window > 0 && t0 + k <= at - p.window)) continue;
+                const float y = load_one<T, F8>(v, d);
+                if (fabsf(y) < INFINITY) continue;
+                const int64_t q = tile.first + tok;
+                const int hd = h * p.group + row - tok * p.group;
+                if (p.splits > 1) {
+                    p.part_o[((int64_t)split * all + q * p.q_heads + hd) * p.head_dim + d] += y;
+                } else {
+                    uint16_t *to = (uint16_t *)(p.out + q * p.o_ts + hd * p.o_hs) + d;
+                    *to = (uint16_t)pack2<T>(T::to_f32(*to) + y, 0.0f);
+                }
+            }
+        }
+    }
 }
 
 // Tiles of 128 rows, 32 a wave, over steps of 64 keys.  K and V of a step go
@@ -317,7 +349,7 @@ __device__ __forceinline__ void many_rows(const AttentionParams &p, const Tile &
     const bool have = myrow < tile.rows, active = wrow < tile.rows;
     const int token = have ? (int)divide(myrow, p.by_group) : 0;
     const int head = h * p.group + (have ? myrow - token * p.group : 0);
-    const int32_t len_raw = p.cache.kv_len[tile.req];
+    const int32_t len_raw = tile.kv_len;
     const int64_t len = min((int64_t)(len_raw < 0 ? 0 : len_raw), (int64_t)p.cache.bt_stride * p.cache.block_size);
     const int64_t ahead = (int64_t)len_raw - divide(tile.rows, p.by_group);    // cache index of the first token
     // keys that rows see, lo <= j < hi: this lane's, those that all or any of the wave's rows see, those of the tile
@@ -540,10 +572,11 @@ template <class T, bool F8, int DP>
 __global__ __launch_bounds__(kThreads) void attention_few_kernel(AttentionParams p) {
     __shared__ __align__(16) char lds[kSplitLds<DP>];
     __shared__ float part[kWaves][16][2];
+    __shared__ int odd;                        // some value that not all rows see is not finite
     const unsigned id = blockIdx.x;
     const int h = (int)(id % p.kv_heads), split = (int)(id / p.kv_heads % p.splits);
     const Tile tile = find_tile<kSplitRows>(p.cache, (int)(id / p.kv_heads / p.splits), p.group);
-    if (tile.row0 < tile.rows) few_rows<T, F8, DP>(p, tile, h, split, lds, part);
+    if (tile.row0 < tile.rows) few_rows<T, F8, DP>(p, tile, h, split, lds, part, &odd);
 }
 
 // Tiles of 128 rows, from the last to the first (a request's last rows see
@@ -557,7 +590,7 @@ __global__ __launch_bounds__(kThreads, DP > 128 ? 1 : 2) void attention_many_ker
     const int h = (int)(id % p.kv_heads), split = (int)(id / p.kv_heads % p.splits);
     const Tile tile = find_tile<kRows>(p.cache, (int)p.tiles - 1 - (int)(id / p.kv_heads / p.splits), p.group);
     if (tile.row0 >= tile.rows) return;
-    if (tile.rows <= kSplitRows) few_rows<T, F8, DP>(p, tile, h, split, lds, part);
+    if (tile.rows <= kSplitRows) few_rows<T, F8, DP>(p, tile, h, split, lds, part, &odd);
     else many_rows<T, F8, DP>(p, tile, h, split, lds, &odd);
 }
 

@@ -34,39 +34,8 @@ template <uint32_t kExponent> __device__ __forceinline__ bool drop_nonfinite_(u3
     return any != 0;
 }
 
-// Take the non-finite elements out of an operand.  Where there are any in the
-// wave, odd[0..2] hold ones at its +inf, -inf and NaN elements.
-template <uint32_t kExponent, uint32_t kOne>
-__device__ __forceinline__ bool take_nonfinite_(u32x4 &v, u32x4 odd[3]) {
-    u32x4 bad;
-    uint32_t any = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        bad[i] = nonfinite_mask<kExponent>(v[i]);
-        any |= bad[i];
-    }
-    if (!__any(any != 0)) return false;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        uint32_t kind[3] = {0, 0, 0};
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const uint32_t at = 0xffffu << (16 * e), x = v[i] & at, one = kOne & at;
-            if (!(bad[i] & at)) continue;
-            const uint32_t inf = kExponent & at, sign = 0x80008000u & at;
-            kind[x == inf ? 0 : (x == (inf | sign) ? 1 : 2)] |= one;
-        }
-        odd[0][i] = kind[0];
-        odd[1][i] = kind[1];
-        odd[2][i] = kind[2];
-        v[i] &= ~bad[i];
-    }
-    return true;
-}
-
 struct Bf16 {
     static constexpr bool kBf16 = true;
-    static constexpr uint32_t kOne = 0x3f803f80u;
     static __device__ __forceinline__ f32x4 mfma16(u32x4 a, u32x4 b, f32x4 c) {
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c,
                                                        0, 0, 0);
@@ -83,17 +52,12 @@ struct Bf16 {
         return __builtin_bit_cast(uint32_t, high ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, 1.0f, true)
                                                  : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, 1.0f, false));
     }
-    static __device__ __forceinline__ uint32_t pair(bool a, bool b) { return (a ? 0x3f80u : 0u) | (b ? 0x3f800000u : 0u); }
-    static __device__ __forceinline__ bool take_nonfinite(u32x4 &v, u32x4 odd[3]) {
-        return take_nonfinite_<0x7f807f80u, kOne>(v, odd);
-    }
     static __device__ __forceinline__ bool drop_nonfinite(u32x4 &v) { return drop_nonfinite_<0x7f807f80u>(v); }
     static __device__ __forceinline__ float to_f32(uint32_t x) { return __builtin_bit_cast(float, x << 16); }
 };
 
 struct F16 {
     static constexpr bool kBf16 = false;
-    static constexpr uint32_t kOne = 0x3c003c00u;
     static __device__ __forceinline__ f32x4 mfma16(u32x4 a, u32x4 b, f32x4 c) {
         return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0,
                                                       0, 0);
@@ -109,10 +73,6 @@ struct F16 {
     static __device__ __forceinline__ uint32_t from_f8(uint32_t x, bool high) {   // exact
         return __builtin_bit_cast(uint32_t, high ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(x, 1.0f, true)
                                                  : __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(x, 1.0f, false));
-    }
-    static __device__ __forceinline__ uint32_t pair(bool a, bool b) { return (a ? 0x3c00u : 0u) | (b ? 0x3c000000u : 0u); }
-    static __device__ __forceinline__ bool take_nonfinite(u32x4 &v, u32x4 odd[3]) {
-        return take_nonfinite_<0x7c007c00u, kOne>(v, odd);
     }
     static __device__ __forceinline__ bool drop_nonfinite(u32x4 &v) { return drop_nonfinite_<0x7c007c00u>(v); }
     static __device__ __forceinline__ float to_f32(uint32_t x) { return (float)__builtin_bit_cast(_Float16, (uint16_t)x); }
