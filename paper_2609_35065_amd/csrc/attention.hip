@@ -100,6 +100,7 @@ template <class T, bool F8, int DP>
 __device__ __forceinline__ void few_rows(const AttentionParams &p, const Tile &tile, int h, int split, char *lds,
                                          float (*part)[16][2], int *odd) {
     constexpr int KS = DP / 32, LD = F8 ? KS / 2 : KS, DT = DP / 16;
+    constexpr int NS = F8 ? 2 : 1, kWide = 32 * NS;    // an 8-bit cache takes two steps at a time: as many bytes
     constexpr int kRow = DP * 2 + 32;          // bytes of an LDS row: 8 rows lie on different banks
     constexpr int VEC = F8 ? 16 : 8;           // elements of a 16-byte vector of the cache
     constexpr int VPR = DP / VEC;              // vectors of a row
@@ -120,10 +121,10 @@ __device__ __forceinline__ void few_rows(const AttentionParams &p, const Tile &t
     const int64_t hi64 = p.causal ? min(len, pos + 1) : len, lo64 = p.window > 0 ? max((int64_t)0, pos - p.window + 1) : 0;
     const int hi = have ? (int)max((int64_t)0, hi64) : 0, lo = (int)lo64;
     const int end = (int)max((int64_t)0, p.causal ? min(len, pos_last + 1) : len);
-    const int begin = (int)(p.window > 0 ? max((int64_t)0, pos_first - p.window + 1) : 0) & ~31;
+    const int begin = (int)(p.window > 0 ? max((int64_t)0, pos_first - p.window + 1) : 0) & ~(kWide - 1);
     const int all_hi = (int)max((int64_t)0, p.causal ? min(len, pos_first + 1) : len);
     const int all_lo = (int)(p.window > 0 ? max((int64_t)0, pos_last - p.window + 1) : 0);
-    const int steps = end > begin ? (end - begin + 31) / 32 : 0;
+    const int steps = end > begin ? (end - begin + kWide - 1) / kWide : 0;
     const int step0 = (int)((int64_t)steps * split / p.splits), step1 = (int)((int64_t)steps * (split + 1) / p.splits);
 
     const float c = p.scale * (F8 && p.k_scale ? p.k_scale[h] : 1.0f);
@@ -134,27 +135,28 @@ __device__ __forceinline__ void few_rows(const AttentionParams &p, const Tile &t
     if (threadIdx.x == 0) *odd = 0;
     __syncthreads();
 
-    // one step ahead: lanes 0..31 look up the keys (lanes 32..63 the same ones), then all load K and V
+    // one step ahead: a lane looks up a key (lanes 32..63 those of the other half, or the same ones), then all load
     int32_t id = -1;
-    uint32_t id_row = 0, there_next = 0;
-    u32x4 kreg[2][LD], vreg[VL];
+    uint32_t id_row = 0;
+    uint64_t there_next = 0;
+    u32x4 kreg[2 * NS][LD], vreg[VL * NS];
     const auto look_up = [&](int step) {
-        const int t = begin + step * 32 + (lane & 31);
+        const int t = begin + step * kWide + (lane & (kWide - 1));
         id = step < step1 && t < end ? block_of(p.cache, tile.req, (uint32_t)t, id_row) : -1;
     };
     const auto offset = [&]() { return id < 0 ? 0u : (uint32_t)id * p.cache.block16 + id_row * p.cache.row16; };
     const auto load = [&]() {
         const uint32_t off = offset();
-        there_next = (uint32_t)__ballot(id >= 0);
+        there_next = __ballot(id >= 0);
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
+        for (int x = 0; x < 2 * NS; ++x) {
             const char *at = kbase + ((int64_t)(uint32_t)__shfl((int)off, x * 16 + col) << 4) + quad * 16;
 #pragma unroll
             for (int ks = 0; ks < LD; ++ks)
                 kreg[x][ks] = ks * 64 + quad * 16 < p.cache.head_bytes ? *(const u32x4 *)(at + ks * 64) : u32x4{0, 0, 0, 0};
         }
 #pragma unroll
-        for (int i = 0; i < VL; ++i) {
+        for (int i = 0; i < VL * NS; ++i) {
             const int x = i * 64 + lane, r = x / VPR, vec = x % VPR;
             const char *at = vbase + ((int64_t)(uint32_t)__shfl((int)off, r) << 4);
             vreg[i] = vec * 16 < p.cache.head_bytes ? *(const u32x4 *)(at + vec * 16) : u32x4{0, 0, 0, 0};
@@ -178,8 +180,11 @@ __device__ __forceinline__ void few_rows(const AttentionParams &p, const Tile &t
     float m = -INFINITY, l = 0.0f;
 
     for (int step = step0 + wave; step < step1; step += kWaves) {
-        const int t0 = begin + step * 32;
-        const uint32_t there = there_next;
+        const uint64_t there_now = there_next;
+#pragma unroll
+        for (int n = 0; n < NS; ++n) {
+        const int t0 = begin + step * kWide + n * 32;
+        const uint32_t there = (uint32_t)(there_now >> (n * 32));
         // A value that is not finite must reach only the rows that see its key: 0 times it is NaN.  In a step that some
         // row does not see whole, such values are staged as 0, and added below to the results that do see them.
         const bool mixed = is_mixed(there, t0);
@@ -188,10 +193,10 @@ __device__ __forceinline__ void few_rows(const AttentionParams &p, const Tile &t
             const int x = i * 64 + lane, r = x / VPR, vec = x % VPR;
             u32x4 y[F8 ? 2 : 1];
             if constexpr (F8) {
-                y[0] = unpack8<T>(vreg[i][0], vreg[i][1]);
-                y[1] = unpack8<T>(vreg[i][2], vreg[i][3]);
+                y[0] = unpack8<T>(vreg[n * VL + i][0], vreg[n * VL + i][1]);
+                y[1] = unpack8<T>(vreg[n * VL + i][2], vreg[n * VL + i][3]);
             } else {
-                y[0] = vreg[i];
+                y[0] = vreg[n * VL + i];
             }
 #pragma unroll
             for (int j = 0; j < (F8 ? 2 : 1); ++j) {
@@ -205,12 +210,14 @@ __device__ __forceinline__ void few_rows(const AttentionParams &p, const Tile &t
             s[x] = f32x4{0, 0, 0, 0};
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) {
-                if constexpr (F8) s[x] = T::mfma16(unpack8<T>(kreg[x][ks / 2][(ks & 1) * 2], kreg[x][ks / 2][(ks & 1) * 2 + 1]), qf[ks], s[x]);
-                else s[x] = T::mfma16(kreg[x][ks], qf[ks], s[x]);
+                if constexpr (F8) s[x] = T::mfma16(unpack8<T>(kreg[n * 2 + x][ks / 2][(ks & 1) * 2], kreg[n * 2 + x][ks / 2][(ks & 1) * 2 + 1]), qf[ks], s[x]);
+                else s[x] = T::mfma16(kreg[n * 2 + x][ks], qf[ks], s[x]);
             }
         }
-        if (step + kWaves < step1) load();
-        look_up(step + 2 * kWaves);
+        if (n == NS - 1) {
+            if (step + kWaves < step1) load();
+            look_up(step + 2 * kWaves);
+        }
         float top = -INFINITY;
 #pragma unroll
         for (int x = 0; x < 2; ++x)
@@ -243,6 +250,7 @@ __device__ __forceinline__ void few_rows(const AttentionParams &p, const Tile &t
 #pragma unroll
             for (int e = 0; e < 4; ++e) o[i][e] *= fade;
             o[i] = T::mfma16(u32x4{a[0], a[1], b[0], b[1]}, pf, o[i]);
+        }
         }
     }
     l += __shfl_xor(l, 16);
@@ -293,11 +301,12 @@ __device__ __forceinline__ void few_rows(const AttentionParams &p, const Tile &t
     __syncthreads();
     // the values staged as 0, to the elements just written
     for (int step = step0; step < step1; ++step) {
-        const int t0 = begin + step * 32;
+        const int t0 = begin + step * kWide;
         look_up(step);
-        const uint32_t off = offset(), in = (uint32_t)__ballot(id >= 0);
-        if (!is_mixed(in, t0)) continue;
-        for (int k = 0; k < 32; ++k) {
+        const uint32_t off = offset();
+        const uint64_t in = __ballot(id >= 0);
+        if (!is_mixed((uint32_t)in, t0) && (NS == 1 || !is_mixed((uint32_t)(in >> 32), t0 + 32))) continue;
+        for (int k = 0; k < kWide; ++k) {
             const char *v = vbase + ((int64_t)(uint32_t)__shfl((int)off, k) << 4);
             if (!((in >> k) & 1)) continue;
             for (int x = threadIdx.x; x < 16 * p.head_dim; x += kThreads) {
