@@ -461,8 +461,8 @@ enum { KV_ROPE_HALF = 0,          /* element i with i + rot_dim/2 */
  * d_freqs float64 [rot_dim/2] in device memory; rot_dim even, 0 <= rot_dim <=
  * head_dim; head_dim a multiple of 8 (16 for an 8-bit cache) up to 256.
  * Cache indices of one batch must name distinct rows.  One launch; num_q == 0
- * enqueues nothing.  Errors: KV_EINVAL, KV_EALIGN, KV_ELIMIT (head_dim, or
- * blocks that span 64 GiB or more of one layer), KV_EHIP. */
+ * enqueues nothing.  Errors: KV_EINVAL, KV_EALIGN, KV_ELIMIT (head_dim, more
+ * than 65,536 heads, or blocks that span 64 GiB or more of one layer), KV_EHIP. */
 int kv_rope_append(const kv_layout *layout, void *d_layer, const kv_batch *batch, const kv_rows *q,
                    const kv_rows *q_out, const kv_rows *k, const kv_rows *v, const double *d_freqs, int32_t rot_dim,
                    int32_t flags, float magnitude, const int32_t *d_positions, int32_t cache_dtype,

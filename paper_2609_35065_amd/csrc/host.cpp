@@ -61,6 +61,7 @@ int check_batch(const kv_batch *b) {
 int check_rows(const kv_rows *x, int64_t num, int32_t head_dim, bool written) {
     if (!x || x->heads <= 0 || (x->dtype != KV_BF16 && x->dtype != KV_F16)) return KV_EINVAL;
     if (num > 0 && !x->d_data) return KV_EINVAL;
+    if (x->heads > kMaxHeads) return KV_ELIMIT;
     if (x->token_stride < 0 || x->head_stride < 0) return KV_EINVAL;
     // rows that are written must not lie on one another
     if (written && ((x->heads > 1 && x->head_stride < head_dim) || (num > 1 && x->token_stride < head_dim)))

@@ -11,7 +11,7 @@
 namespace tkv {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 256, kMaxTokens = 8;
 
 struct RopeParams {
     Paged cache;
@@ -22,11 +22,12 @@ struct RopeParams {
     const int32_t *positions;
     const float *k_scale, *v_scale;
     int32_t q_heads, kv_heads;
+    Divider by_token, by_row, by_half;
     int32_t vecs;          // 16-byte vectors (8 elements) of a row
     int32_t half;          // rotated pairs
+    int32_t row_units, token_units;
     int32_t per_block;     // tokens a workgroup takes
     float magnitude, sign;
-    bool interleaved;
 };
 
 template <bool BF16> __device__ __forceinline__ float to_f32(uint32_t bits16) {
@@ -53,20 +54,70 @@ __device__ __forceinline__ uint32_t pack4_f8(float a, float b, float c, float d)
     return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(clamp_f8(c), clamp_f8(d), x, true);
 }
 
-// A workgroup takes per_block consecutive tokens: their angles first (one
-// lane per token and pair), then every row of q, k and v.  A row lies in one
-// wave (8 elements a lane, 64 / vecs rows a wave), which reads all of it
-// before it writes, so q may be rotated in place.
-template <bool BF16, bool F8>
+// A token's angles are shared by its rows, so a workgroup takes per_block
+// tokens: where each goes and its angles first (one lane per token and pair),
+// then the rows, in units of two 16-byte vectors that need nothing else:
+//   HALF         vectors v and v + half/8, whose elements are each other's partners (half a multiple of 8)
+//   INTERLEAVED  neighbouring vectors
+//   ODD          half not a multiple of 8: neighbouring vectors, partners by way of LDS
+// What is not rotated (the rest of a row, v) comes in neighbouring vectors.
+// A row lies in one wave, which reads all of it before it writes, so q may be
+// rotated in place.  A lane's first unit is loaded before the angles.
+enum Pairing { HALF, INTERLEAVED, ODD };
+
+template <bool BF16, bool F8, Pairing PAIR>
 __global__ __launch_bounds__(kThreads) void rope_append_kernel(RopeParams p) {
-    extern __shared__ float trig[];                        // [per_block][half] cos, then sin
-    __shared__ int32_t where_req[16], where_index[16];
-    __shared__ uint32_t rows[kThreads / 64][64 * 4];       // a wave's rows, for partners in other lanes
+    extern __shared__ __align__(16) float trig[];                       // [per_block][half4] cos, then sin
+    __shared__ int32_t where_index[kMaxTokens];
+    __shared__ uint32_t where_row[kMaxTokens];             // 16-byte units from the plane's start
+    __shared__ bool where_in[kMaxTokens];
+    __shared__ uint32_t rows[PAIR == ODD ? kThreads / 64 : 1][PAIR == ODD ? 64 * 8 : 1];   // a wave's rows
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int64_t t0 = (int64_t)blockIdx.x * p.per_block;
     const int n = (int)(p.cache.num_q - t0 < p.per_block ? p.cache.num_q - t0 : p.per_block);
+    const int half4 = (p.half + 3) & ~3;
+    const int total = n * p.token_units;
+
+    // unit x: its row, and its vectors a and b (b = -1: none)
+    struct Unit {
+        int token, head, a, b;     // head: of q, then k, then v
+        bool on;
+    };
+    const int per_wave = PAIR == ODD ? 64 / p.row_units * p.row_units : 64;    // whole rows where LDS is in between
+    const int stride = kThreads / 64 * per_wave, start = wave * per_wave + lane;
+    const auto unit_of = [&](int x) {
+        Unit u;
+        u.on = x < total && lane < per_wave;
+        if (!u.on) x = 0;
+        u.token = (int)divide(x, p.by_token);
+        const int y = x - u.token * p.token_units;
+        u.head = (int)divide(y, p.by_row);
+        const int z = y - u.head * p.row_units, hv = p.half / 8;
+        const bool partners = PAIR == HALF && z < hv;
+        u.a = partners ? z : 2 * z;          // past the partners' units: 2 hv + 2 (z - hv)
+        u.b = partners ? z + hv : u.a + 1;
+        if (u.b >= p.vecs) u.b = -1;
+        return u;
+    };
+    const int nq = p.q_heads, nk = p.k ? p.kv_heads : 0;
+    const auto source = [&](const Unit &u) {
+        const int64_t t = t0 + u.token;
+        if (u.head < nq) return p.q + t * p.q_ts + u.head * p.q_hs;
+        if (u.head < nq + nk) return p.k + t * p.k_ts + (u.head - nq) * p.k_hs;
+        return p.v + t * p.v_ts + (u.head - nq - nk) * p.v_hs;
+    };
+    const auto fetch = [&](const Unit &u, u32x4 &a, u32x4 &b) {
+        if (!u.on) return;
+        const char *src = source(u);
+        a = *(const u32x4 *)(src + u.a * 16);
+        if (u.b >= 0) b = *(const u32x4 *)(src + u.b * 16);
+    };
+    u32x4 ra = {0, 0, 0, 0}, rb = {0, 0, 0, 0};
+    Unit u = unit_of(start);
+    fetch(u, ra, rb);
+
     for (int i = wave; i < n; i += kThreads / 64) {
-        // request of the token: how many requests end at or before it
+        // the token's request: how many requests end at or before it
         int r = 0;
         for (int base = 0; base < p.cache.num_reqs; base += 64) {
             const bool before = base + lane < p.cache.num_reqs && p.cache.q_off[base + lane + 1] <= t0 + i;
@@ -76,101 +127,130 @@ __global__ __launch_bounds__(kThreads) void rope_append_kernel(RopeParams p) {
         }
         if (lane == 0) {
             const bool known = r < p.cache.num_reqs;
-            where_req[i] = known ? r : -1;
-            where_index[i] = known ? p.cache.kv_len[r] - (int32_t)(p.cache.q_off[r + 1] - (t0 + i)) : -1;
+            const int32_t index = known ? p.cache.kv_len[r] - (int32_t)(p.cache.q_off[r + 1] - (t0 + i)) : -1;
+            uint32_t row = 0;
+            const int32_t id = index >= 0 ? block_of(p.cache, r, (uint32_t)index, row) : -1;
+            where_index[i] = index;
+            where_in[i] = id >= 0;
+            where_row[i] = id < 0 ? 0u : (uint32_t)id * p.cache.block16 + row * p.cache.row16;
         }
     }
     __syncthreads();
     for (int x = tid; x < n * p.half; x += kThreads) {
-        const int i = x / p.half, j = x - i * p.half;
+        const int i = (int)divide(x, p.by_half), j = x - i * p.half;
         const double pos = p.positions ? p.positions[t0 + i] : where_index[i];
-        double u = pos * p.freqs[j];
-        u -= rint(u * 0.15915494309189533577) * 6.283185307179586476925;
+        double angle = pos * p.freqs[j];
+        angle -= rint(angle * 0.15915494309189533577) * 6.283185307179586476925;
         float s, c;
-        sincosf((float)u, &s, &c);
-        trig[x] = c * p.magnitude;
-        trig[n * p.half + x] = s * p.magnitude * p.sign;
+        sincosf((float)angle, &s, &c);
+        trig[i * half4 + j] = c * p.magnitude;
+        trig[(n + i) * half4 + j] = s * p.magnitude * p.sign;
     }
     __syncthreads();
-    const int nq = p.q ? p.q_heads : 0, nk = p.k ? p.kv_heads : 0;
-    const int per_token = nq + 2 * nk, per_wave = 64 / p.vecs;
-    const int sub = lane / p.vecs, vec = lane - sub * p.vecs;
-    const int total = n * per_token;
-    for (int first = wave * per_wave; first < total; first += (kThreads / 64) * per_wave) {
-        const int item = first + sub;
-        const bool on = sub < per_wave && item < total;
-        const int i = on ? item / per_token : 0, h = on ? item - i * per_token : 0;
-        const int64_t t = t0 + i;
-        const bool is_q = h < nq, is_k = !is_q && h < nq + nk;
-        const int kh = is_q ? 0 : (is_k ? h - nq : h - nq - nk);
-        const char *src = is_q ? p.q + t * p.q_ts + h * p.q_hs
-                               : (is_k ? p.k + t * p.k_ts + kh * p.k_hs : p.v + t * p.v_ts + kh * p.v_hs);
-        u32x4 raw = {0, 0, 0, 0};
-        if (on) raw = *(const u32x4 *)(src + vec * 16);
-        float x[8];
+    // (uniform in the wave: the LDS of ODD is its own)
+    for (int x = start; x - lane < total; x += stride) {
+        u32x4 na = {0, 0, 0, 0}, nb = {0, 0, 0, 0};
+        const Unit next = unit_of(x + stride);
+        fetch(next, na, nb);
+        const bool is_q = u.head < nq, is_k = !is_q && u.head < nq + nk;
+        const float *c = trig + u.token * half4, *s = c + n * half4;
+        float xa[8], xb[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = to_f32<BF16>((raw[e / 2] >> (16 * (e & 1))) & 0xffff);
-        const bool turned = on && (is_q || is_k);
-        const float *c = trig + i * p.half, *s = c + n * p.half;
-        if (p.interleaved) {
-            if (turned)
+        for (int e = 0; e < 8; ++e) {
+            xa[e] = to_f32<BF16>((ra[e / 2] >> (16 * (e & 1))) & 0xffff);
+            xb[e] = to_f32<BF16>((rb[e / 2] >> (16 * (e & 1))) & 0xffff);
+        }
+        const bool turned = u.on && (is_q || is_k);
+        if constexpr (PAIR == HALF) {
+            if (turned && u.a < p.half / 8) {
+                f32x4 cc[2], ss[2];
 #pragma unroll
-                for (int e = 0; e < 8; e += 2) {
-                    const int j = vec * 4 + e / 2;
-                    if (j < p.half) {
-                        const float a = x[e], b = x[e + 1];
-                        x[e] = __builtin_fmaf(a, c[j], -b * s[j]);
-                        x[e + 1] = __builtin_fmaf(a, s[j], b * c[j]);
-                    }
+                for (int g = 0; g < 2; ++g) {
+                    cc[g] = *(const f32x4 *)(c + u.a * 8 + g * 4);
+                    ss[g] = *(const f32x4 *)(s + u.a * 8 + g * 4);
                 }
-        } else {
-            // partners half a rotated part away, by way of LDS (the wave's own rows)
-            uint16_t *mine = (uint16_t *)rows[wave] + sub * p.vecs * 8;
-            if (on) *(u32x4 *)(mine + vec * 8) = raw;
-            __builtin_amdgcn_wave_barrier();
-            if (turned)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    const int d = vec * 8 + e;
-                    if (d < p.half) {
-                        x[e] = __builtin_fmaf(x[e], c[d], -to_f32<BF16>(mine[d + p.half]) * s[d]);
-                    } else if (d < 2 * p.half) {
-                        const int j = d - p.half;
-                        x[e] = __builtin_fmaf(to_f32<BF16>(mine[j]), s[j], x[e] * c[j]);
+                    const float a = xa[e], b = xb[e], co = cc[e / 4][e % 4], si = ss[e / 4][e % 4];
+                    xa[e] = __builtin_fmaf(a, co, -b * si);
+                    xb[e] = __builtin_fmaf(a, si, b * co);
+                }
+            }
+        } else if constexpr (PAIR == INTERLEAVED) {
+            if (turned)
+#pragma unroll
+                for (int v = 0; v < 2; ++v) {
+                    const int j0 = (v ? u.b : u.a) * 4;
+                    if (j0 < 0 || j0 >= p.half) continue;
+                    const f32x4 co = *(const f32x4 *)(c + j0), si = *(const f32x4 *)(s + j0);
+                    float *y = v ? xb : xa;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float a = y[2 * e], b = y[2 * e + 1];
+                        if (j0 + e < p.half) {
+                            y[2 * e] = __builtin_fmaf(a, co[e], -b * si[e]);
+                            y[2 * e + 1] = __builtin_fmaf(a, si[e], b * co[e]);
+                        }
                     }
                 }
-            __builtin_amdgcn_wave_barrier();
-        }
-        if (!on) continue;
-        if (is_q) {
-            const u32x4 y = {pack2<BF16>(x[0], x[1]), pack2<BF16>(x[2], x[3]), pack2<BF16>(x[4], x[5]),
-                             pack2<BF16>(x[6], x[7])};
-            *(u32x4 *)(p.q_out + t * p.o_ts + h * p.o_hs + vec * 16) = y;
-            continue;
-        }
-        const int32_t r = where_req[i], index = where_index[i];
-        if (r < 0 || index < 0) continue;
-        uint32_t row;
-        const int32_t id = block_of(p.cache, r, (uint32_t)index, row);
-        if (id < 0) continue;
-        char *dst = p.cache.layer + (is_k ? 0 : p.cache.kv_stride) +
-                    (((int64_t)id * p.cache.block16 + (int64_t)row * p.cache.row16) << 4) +
-                    (int64_t)kh * p.cache.head_bytes;
-        if constexpr (F8) {
-            const float *scale = is_k ? p.k_scale : p.v_scale;
-            if (scale) {
-                const float by = scale[kh];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) x[e] /= by;
-            }
-            const u32x2 y = {pack4_f8(x[0], x[1], x[2], x[3]), pack4_f8(x[4], x[5], x[6], x[7])};
-            *(u32x2 *)(dst + vec * 8) = y;
         } else {
-            const u32x4 y = {pack2<BF16>(x[0], x[1]), pack2<BF16>(x[2], x[3]), pack2<BF16>(x[4], x[5]),
-                             pack2<BF16>(x[6], x[7])};
-            *(u32x4 *)(dst + vec * 16) = is_k ? y : raw;
+            const int first = lane / p.row_units * p.row_units;            // lane of the row's first unit
+            uint16_t *mine = (uint16_t *)rows[wave] + first * 16;
+            __builtin_amdgcn_wave_barrier();
+            if (u.on) {
+                *(u32x4 *)(mine + u.a * 8) = ra;
+                if (u.b >= 0) *(u32x4 *)(mine + u.b * 8) = rb;
+            }
+            __builtin_amdgcn_wave_barrier();
+            if (turned)
+#pragma unroll
+                for (int v = 0; v < 2; ++v) {
+                    float *y = v ? xb : xa;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const int d = (v ? u.b : u.a) * 8 + e;
+                        if (d < 0) continue;
+                        if (d < p.half) {
+                            y[e] = __builtin_fmaf(y[e], c[d], -to_f32<BF16>(mine[d + p.half]) * s[d]);
+                        } else if (d < 2 * p.half) {
+                            const int j = d - p.half;
+                            y[e] = __builtin_fmaf(to_f32<BF16>(mine[j]), s[j], y[e] * c[j]);
+                        }
+                    }
+                }
         }
+        if (u.on && (is_q || where_in[u.token])) {
+            const int kh = is_k ? u.head - nq : u.head - nq - nk;
+            char *dst = is_q ? p.q_out + (t0 + u.token) * p.o_ts + u.head * p.o_hs
+                             : p.cache.layer + (is_k ? 0 : p.cache.kv_stride) + ((int64_t)where_row[u.token] << 4) +
+                                   (int64_t)kh * p.cache.head_bytes;
+            const float *scale = is_k ? p.k_scale : p.v_scale;
+            const float by = F8 && !is_q && scale ? 1.0f / scale[kh] : 1.0f;
+#pragma unroll
+            for (int v = 0; v < 2; ++v) {
+                const int vec = v ? u.b : u.a;
+                const float *y = v ? xb : xa;
+                if (vec < 0) continue;
+                if (F8 && !is_q) {
+                    const u32x2 z = {pack4_f8(y[0] * by, y[1] * by, y[2] * by, y[3] * by),
+                                     pack4_f8(y[4] * by, y[5] * by, y[6] * by, y[7] * by)};
+                    *(u32x2 *)(dst + vec * 8) = z;
+                } else {
+                    const u32x4 z = {pack2<BF16>(y[0], y[1]), pack2<BF16>(y[2], y[3]), pack2<BF16>(y[4], y[5]),
+                                     pack2<BF16>(y[6], y[7])};
+                    *(u32x4 *)(dst + vec * 16) = is_q || is_k ? z : (v ? rb : ra);
+                }
+            }
+        }
+        u = next;
+        ra = na;
+        rb = nb;
     }
+}
+
+template <bool BF16, bool F8> auto rope_kernel(Pairing pair) {
+    return pair == HALF ? rope_append_kernel<BF16, F8, HALF>
+                        : (pair == INTERLEAVED ? rope_append_kernel<BF16, F8, INTERLEAVED> : rope_append_kernel<BF16, F8, ODD>);
 }
 
 }  // namespace
@@ -220,16 +300,24 @@ int kv_rope_append(const kv_layout *layout, void *d_layer, const kv_batch *batch
     p.kv_heads = layout->kv_heads;
     p.vecs = d / 8;
     p.half = rot_dim / 2;
-    p.per_block = 4;
     p.magnitude = magnitude;
     p.sign = (flags & KV_ROPE_INVERSE) ? -1.0f : 1.0f;
-    p.interleaved = (flags & KV_ROPE_INTERLEAVED) != 0;
+    const tkv::Pairing pair = (flags & KV_ROPE_INTERLEAVED) ? tkv::INTERLEAVED : (p.half % 8 ? tkv::ODD : tkv::HALF);
+    const int hv = pair == tkv::HALF ? p.half / 8 : 0;
+    p.row_units = hv + (p.vecs - 2 * hv + 1) / 2;
+    p.token_units = p.row_units * (p.q_heads + (k ? 2 * p.kv_heads : 0));
+    p.by_row = tkv::make_divider((uint32_t)p.row_units);
+    p.by_token = tkv::make_divider((uint32_t)p.token_units);
+    p.by_half = tkv::make_divider((uint32_t)(p.half ? p.half : 1));
+    // Eight tokens share a workgroup's start where there are workgroups enough; few tokens take one each.
+    const int64_t share = batch->num_q / 1024;
+    p.per_block = share < 1 ? 1 : (share > tkv::kMaxTokens ? tkv::kMaxTokens : (int)share);
     const int64_t blocks = (batch->num_q + p.per_block - 1) / p.per_block;
     if (blocks >= (int64_t(1) << 31)) return KV_ELIMIT;
-    const size_t lds = (size_t)p.per_block * p.half * 2 * sizeof(float);
+    const size_t lds = (size_t)p.per_block * ((p.half + 3) & ~3) * 2 * sizeof(float);
     const bool f8 = cache_dtype == KV_F8E4M3;
-    auto kernel = dtype == KV_BF16 ? (f8 ? tkv::rope_append_kernel<true, true> : tkv::rope_append_kernel<true, false>)
-                                   : (f8 ? tkv::rope_append_kernel<false, true> : tkv::rope_append_kernel<false, false>);
+    auto kernel = dtype == KV_BF16 ? (f8 ? tkv::rope_kernel<true, true>(pair) : tkv::rope_kernel<true, false>(pair))
+                                   : (f8 ? tkv::rope_kernel<false, true>(pair) : tkv::rope_kernel<false, false>(pair));
     (void)hipGetLastError();
     hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(tkv::kThreads), lds, (hipStream_t)stream, p);
     return hipGetLastError() == hipSuccess ? KV_OK : KV_EHIP;
