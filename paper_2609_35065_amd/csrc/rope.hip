@@ -11,7 +11,7 @@
 namespace tkv {
 namespace {
 
-constexpr int kThreads = 256, kMaxTokens = 8;
+constexpr int kThreads = 256, kMaxTokens = 4;
 
 struct RopeParams {
     Paged cache;
@@ -309,7 +309,7 @@ int kv_rope_append(const kv_layout *layout, void *d_layer, const kv_batch *batch
     p.by_row = tkv::make_divider((uint32_t)p.row_units);
     p.by_token = tkv::make_divider((uint32_t)p.token_units);
     p.by_half = tkv::make_divider((uint32_t)(p.half ? p.half : 1));
-    // Eight tokens share a workgroup's start where there are workgroups enough; few tokens take one each.
+    // Four tokens share a workgroup's start where there are workgroups enough; few tokens take one each.
     const int64_t share = batch->num_q / 1024;
     p.per_block = share < 1 ? 1 : (share > tkv::kMaxTokens ? tkv::kMaxTokens : (int)share);
     const int64_t blocks = (batch->num_q + p.per_block - 1) / p.per_block;
