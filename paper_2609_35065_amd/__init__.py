@@ -11,6 +11,7 @@ from __future__ import annotations
 
 import ctypes as ct
 import os
+import struct
 from array import array
 from typing import List, Optional, Sequence, Tuple
 
@@ -708,20 +709,24 @@ def _dtypes():
 
 
 _dtype_codes = None
+_pack_rows = struct.Struct("=qqqii").pack    # a kv_rows (struct-packed: a third of the cost of a ctypes structure)
 
 
-def _rows(t, batch: KvBatch, layout: KvLayout, what: str) -> KvRows:
-    """Rows [num_q, heads, head_dim] of a device tensor whose last dimension is dense."""
+def _rows(t, num_q: int, head_dim: int, what: str) -> Tuple[bytes, int, int]:
+    """(kv_rows as bytes, heads, kv_dtype) of a device tensor [num_q, heads, head_dim] whose last dimension is dense."""
     if not t.is_cuda:
         raise ValueError(f"{what} must be a device tensor")
-    shape, (ts, hs, es) = t.shape, t.stride() if t.dim() == 3 else (0, 0, 0)
-    if t.dim() != 3 or shape[0] != batch.num_q or shape[2] != layout.head_dim or (es != 1 and shape[2] > 1):
-        raise ValueError(f"{what} must be [{batch.num_q}, heads, {layout.head_dim}] with dense rows, got "
-                         f"{tuple(t.shape)} with strides {t.stride()}")
-    code = _dtypes().get(t.dtype)
+    shape = t.shape
+    if len(shape) != 3 or shape[0] != num_q or shape[2] != head_dim:
+        raise ValueError(f"{what} must be [{num_q}, heads, {head_dim}], got {tuple(shape)}")
+    ts, hs, es = t.stride()
+    if es != 1 and head_dim > 1:
+        raise ValueError(f"{what} must have dense rows, got strides {t.stride()}")
+    code = (_dtype_codes or _dtypes()).get(t.dtype)
     if code is None:
         raise ValueError(f"{what} must be bfloat16 or float16, got {t.dtype}")
-    return KvRows(t.data_ptr(), ts, hs, shape[1], code)
+    heads = shape[1]
+    return _pack_rows(t.data_ptr(), ts, hs, heads, code), heads, code
 
 
 def _cache_code(cache_dtype, layout: KvLayout, dtype: int) -> int:
@@ -758,22 +763,29 @@ def kv_rope_append(layout: KvLayout, layer, batch: KvBatch, q, k, v, d_freqs, *,
     """Rotate q into q_out (default: in place) and append rotated k, and v, to the cache.  q, or both k and v, may be
     None; layer may be None without k and v."""
     torch = _torch()
-    if q is None and k is None:
-        raise ValueError("nothing to do: q and k are both None")
-    if (k is None) != (v is None):
+    n, d = batch.num_q, layout.head_dim
+    rq = ro = rk = rv = None
+    code = -1
+    if q is not None:
+        rq, _, code = _rows(q, n, d, "q")
+        ro = rq if q_out is None else _rows(q_out, n, d, "q_out")[0]
+    if k is not None:
+        rk, _, code = _rows(k, n, d, "k")
+    if v is not None:
+        rv = _rows(v, n, d, "v")[0]
+    if (rk is None) != (rv is None):
         raise ValueError("k and v go together")
-    refs = [None if t is None else _rows(t, batch, layout, what)
-            for t, what in ((q, "q"), (q if q_out is None else q_out, "q_out"), (k, "k"), (v, "v"))]
-    code = _cache_code(cache_dtype, layout, (refs[0] or refs[2]).dtype)
-    if positions is not None and not isinstance(positions, int) and positions.numel() != batch.num_q:
+    if code < 0:
+        raise ValueError("nothing to do: q and k are both None")
+    if positions is not None and not isinstance(positions, int) and positions.numel() != n:
         raise ValueError("positions must hold one position per row")
     _check(lib().kv_rope_append(ct.addressof(layout), None if layer is None else _dptr(layer, None, "layer"),
-                                ct.addressof(batch), *[None if r is None else ct.addressof(r) for r in refs],
-                                _dptr(d_freqs, torch.float64, "freqs"), 2 * d_freqs.numel(),
-                                KV_ROPE_INTERLEAVED * bool(interleaved) | KV_ROPE_INVERSE * bool(inverse), magnitude,
-                                None if positions is None else _dptr(positions, torch.int32, "positions"), code,
-                                _scale_ptr(k_scale, layout, "k_scale"), _scale_ptr(v_scale, layout, "v_scale"),
-                                _stream(stream)), "kv_rope_append")
+                                ct.addressof(batch), rq, ro, rk, rv, _dptr(d_freqs, torch.float64, "freqs"),
+                                2 * d_freqs.numel(),
+                                (KV_ROPE_INTERLEAVED if interleaved else 0) | (KV_ROPE_INVERSE if inverse else 0),
+                                magnitude, None if positions is None else _dptr(positions, torch.int32, "positions"),
+                                _cache_code(cache_dtype, layout, code), _scale_ptr(k_scale, layout, "k_scale"),
+                                _scale_ptr(v_scale, layout, "v_scale"), _stream(stream)), "kv_rope_append")
 
 
 def kv_paged_attention_workspace(layout: KvLayout, batch: KvBatch, q_heads: int, window: int = 0) -> int:
@@ -788,13 +800,14 @@ def kv_paged_attention(layout: KvLayout, layer, batch: KvBatch, q, out, scale: f
                        window: int = 0, lse=None, k_scale=None, v_scale=None, cache_dtype=None, workspace=None,
                        stream=None) -> None:
     """Attention of the batch's rows over the paged cache, into out (and lse, float32 [num_q, heads])."""
-    rq, ro = _rows(q, batch, layout, "q"), _rows(out, batch, layout, "out")
+    n, d = batch.num_q, layout.head_dim
+    rq, heads, code = _rows(q, n, d, "q")
+    ro = _rows(out, n, d, "out")[0]
     ws, size = (None, 0) if workspace is None else (_dptr(workspace, None, "workspace"), workspace.nbytes)
-    if lse is not None and lse.numel() != batch.num_q * rq.heads:
+    if lse is not None and lse.numel() != n * heads:
         raise ValueError("lse must be [rows, heads]")
-    _check(lib().kv_paged_attention(ct.addressof(layout), _dptr(layer, None, "layer"), ct.addressof(batch),
-                                    ct.addressof(rq), ct.addressof(ro), scale, 1 if causal else 0, window,
-                                    _cache_code(cache_dtype, layout, rq.dtype),
+    _check(lib().kv_paged_attention(ct.addressof(layout), _dptr(layer, None, "layer"), ct.addressof(batch), rq, ro,
+                                    scale, 1 if causal else 0, window, _cache_code(cache_dtype, layout, code),
                                     _scale_ptr(k_scale, layout, "k_scale"), _scale_ptr(v_scale, layout, "v_scale"),
                                     None if lse is None else _dptr(lse, _torch().float32, "lse"), ws, size,
                                     _stream(stream)), "kv_paged_attention")
@@ -806,16 +819,16 @@ def kv_attention_weights(layout: KvLayout, layer, batch: KvBatch, q, lse, weight
     """weights (float32 [requests, kv_heads, n]) = decay * weights + the attention that each cached token receives
     from the batch's rows; lse as kv_paged_attention left it."""
     torch = _torch()
-    rq = _rows(q, batch, layout, "q")
-    if lse.numel() != batch.num_q * rq.heads:
+    rq, heads, code = _rows(q, batch.num_q, layout.head_dim, "q")
+    if lse.numel() != batch.num_q * heads:
         raise ValueError("lse must be [rows, heads]")
-    if weights.dim() != 3 or weights.shape[0] != batch.num_reqs or weights.shape[1] != layout.kv_heads:
+    shape = weights.shape
+    if len(shape) != 3 or shape[0] != batch.num_reqs or shape[1] != layout.kv_heads:
         raise ValueError("weights must be [requests, kv_heads, n]")
     _check(lib().kv_attention_weights(ct.addressof(layout), _dptr(layer, None, "layer"), ct.addressof(batch),
-                                      ct.addressof(rq), _dptr(lse, torch.float32, "lse"), scale, 1 if causal else 0,
-                                      window, _cache_code(cache_dtype, layout, rq.dtype),
-                                      _scale_ptr(k_scale, layout, "k_scale"), decay,
-                                      _dptr(weights, torch.float32, "weights"), weights.shape[2], _stream(stream)),
+                                      rq, _dptr(lse, torch.float32, "lse"), scale, 1 if causal else 0, window,
+                                      _cache_code(cache_dtype, layout, code), _scale_ptr(k_scale, layout, "k_scale"),
+                                      decay, _dptr(weights, torch.float32, "weights"), shape[2], _stream(stream)),
            "kv_attention_weights")
 
 

@@ -603,34 +603,70 @@ __global__ __launch_bounds__(kThreads, DP > 128 ? 1 : 2) void attention_many_ker
     else many_rows<T, F8, DP>(p, tile, h, split, lds, &odd);
 }
 
-// Join the parts of each row: one wave a row.
+// Join the parts of each row: one wave a row, each half of it every other
+// part, eight elements a lane; the parts' sums and values are loaded together.
 template <class T>
 __global__ __launch_bounds__(kThreads) void attention_join_kernel(AttentionParams p) {
-    const int lane = threadIdx.x & 63;
+    const int lane = threadIdx.x & 63, half = lane >> 5, d = (lane & 31) * 8;
     const int64_t all = p.cache.num_q * p.q_heads, row = (int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6);
     if (row >= all) return;
-    const int64_t q = row / p.q_heads;
-    const int head = (int)(row % p.q_heads);
-    float m = -INFINITY, l = 0.0f;
-    if (lane < p.splits) {
-        m = p.part_ml[(lane * all + row) * 2];
-        l = p.part_ml[(lane * all + row) * 2 + 1];
-    }
-    float top = m;
+    f32x2 ml = {-INFINITY, 0.0f};
+    if (lane < p.splits) ml = *(const f32x2 *)(p.part_ml + (lane * all + row) * 2);
+    const float *at = p.part_o + row * p.head_dim + d;
+    const bool in = d < p.head_dim;
+    constexpr int kAhead = 4;
+    f32x4 x[kAhead], y[kAhead];
+    const auto load = [&](int s0) {
 #pragma unroll
-    for (int x = 1; x < 64; x *= 2) top = fmaxf(top, __shfl_xor(top, x));
-    const float by = top == -INFINITY ? 0.0f : exp2_(m - top);
-    l *= by;
+        for (int i = 0; i < kAhead; ++i) {
+            const int s = s0 + 2 * i + half;
+            x[i] = y[i] = f32x4{0, 0, 0, 0};
+            if (in && s < p.splits) {
+                const f32x4 *from = (const f32x4 *)(at + s * all * p.head_dim);
+                x[i] = from[0];
+                y[i] = from[1];
+            }
+        }
+    };
+    load(0);
+    float top = ml[0];
 #pragma unroll
-    for (int x = 1; x < 64; x *= 2) l += __shfl_xor(l, x);
-    const float inv = top == -INFINITY ? 0.0f : (p.v_scale ? p.v_scale[head / p.group] : 1.0f) / l;
-    const int d = lane * 4;                // head_dim is at most 256
-    f32x4 acc = {0, 0, 0, 0};
-    for (int s = 0; s < p.splits; ++s) {
-        const float w = __shfl(by, s);
-        if (w != 0.0f && d < p.head_dim) acc += *(const f32x4 *)(p.part_o + (s * all + row) * p.head_dim + d) * w;
+    for (int i = 1; i < 32; i *= 2) top = fmaxf(top, __shfl_xor(top, i));
+    const f32x2 tops = both_halves(top);
+    top = fmaxf(tops[0], tops[1]);
+    const float base = top == -INFINITY ? 0.0f : top, by = exp2_(ml[0] - base);
+    float l = ml[1] * by;
+#pragma unroll
+    for (int i = 1; i < 32; i *= 2) l += __shfl_xor(l, i);
+    const f32x2 ls = both_halves(l);
+    l = ls[0] + ls[1];
+    f32x4 a = {0, 0, 0, 0}, b = {0, 0, 0, 0};
+    for (int s0 = 0; s0 < p.splits; s0 += 2 * kAhead) {
+        if (s0 > 0) load(s0);
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const float w = __shfl(by, s0 + 2 * i + half);     // 0 past the last part, and for one that saw nothing
+            if (w != 0.0f) {
+                a += x[i] * w;
+                b += y[i] * w;
+            }
+        }
     }
-    if (d < p.head_dim) store_out(p, q, head, d, top == -INFINITY ? acc : acc * inv, T::kBf16);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const f32x2 u = both_halves(a[e]), v = both_halves(b[e]);
+        a[e] = u[0] + u[1];
+        b[e] = v[0] + v[1];
+    }
+    const int64_t q = (uint32_t)row / (uint32_t)p.q_heads;
+    const int head = (int)(row - q * p.q_heads);
+    const float inv = top == -INFINITY ? 0.0f : (p.v_scale ? p.v_scale[(int)divide(head, p.by_group)] : 1.0f) / l;
+    if (half == 0 && in) {
+        char *to = p.out + q * p.o_ts + head * p.o_hs + d * 2;
+        if (top == -INFINITY) *(u32x4 *)to = u32x4{0, 0, 0, 0};
+        else *(u32x4 *)to = u32x4{pack2<T>(a[0] * inv, a[1] * inv), pack2<T>(a[2] * inv, a[3] * inv),
+                                  pack2<T>(b[0] * inv, b[1] * inv), pack2<T>(b[2] * inv, b[3] * inv)};
+    }
     if (lane == 0 && p.lse) p.lse[row] = top == -INFINITY ? -INFINITY : (top + log2_(l)) * kLn2;
 }
 
