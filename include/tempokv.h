@@ -403,7 +403,7 @@ typedef struct kv_rows {
 
 /* A ragged batch of new tokens and the cache they belong to.  Request r has
  * the rows d_q_off[r] .. d_q_off[r+1] (n_r of them) and, these included,
- * d_kv_len[r] tokens in the cache: new token i has cache index
+ * d_kv_len[r] tokens (up to 2^30) in the cache: new token i has cache index
  * d_kv_len[r] - n_r + i, and cache index t lies at row t % B of the block
  * d_block_tables[r*bt_stride + t / B].  A block id outside [0, num_blocks) is
  * a missing block, and indices past the table are missing too: nothing is

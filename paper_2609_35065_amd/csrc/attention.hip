@@ -57,7 +57,7 @@ template <int ROWS> __device__ __forceinline__ Tile find_tile(const Paged &c, in
     for (int base = 0; base < c.num_reqs; base += 64) {
         const int r = min(base + lane, c.num_reqs - 1);
         const int64_t first = clamp_row(c, c.q_off[r]), next = clamp_row(c, c.q_off[r + 1]);
-        const int len = c.kv_len[r], tile0 = (int)first * group / ROWS + base + lane;
+        const int len = min(max(c.kv_len[r], 0), kMaxLength), tile0 = (int)first * group / ROWS + base + lane;
         // the last request that starts at or before the tile
         const int n = __popcll(__ballot(base + lane < c.num_reqs && tile0 <= tile));
         if (n == 0) break;
@@ -83,6 +83,14 @@ __device__ __forceinline__ void store_out(const AttentionParams &p, int64_t row,
 template <class T, bool F8> __device__ __forceinline__ float load_one(const char *row, int d) {
     if constexpr (F8) return T::to_f32(T::from_f8(*(const uint8_t *)(row + d), false));
     return T::to_f32(*(const uint16_t *)(row + d * 2));
+}
+
+// A value that is the same in all lanes, as a scalar.
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
+// Start of part i of n steps cut into `parts`.
+__device__ __forceinline__ int part_of(int n, int i, int parts) {
+    return parts == 1 ? n * i : uniform((int)((uint64_t)n * i / parts));
 }
 
 // Bytes of LDS that a body needs.
@@ -125,7 +133,7 @@ __device__ __forceinline__ void few_rows(const AttentionParams &p, const Tile &t
     const int all_hi = (int)max((int64_t)0, p.causal ? min(len, pos_first + 1) : len);
     const int all_lo = (int)(p.window > 0 ? max((int64_t)0, pos_last - p.window + 1) : 0);
     const int steps = end > begin ? (end - begin + kWide - 1) / kWide : 0;
-    const int step0 = (int)((int64_t)steps * split / p.splits), step1 = (int)((int64_t)steps * (split + 1) / p.splits);
+    const int step0 = part_of(steps, split, p.splits), step1 = part_of(steps, split + 1, p.splits);
 
     const float c = p.scale * (F8 && p.k_scale ? p.k_scale[h] : 1.0f);
     const char *kbase = p.cache.layer + (int64_t)h * p.cache.head_bytes;
@@ -351,27 +359,27 @@ __device__ __forceinline__ void many_rows(const AttentionParams &p, const Tile &
                                           int *odd) {
     constexpr int KS = DP / 16, DT = DP / 32;
     constexpr int VEC = F8 ? 16 : 8, VPR = DP / VEC, VL = kStep * VPR / kThreads;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 31, half = lane >> 5;
+    const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), col = lane & 31, half = lane >> 5;
     char *const kbuf = lds, *const vbuf = lds + 2 * kStep * kKeyRow<DP>;
 
-    const int wrow = tile.row0 + wave * 32, myrow = wrow + col;
-    const bool have = myrow < tile.rows, active = wrow < tile.rows;
+    const int wrow = tile.row0 + wave * 32, myrow = wrow + col, last_row = tile.rows - 1;
+    const bool have = myrow < tile.rows;
     const int token = have ? (int)divide(myrow, p.by_group) : 0;
     const int head = h * p.group + (have ? myrow - token * p.group : 0);
-    const int32_t len_raw = tile.kv_len;
-    const int64_t len = min((int64_t)(len_raw < 0 ? 0 : len_raw), (int64_t)p.cache.bt_stride * p.cache.block_size);
-    const int64_t ahead = (int64_t)len_raw - divide(tile.rows, p.by_group);    // cache index of the first token
+    const int len_raw = tile.kv_len;
+    const int len = (int)min((int64_t)max(len_raw, 0), (int64_t)p.cache.bt_stride * p.cache.block_size);
+    const int ahead = len_raw - (int)divide(tile.rows, p.by_group);    // cache index of the first token
     // keys that rows see, lo <= j < hi: this lane's, those that all or any of the wave's rows see, those of the tile
-    const auto hi_of = [&](int64_t tok) { return (int)max((int64_t)0, p.causal ? min(len, ahead + tok + 1) : len); };
-    const auto lo_of = [&](int64_t tok) { return (int)(p.window > 0 ? max((int64_t)0, ahead + tok - p.window + 1) : 0); };
+    const auto hi_of = [&](int tok) { return max(0, p.causal ? min(len, ahead + tok + 1) : len); };
+    const auto lo_of = [&](int tok) { return p.window > 0 ? max(0, ahead + tok - p.window + 1) : 0; };
+    const auto token_of = [&](int row) { return uniform((int)divide(min(row, last_row), p.by_group)); };
     const int hi = have ? hi_of(token) : 0, lo = lo_of(token);
-    const int last_row = tile.rows - 1;
-    const int64_t wfirst = divide(min(wrow, last_row), p.by_group), wlast = divide(min(wrow + 31, last_row), p.by_group);
-    const int64_t first = divide(tile.row0, p.by_group), last = divide(min(tile.row0 + kRows - 1, last_row), p.by_group);
-    const int all_hi = hi_of(wfirst), all_lo = lo_of(wlast), any_hi = active ? hi_of(wlast) : 0, any_lo = lo_of(wfirst);
+    const int wfirst = token_of(wrow), wlast = token_of(wrow + 31), first = token_of(tile.row0), last = token_of(tile.row0 + kRows - 1);
+    const int all_hi = hi_of(wfirst), all_lo = lo_of(wlast), any_hi = wrow < tile.rows ? hi_of(wlast) : 0, any_lo = lo_of(wfirst);
+    const int tile_hi = hi_of(first), tile_lo = lo_of(last);
     const int end = hi_of(last), begin = lo_of(first) & ~(kStep - 1);
     const int steps = end > begin ? (end - begin + kStep - 1) / kStep : 0;
-    const int step0 = (int)((int64_t)steps * split / p.splits), step1 = (int)((int64_t)steps * (split + 1) / p.splits);
+    const int step0 = part_of(steps, split, p.splits), step1 = part_of(steps, split + 1, p.splits);
 
     u32x4 qf[KS];
 #pragma unroll
@@ -384,37 +392,51 @@ __device__ __forceinline__ void many_rows(const AttentionParams &p, const Tile &
     const char *kbase = p.cache.layer + (int64_t)h * p.cache.head_bytes;
     const char *vbase = kbase + p.cache.kv_stride;
 
-    const int tile_hi = hi_of(first), tile_lo = lo_of(last);
     uint64_t there = 0, there_next = 0;        // bit k: key k of the step is in the cache
     const auto is_mixed = [&](uint64_t there, int t0) { return there != ~uint64_t(0) || t0 < tile_lo || t0 + kStep > tile_hi; };
     if (tid == 0) *odd = 0;
     __syncthreads();
 
-    // staging: one lane looks up one key of a step; vectors x = i kThreads + tid
+    // Staging.  A lane looks up one key of a step, two steps ahead (the table's answer is not looked at before it is
+    // needed); then all load vectors x = i kThreads + tid, one step ahead.
+    const int32_t *const table = p.cache.bt + (int64_t)tile.req * p.cache.bt_stride;
     u32x4 kreg[VL], vreg[VL];
     int32_t id = -1;
     uint32_t id_row = 0;
     const auto look_up = [&](int step) {
-        const int t = begin + step * kStep + lane;
-        id = step < step1 && t < end ? block_of(p.cache, tile.req, (uint32_t)t, id_row) : -1;
+        const uint32_t t = begin + step * kStep + lane, blk = divide(t, p.cache.by_block);
+        id_row = t - blk * p.cache.block_size;
+        id = -1;
+        if (step < step1 && t < (uint32_t)end) id = table[blk];        // t < end <= the table's span
+    };
+    const auto offset = [&]() {
+        const bool in = (uint32_t)id < p.cache.blocks;
+        there_next = __ballot(in);
+        return in ? (uint32_t)id * p.cache.block16 + id_row * p.cache.row16 : 0u;
     };
     const auto load = [&]() {
-        const uint32_t off = id < 0 ? 0u : (uint32_t)id * p.cache.block16 + id_row * p.cache.row16;
-        there_next = __ballot(id >= 0);
+        const uint32_t off = offset();
+        uint32_t at[VL];
+#pragma unroll
+        for (int i = 0; i < VL; ++i) at[i] = (uint32_t)__shfl((int)off, (i * kThreads + tid) / VPR);
 #pragma unroll
         for (int i = 0; i < VL; ++i) {
-            const int x = i * kThreads + tid, r = x / VPR, vec = x % VPR;
-            const int64_t at = ((int64_t)(uint32_t)__shfl((int)off, r) << 4) + vec * 16;
-            const bool in = vec * VEC < p.head_dim;
-            kreg[i] = in ? *(const u32x4 *)(kbase + at) : u32x4{0, 0, 0, 0};
-            vreg[i] = in ? *(const u32x4 *)(vbase + at) : u32x4{0, 0, 0, 0};
+            // (past a head narrower than DP its last vector is read again, and dropped in stage)
+            const int vec = min((i * kThreads + tid) % VPR, p.cache.head_bytes / 16 - 1);
+            const int64_t x = ((int64_t)at[i] + vec) << 4;
+            kreg[i] = *(const u32x4 *)(kbase + x);
+            vreg[i] = *(const u32x4 *)(vbase + x);
         }
     };
     // A value that is not finite must reach only the rows that see its key: 0 times it is NaN.  In a step that some
-    // row does not see whole, such values are staged as 0; add_nonfinite adds them to the results that do see them.
+    // row does not see whole, such values are staged as 0; below they are added to the results that do see them.
     const auto stage = [&](int buf, int step) {
-        const int t0 = begin + step * kStep;
-        const bool mixed = is_mixed(there_next, t0);
+        const bool mixed = is_mixed(there_next, begin + step * kStep);
+        if (p.head_dim < DP) {
+#pragma unroll
+            for (int i = 0; i < VL; ++i)
+                if ((i * kThreads + tid) % VPR * VEC >= p.head_dim) kreg[i] = vreg[i] = u32x4{0, 0, 0, 0};
+        }
 #pragma unroll
         for (int i = 0; i < VL; ++i) {
             const int x = i * kThreads + tid, r = x / VPR, vec = x % VPR;
@@ -449,42 +471,50 @@ __device__ __forceinline__ void many_rows(const AttentionParams &p, const Tile &
     if (step0 < step1) load();
     look_up(step0 + 1);
     for (int step = step0; step < step1; ++step) {
-        const int buf = (step - step0) & 1;
+        const int buf = (step - step0) & 1, t0 = begin + step * kStep;
         stage(buf, step);
         there = there_next;
         __syncthreads();
         if (step + 1 < step1) load();
         look_up(step + 2);
-        const int t0 = begin + step * kStep;
         if (t0 >= any_hi || t0 + kStep <= any_lo || !there) continue;
 
         f32x16 s[2];
         const char *kat = kbuf + (buf * kStep + col) * kKeyRow<DP> + half * 16;
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
+            u32x4 kf[KS];
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) kf[ks] = *(const u32x4 *)(kat + x * 32 * kKeyRow<DP> + ks * 32);
+            if (DP <= 128) __builtin_amdgcn_sched_barrier(0);      // the reads are on their way before a product waits
 #pragma unroll
             for (int e = 0; e < 16; ++e) s[x][e] = 0.0f;
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks)
-                s[x] = T::mfma32(*(const u32x4 *)(kat + x * 32 * kKeyRow<DP> + ks * 32), qf[ks], s[x]);
+            for (int ks = 0; ks < KS; ++ks) s[x] = T::mfma32(kf[ks], qf[ks], s[x]);
         }
-        const bool whole = there == ~uint64_t(0) && t0 >= all_lo && t0 + kStep <= all_hi;
-        if (!whole) {
+        if (there != ~uint64_t(0) || t0 < all_lo || t0 + kStep > all_hi) {
+            // bit k: this lane's row sees key 4 half + k, for the k below (x = 32, 8 and 1 times the indices)
+            const int from = min(max(lo - t0, 0), kStep), to = min(max(hi - t0, 0), kStep);
+            uint64_t see = there;
+            see = from < kStep ? see & (~uint64_t(0) << from) : 0;
+            see = to < kStep ? see & ((uint64_t(1) << to) - 1) : see;
+            see >>= 4 * half;
 #pragma unroll
-            for (int x = 0; x < 2; ++x)
+            for (int x = 0; x < 2; ++x) {
+                const uint32_t bits = (uint32_t)(see >> (32 * x));
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int k = x * 32 + 8 * (i / 4) + 4 * half + i % 4;
-                    if (!((there >> k) & 1) || t0 + k < lo || t0 + k >= hi) s[x][i] = -INFINITY;
-                }
+                for (int i = 0; i < 16; ++i) s[x][i] = bits & (1u << (8 * (i / 4) + i % 4)) ? s[x][i] : -INFINITY;
+            }
         }
-        float top = s[0][0];
+        float tops[4];
 #pragma unroll
-        for (int i = 1; i < 16; ++i) top = fmaxf(top, s[0][i]);
+        for (int i = 0; i < 4; ++i) {
+            tops[i] = fmaxf(s[i / 2][i % 2 * 8], s[i / 2][i % 2 * 8 + 1]);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) top = fmaxf(top, s[1][i]);
-        const f32x2 tops = both_halves(top);
-        top = fmaxf(tops[0], tops[1]) * c;
+            for (int e = 2; e < 8; ++e) tops[i] = fmaxf(tops[i], s[i / 2][i % 2 * 8 + e]);
+        }
+        const f32x2 both = both_halves(fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])));
+        const float top = fmaxf(both[0], both[1]) * c;
         if (__any(top > m + kLag)) {
             const float m1 = fmaxf(m, top), b1 = m1 == -INFINITY ? 0.0f : m1, fade = exp2_(m - b1);
             m = m1;
@@ -495,25 +525,26 @@ __device__ __forceinline__ void many_rows(const AttentionParams &p, const Tile &
 #pragma unroll
                 for (int e = 0; e < 16; ++e) o[i][e] *= fade;
         }
-        u32x4 pf[4];
-#pragma unroll
-        for (int x = 0; x < 2; ++x)
-#pragma unroll
-            for (int i = 0; i < 16; i += 2) {
-                const float a = exp2_(__builtin_fmaf(s[x][i], c, -base)), b = exp2_(__builtin_fmaf(s[x][i + 1], c, -base));
-                l += a;
-                l += b;
-                pf[x * 2 + i / 8][i / 2 % 4] = pack2<T>(a, b);
-            }
         const char *vat = vbuf + (buf * kStep + half * 4 + (lane >> 2 & 3)) * kValueRow<DP> + (lane >> 4 & 1) * 32 + (lane & 3) * 8;
+        float sums[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-        for (int kk = 0; kk < 4; ++kk)
+        for (int kk = 0; kk < 4; ++kk) {
+            u32x4 pf;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int i = (kk & 1) * 8 + e * 2;
+                const float a = exp2_(__builtin_fmaf(s[kk / 2][i], c, -base)), b = exp2_(__builtin_fmaf(s[kk / 2][i + 1], c, -base));
+                sums[kk] += a + b;
+                pf[e] = pack2<T>(a, b);
+            }
 #pragma unroll
             for (int i = 0; i < DT; ++i) {
                 const char *at = vat + kk * 16 * kValueRow<DP> + i * 64;
                 const u32x2 a = read_transposed(at), b = read_transposed(at + 8 * kValueRow<DP>);
-                o[i] = T::mfma32(u32x4{a[0], a[1], b[0], b[1]}, pf[kk], o[i]);
+                o[i] = T::mfma32(u32x4{a[0], a[1], b[0], b[1]}, pf, o[i]);
             }
+        }
+        l += (sums[0] + sums[1]) + (sums[2] + sums[3]);
     }
     const f32x2 ls = both_halves(l);
     l = ls[0] + ls[1];
@@ -560,8 +591,8 @@ __device__ __forceinline__ void many_rows(const AttentionParams &p, const Tile &
     for (int step = step0; step < step1; ++step) {
         const int t0 = begin + step * kStep;
         look_up(step);
-        const uint32_t off = id < 0 ? 0u : (uint32_t)id * p.cache.block16 + id_row * p.cache.row16;
-        const uint64_t in = __ballot(id >= 0);
+        const uint32_t off = offset();
+        const uint64_t in = there_next;
         if (!is_mixed(in, t0)) continue;
         for (int k = 0; k < kStep; ++k) {
             const char *v = vbase + ((int64_t)(uint32_t)__shfl((int)off, k) << 4);
@@ -723,7 +754,7 @@ int kv_paged_attention(const kv_layout *layout, const void *d_layer, const kv_ba
     p.by_group = tkv::make_divider((uint32_t)p.group);
     p.head_dim = layout->head_dim;
     p.splits = plan.splits;
-    p.window = window;
+    p.window = window < tkv::kMaxLength ? window : 0;
     p.causal = causal != 0;
     const bool bf16 = q->dtype == KV_BF16, f8 = cache_dtype == KV_F8E4M3;
     const int d = layout->head_dim;

@@ -14,7 +14,7 @@ int check_layout(const kv_layout *lo);
 
 // Operators over the paged cache: checks of their arguments, and the launch
 // plan of the attention.
-constexpr int kMaxHeadDim = 256, kMaxHeads = 65536;
+constexpr int kMaxHeadDim = 256, kMaxHeads = 65536, kMaxLength = 1 << 30;
 constexpr int kSplitRows = 16, kSplitStep = 128;   // rows (query, head of the group) of a small attention tile, and
                                                    // keys that its workgroup takes in one step
 constexpr int kTileRows = 128, kTileStep = 64;     // the same of a large one

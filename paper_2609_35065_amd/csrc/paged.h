@@ -40,6 +40,7 @@ struct Paged {
     int64_t kv_stride;
     int64_t num_blocks;
     int64_t num_q;
+    uint32_t blocks;       // num_blocks, block ids being 31 bits
     uint32_t block16;      // 16-byte units between blocks of a plane
     uint32_t row16;        // and between the token rows of a block
     uint32_t block_size;
@@ -57,6 +58,7 @@ inline Paged make_paged(const kv_layout *lo, const void *layer, const kv_batch *
     p.kv_len = b->d_kv_len;
     p.kv_stride = lo->paged_kv_stride;
     p.num_blocks = lo->num_blocks;
+    p.blocks = (uint32_t)(lo->num_blocks < INT32_MAX ? lo->num_blocks : INT32_MAX);
     p.num_q = b->num_q;
     p.block16 = (uint32_t)(lo->paged_block_stride / 16);
     p.head_bytes = lo->head_dim * lo->elem_bytes;

@@ -55,10 +55,10 @@ __global__ __launch_bounds__(kThreads, DP > 128 ? 1 : 2) void attention_weights_
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 31, half = lane >> 5;
     const int kw = wave % KW, rw = wave / KW;
     const int h = (int)(blockIdx.x % p.kv_heads), r = (int)(blockIdx.x / p.kv_heads);
-    const int32_t len_raw = p.cache.kv_len[r];
+    const int len_raw = min(max(p.cache.kv_len[r], 0), kMaxLength);
     const int64_t first = clamp_row(p.cache, p.cache.q_off[r]);
     const int ntok = (int)max((int64_t)0, clamp_row(p.cache, p.cache.q_off[r + 1]) - first);
-    const int64_t len = min((int64_t)(len_raw < 0 ? 0 : len_raw), p.weight_stride), ahead = len_raw - ntok;
+    const int64_t len = min((int64_t)len_raw, p.weight_stride), ahead = len_raw - ntok;
     const float c = p.scale * (F8 && p.k_scale ? p.k_scale[h] : 1.0f);
     float *out = p.weights + ((int64_t)r * p.kv_heads + h) * p.weight_stride;
 
@@ -229,10 +229,10 @@ __global__ __launch_bounds__(kThreads) void attention_weights_few_kernel(WeightP
     constexpr int KS = DP / 32, LD = F8 ? KS / 2 : KS, KT = kWaveKeys / 16;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, quad = lane >> 4;
     const int h = (int)(blockIdx.x % p.kv_heads), r = (int)(blockIdx.x / p.kv_heads);
-    const int32_t len_raw = p.cache.kv_len[r];
+    const int len_raw = min(max(p.cache.kv_len[r], 0), kMaxLength);
     const int64_t first = clamp_row(p.cache, p.cache.q_off[r]);
     const int ntok = (int)max((int64_t)0, clamp_row(p.cache, p.cache.q_off[r + 1]) - first), nrows = ntok * p.group;
-    const int64_t len = min((int64_t)(len_raw < 0 ? 0 : len_raw), p.weight_stride), ahead = len_raw - ntok;
+    const int64_t len = min((int64_t)len_raw, p.weight_stride), ahead = len_raw - ntok;
     const float c = p.scale * (F8 && p.k_scale ? p.k_scale[h] : 1.0f);
     float *out = p.weights + ((int64_t)r * p.kv_heads + h) * p.weight_stride;
 
@@ -366,7 +366,7 @@ int kv_attention_weights(const kv_layout *layout, const void *d_layer, const kv_
     p.group = q->heads / layout->kv_heads;
     p.by_group = tkv::make_divider((uint32_t)p.group);
     p.head_dim = layout->head_dim;
-    p.window = window;
+    p.window = window < tkv::kMaxLength ? window : 0;
     p.causal = causal != 0;
     // Keys of a workgroup: 256, each wave 64 of its own, or 64, with the waves sharing the rows, where that is needed to
     // give each compute unit two workgroups.  Up to 16 rows take a kernel of their own.
