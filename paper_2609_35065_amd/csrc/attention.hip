@@ -367,15 +367,15 @@ __device__ __forceinline__ void many_rows(const AttentionParams &p, const Tile &
     const int token = have ? (int)divide(myrow, p.by_group) : 0;
     const int head = h * p.group + (have ? myrow - token * p.group : 0);
     const int len_raw = tile.kv_len;
-    const int len = (int)min((int64_t)max(len_raw, 0), (int64_t)p.cache.bt_stride * p.cache.block_size);
+    const int len = uniform((int)min((int64_t)len_raw, (int64_t)p.cache.bt_stride * p.cache.block_size));
     const int ahead = len_raw - (int)divide(tile.rows, p.by_group);    // cache index of the first token
-    // keys that rows see, lo <= j < hi: this lane's, those that all or any of the wave's rows see, those of the tile
+    // keys that rows see, lo <= j < hi: this lane's, those that all of the wave's rows see, and all of the tile's
     const auto hi_of = [&](int tok) { return max(0, p.causal ? min(len, ahead + tok + 1) : len); };
     const auto lo_of = [&](int tok) { return p.window > 0 ? max(0, ahead + tok - p.window + 1) : 0; };
     const auto token_of = [&](int row) { return uniform((int)divide(min(row, last_row), p.by_group)); };
     const int hi = have ? hi_of(token) : 0, lo = lo_of(token);
     const int wfirst = token_of(wrow), wlast = token_of(wrow + 31), first = token_of(tile.row0), last = token_of(tile.row0 + kRows - 1);
-    const int all_hi = hi_of(wfirst), all_lo = lo_of(wlast), any_hi = wrow < tile.rows ? hi_of(wlast) : 0, any_lo = lo_of(wfirst);
+    const int all_hi = hi_of(wfirst), all_lo = lo_of(wlast);
     const int tile_hi = hi_of(first), tile_lo = lo_of(last);
     const int end = hi_of(last), begin = lo_of(first) & ~(kStep - 1);
     const int steps = end > begin ? (end - begin + kStep - 1) / kStep : 0;
@@ -477,21 +477,39 @@ __device__ __forceinline__ void many_rows(const AttentionParams &p, const Tile &
         __syncthreads();
         if (step + 1 < step1) load();
         look_up(step + 2);
-        if (t0 >= any_hi || t0 + kStep <= any_lo || !there) continue;
 
+        // S: the reads of K are ahead of the products, of the second half among those of the first
         f32x16 s[2];
         const char *kat = kbuf + (buf * kStep + col) * kKeyRow<DP> + half * 16;
+        u32x4 kf[2][KS];
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
-            u32x4 kf[KS];
+        for (int ks = 0; ks < KS; ++ks) kf[0][ks] = *(const u32x4 *)(kat + ks * 32);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks) kf[ks] = *(const u32x4 *)(kat + x * 32 * kKeyRow<DP> + ks * 32);
-            if (DP <= 128) __builtin_amdgcn_sched_barrier(0);      // the reads are on their way before a product waits
+        for (int x = 0; x < 2; ++x)
 #pragma unroll
             for (int e = 0; e < 16; ++e) s[x][e] = 0.0f;
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks) s[x] = T::mfma32(kf[ks], qf[ks], s[x]);
+        for (int ks = 0; ks < KS; ++ks) {
+            s[0] = T::mfma32(kf[0][ks], qf[ks], s[0]);
+            kf[1][ks] = *(const u32x4 *)(kat + 32 * kKeyRow<DP> + ks * 32);
+            __builtin_amdgcn_sched_barrier(0);
         }
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) s[1] = T::mfma32(kf[1][ks], qf[ks], s[1]);
+        // V for the first 16 keys
+        const char *vat = vbuf + (buf * kStep + half * 4 + (lane >> 2 & 3)) * kValueRow<DP> + (lane >> 4 & 1) * 32 + (lane & 3) * 8;
+        u32x4 vf[2][DT];
+        const auto read_v = [&](int kk) {
+#pragma unroll
+            for (int i = 0; i < DT; ++i) {
+                const char *at = vat + kk * 16 * kValueRow<DP> + i * 64;
+                const u32x2 a = read_transposed(at), b = read_transposed(at + 8 * kValueRow<DP>);
+                vf[kk & 1][i] = u32x4{a[0], a[1], b[0], b[1]};
+            }
+        };
+        read_v(0);
+        __builtin_amdgcn_sched_barrier(0);
         if (there != ~uint64_t(0) || t0 < all_lo || t0 + kStep > all_hi) {
             // bit k: this lane's row sees key 4 half + k, for the k below (x = 32, 8 and 1 times the indices)
             const int from = min(max(lo - t0, 0), kStep), to = min(max(hi - t0, 0), kStep);
@@ -525,24 +543,25 @@ __device__ __forceinline__ void many_rows(const AttentionParams &p, const Tile &
 #pragma unroll
                 for (int e = 0; e < 16; ++e) o[i][e] *= fade;
         }
-        const char *vat = vbuf + (buf * kStep + half * 4 + (lane >> 2 & 3)) * kValueRow<DP> + (lane >> 4 & 1) * 32 + (lane & 3) * 8;
         float sums[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-        for (int kk = 0; kk < 4; ++kk) {
-            u32x4 pf;
+        u32x4 pf[2];
+        const auto exponentials = [&](int kk) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const int i = (kk & 1) * 8 + e * 2;
                 const float a = exp2_(__builtin_fmaf(s[kk / 2][i], c, -base)), b = exp2_(__builtin_fmaf(s[kk / 2][i + 1], c, -base));
                 sums[kk] += a + b;
-                pf[e] = pack2<T>(a, b);
+                pf[kk & 1][e] = pack2<T>(a, b);
             }
+        };
+        exponentials(0);
 #pragma unroll
-            for (int i = 0; i < DT; ++i) {
-                const char *at = vat + kk * 16 * kValueRow<DP> + i * 64;
-                const u32x2 a = read_transposed(at), b = read_transposed(at + 8 * kValueRow<DP>);
-                o[i] = T::mfma32(u32x4{a[0], a[1], b[0], b[1]}, pf, o[i]);
-            }
+        for (int kk = 0; kk < 4; ++kk) {
+            if (kk < 3) read_v(kk + 1);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int i = 0; i < DT; ++i) o[i] = T::mfma32(vf[kk & 1][i], pf[kk & 1], o[i]);
+            if (kk < 3) exponentials(kk + 1);
         }
         l += (sums[0] + sums[1]) + (sums[2] + sums[3]);
     }
