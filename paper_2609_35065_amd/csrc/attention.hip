@@ -87,10 +87,14 @@ template <class T, bool F8> __device__ __forceinline__ float load_one(const char
 
 // A value that is the same in all lanes, as a scalar.
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ uint64_t uniform(uint64_t x) {
+    return (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32 |
+           (uint32_t)__builtin_amdgcn_readfirstlane((int)x);
+}
 
 // Start of part i of n steps cut into `parts`.
 __device__ __forceinline__ int part_of(int n, int i, int parts) {
-    return parts == 1 ? n * i : uniform((int)((uint64_t)n * i / parts));
+    return uniform(parts == 1 ? n * i : (int)((uint64_t)n * i / parts));
 }
 
 // Bytes of LDS that a body needs.
@@ -375,9 +379,9 @@ __device__ __forceinline__ void many_rows(const AttentionParams &p, const Tile &
     const auto token_of = [&](int row) { return uniform((int)divide(min(row, last_row), p.by_group)); };
     const int hi = have ? hi_of(token) : 0, lo = lo_of(token);
     const int wfirst = token_of(wrow), wlast = token_of(wrow + 31), first = token_of(tile.row0), last = token_of(tile.row0 + kRows - 1);
-    const int all_hi = hi_of(wfirst), all_lo = lo_of(wlast);
-    const int tile_hi = hi_of(first), tile_lo = lo_of(last);
-    const int end = hi_of(last), begin = lo_of(first) & ~(kStep - 1);
+    const int all_hi = uniform(hi_of(wfirst)), all_lo = uniform(lo_of(wlast));
+    const int tile_hi = uniform(hi_of(first)), tile_lo = uniform(lo_of(last));
+    const int end = uniform(hi_of(last)), begin = uniform(lo_of(first) & ~(kStep - 1));
     const int steps = end > begin ? (end - begin + kStep - 1) / kStep : 0;
     const int step0 = part_of(steps, split, p.splits), step1 = part_of(steps, split + 1, p.splits);
 
@@ -411,7 +415,7 @@ __device__ __forceinline__ void many_rows(const AttentionParams &p, const Tile &
     };
     const auto offset = [&]() {
         const bool in = (uint32_t)id < p.cache.blocks;
-        there_next = __ballot(in);
+        there_next = uniform((uint64_t)__ballot(in));
         return in ? (uint32_t)id * p.cache.block16 + id_row * p.cache.row16 : 0u;
     };
     const auto load = [&]() {
