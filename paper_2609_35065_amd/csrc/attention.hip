@@ -16,11 +16,11 @@
 namespace tkv {
 namespace {
 
-constexpr int kWaves = 4;
+constexpr int kWaves = 4;                  // of a workgroup that takes few rows, and of a join
 constexpr int kThreads = 64 * kWaves;
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 static_assert(kSplitStep == 32 * kWaves, "a wave takes 32 keys a step");
-static_assert(kTileRows == 32 * kWaves && kTileStep == 64, "four waves of 32 rows");
+static_assert(kTileStep == 64, "a lane looks up one key");
 
 struct AttentionParams {
     Paged cache;
@@ -98,7 +98,7 @@ __device__ __forceinline__ int part_of(int n, int i, int parts) {
 }
 
 // Bytes of LDS that a body needs.
-template <int DP> constexpr int kSplitLds = kWaves * 32 * (DP * 2 + 32);
+template <int DP, int W> constexpr int kSplitLds = W * 32 * (DP * 2 + 32);
 
 // Tiles of 16 rows; the keys of a tile are cut into p.splits parts, one
 // workgroup each, and a part's steps of 32 keys go to its waves in turn.
@@ -108,7 +108,7 @@ template <int DP> constexpr int kSplitLds = kWaves * 32 * (DP * 2 + 32);
 // order; so P never leaves its registers.  K is loaded from memory as the
 // matrix operand itself; V goes through LDS, the wave's own, to be read
 // transposed.
-template <class T, bool F8, int DP>
+template <class T, bool F8, int DP, int W>
 __device__ __forceinline__ void few_rows(const AttentionParams &p, const Tile &tile, int h, int split, char *lds,
                                          float (*part)[16][2], int *odd) {
     constexpr int KS = DP / 32, LD = F8 ? KS / 2 : KS, DT = DP / 16;
@@ -184,14 +184,14 @@ __device__ __forceinline__ void few_rows(const AttentionParams &p, const Tile &t
         if (have && d < p.head_dim) qf[ks] = *(const u32x4 *)(p.q + (tile.first + token) * p.q_ts + head * p.q_hs + d * 2);
     }
     if (step0 + wave < step1) load();
-    look_up(step0 + wave + kWaves);
+    look_up(step0 + wave + W);
 
     f32x4 o[DT];
 #pragma unroll
     for (int i = 0; i < DT; ++i) o[i] = f32x4{0, 0, 0, 0};
     float m = -INFINITY, l = 0.0f;
 
-    for (int step = step0 + wave; step < step1; step += kWaves) {
+    for (int step = step0 + wave; step < step1; step += W) {
         const uint64_t there_now = there_next;
 #pragma unroll
         for (int n = 0; n < NS; ++n) {
@@ -227,8 +227,8 @@ __device__ __forceinline__ void few_rows(const AttentionParams &p, const Tile &t
             }
         }
         if (n == NS - 1) {
-            if (step + kWaves < step1) load();
-            look_up(step + 2 * kWaves);
+            if (step + W < step1) load();
+            look_up(step + 2 * W);
         }
         float top = -INFINITY;
 #pragma unroll
@@ -278,7 +278,7 @@ __device__ __forceinline__ void few_rows(const AttentionParams &p, const Tile &t
     }
     __syncthreads();
     const int64_t all = p.cache.num_q * p.q_heads;
-    for (int x = threadIdx.x; x < 16 * DP / 4; x += kThreads) {
+    for (int x = threadIdx.x; x < 16 * DP / 4; x += (64 * W)) {
         const int r = x / (DP / 4), d = x % (DP / 4) * 4;
         const int row = tile.row0 + r, tok = (int)divide(row, p.by_group);
         if (row >= tile.rows || d >= p.head_dim) continue;
@@ -286,11 +286,11 @@ __device__ __forceinline__ void few_rows(const AttentionParams &p, const Tile &t
         const int hd = h * p.group + row - tok * p.group;
         float mm = -INFINITY, ll = 0.0f;
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) mm = fmaxf(mm, part[w][r][0]);
+        for (int w = 0; w < W; ++w) mm = fmaxf(mm, part[w][r][0]);
         const float base = mm == -INFINITY ? 0.0f : mm;
         f32x4 acc = {0, 0, 0, 0};
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
+        for (int w = 0; w < W; ++w) {
             const float by = exp2_(part[w][r][0] - base);
             ll += part[w][r][1] * by;
             const f32x4 y = *(const f32x4 *)((const float *)(lds + w * 32 * kRow) + r * (DP + 4) + d);
@@ -321,7 +321,7 @@ __device__ __forceinline__ void few_rows(const AttentionParams &p, const Tile &t
         for (int k = 0; k < kWide; ++k) {
             const char *v = vbase + ((int64_t)(uint32_t)__shfl((int)off, k) << 4);
             if (!((in >> k) & 1)) continue;
-            for (int x = threadIdx.x; x < 16 * p.head_dim; x += kThreads) {
+            for (int x = threadIdx.x; x < 16 * p.head_dim; x += (64 * W)) {
                 const int r = x / p.head_dim, d = x - r * p.head_dim, row = tile.row0 + r, tok = (int)divide(row, p.by_group);
                 const int64_t at = ahead + tok;
                 if (row >= tile.rows || (p.causal && t0 + k > at) || (p.window > 0 && t0 + k <= at - p.window)) continue;
@@ -340,8 +340,8 @@ __device__ __forceinline__ void few_rows(const AttentionParams &p, const Tile &t
     }
 }
 
-// Tiles of 128 rows, 32 a wave, over steps of 64 keys.  K and V of a step go
-// through LDS for all four waves, one step ahead: loaded into registers while
+// Tiles of 32 rows a wave over steps of 64 keys.  K and V of a step go
+// through LDS for all waves, one step ahead: loaded into registers while
 // the step before is computed, written to the other buffer, one barrier.
 // Again S^T = K Q^T and O^T = V^T P^T, with 32 x 32 products: a lane holds
 // one row's scores for half of the keys, so that a row's maximum and sum need
@@ -353,16 +353,16 @@ __device__ __forceinline__ void few_rows(const AttentionParams &p, const Tile &t
 // l and o (32 bits) nor in P (a rounding relative to its size; 2^8 is far
 // below the 16-bit types' ends).
 constexpr float kLag = 8.0f;
-constexpr int kRows = 32 * kWaves, kStep = 64;
+constexpr int kStep = kTileStep;
 template <int DP> constexpr int kKeyRow = DP * 2 + 16;     // bytes of an LDS row of K: 8 rows on different banks
 template <int DP> constexpr int kValueRow = DP * 2 + (DP * 2 % 128 ? 0 : 64);   // of V: 4 rows, 64 bytes of each
 template <int DP> constexpr int kTileLds = 2 * kStep * (kKeyRow<DP> + kValueRow<DP>);
 
-template <class T, bool F8, int DP>
+template <class T, bool F8, int DP, int W>
 __device__ __forceinline__ void many_rows(const AttentionParams &p, const Tile &tile, int h, int split, char *lds,
                                           int *odd) {
-    constexpr int KS = DP / 16, DT = DP / 32;
-    constexpr int VEC = F8 ? 16 : 8, VPR = DP / VEC, VL = kStep * VPR / kThreads;
+    constexpr int KS = DP / 16, DT = DP / 32, kThreads = 64 * W, kRows = 32 * W;
+    constexpr int VEC = F8 ? 16 : 8, VPR = DP / VEC, kVecs = kStep * VPR, VL = (kVecs + kThreads - 1) / kThreads;
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), col = lane & 31, half = lane >> 5;
     char *const kbuf = lds, *const vbuf = lds + 2 * kStep * kKeyRow<DP>;
 
@@ -422,12 +422,12 @@ __device__ __forceinline__ void many_rows(const AttentionParams &p, const Tile &
         const uint32_t off = offset();
         uint32_t at[VL];
 #pragma unroll
-        for (int i = 0; i < VL; ++i) at[i] = (uint32_t)__shfl((int)off, (i * kThreads + tid) / VPR);
+        for (int i = 0; i < VL; ++i) at[i] = (uint32_t)__shfl((int)off, (i * kThreads + tid) / VPR % kStep);
 #pragma unroll
         for (int i = 0; i < VL; ++i) {
             // (past a head narrower than DP its last vector is read again, and dropped in stage)
             const int vec = min((i * kThreads + tid) % VPR, p.cache.head_bytes / 16 - 1);
-            const int64_t x = ((int64_t)at[i] + vec) << 4;
+            const uint64_t x = ((uint64_t)at[i] + vec) << 4;
             kreg[i] = *(const u32x4 *)(kbase + x);
             vreg[i] = *(const u32x4 *)(vbase + x);
         }
@@ -444,6 +444,7 @@ __device__ __forceinline__ void many_rows(const AttentionParams &p, const Tile &
 #pragma unroll
         for (int i = 0; i < VL; ++i) {
             const int x = i * kThreads + tid, r = x / VPR, vec = x % VPR;
+            if (kVecs % kThreads && x >= kVecs) break;         // (whole waves; what they loaded is not used)
             char *k = kbuf + (buf * kStep + r) * kKeyRow<DP> + vec * VEC * 2;
             char *v = vbuf + (buf * kStep + r) * kValueRow<DP> + vec * VEC * 2;
             u32x4 y[F8 ? 2 : 1];
@@ -633,28 +634,28 @@ __device__ __forceinline__ void many_rows(const AttentionParams &p, const Tile &
 // Every request in tiles of 16 rows.
 template <class T, bool F8, int DP>
 __global__ __launch_bounds__(kThreads) void attention_few_kernel(AttentionParams p) {
-    __shared__ __align__(16) char lds[kSplitLds<DP>];
+    __shared__ __align__(16) char lds[kSplitLds<DP, kWaves>];
     __shared__ float part[kWaves][16][2];
     __shared__ int odd;                        // some value that not all rows see is not finite
     const unsigned id = blockIdx.x;
     const int h = (int)(id % p.kv_heads), split = (int)(id / p.kv_heads % p.splits);
     const Tile tile = find_tile<kSplitRows>(p.cache, (int)(id / p.kv_heads / p.splits), p.group);
-    if (tile.row0 < tile.rows) few_rows<T, F8, DP>(p, tile, h, split, lds, part, &odd);
+    if (tile.row0 < tile.rows) few_rows<T, F8, DP, kWaves>(p, tile, h, split, lds, part, &odd);
 }
 
-// Tiles of 128 rows, from the last to the first (a request's last rows see
-// most keys); a request with no more than 16 rows in all takes the other body.
-template <class T, bool F8, int DP>
-__global__ __launch_bounds__(kThreads, DP > 128 ? 1 : 2) void attention_many_kernel(AttentionParams p) {
-    __shared__ __align__(16) char lds[kTileLds<DP> > kSplitLds<DP> ? kTileLds<DP> : kSplitLds<DP>];
-    __shared__ float part[kWaves][16][2];
+// Large tiles, from the last to the first (a request's last rows see most
+// keys); a request with no more than 16 rows in all takes the other body.
+template <class T, bool F8, int DP, int W>
+__global__ __launch_bounds__(64 * W, DP > 128 ? 1 : 2) void attention_many_kernel(AttentionParams p) {
+    __shared__ __align__(16) char lds[kTileLds<DP> > kSplitLds<DP, W> ? kTileLds<DP> : kSplitLds<DP, W>];
+    __shared__ float part[W][16][2];
     __shared__ int odd;                        // some value that not all rows see is not finite
     const unsigned id = blockIdx.x;
     const int h = (int)(id % p.kv_heads), split = (int)(id / p.kv_heads % p.splits);
-    const Tile tile = find_tile<kRows>(p.cache, (int)p.tiles - 1 - (int)(id / p.kv_heads / p.splits), p.group);
+    const Tile tile = find_tile<32 * W>(p.cache, (int)p.tiles - 1 - (int)(id / p.kv_heads / p.splits), p.group);
     if (tile.row0 >= tile.rows) return;
-    if (tile.rows <= kSplitRows) few_rows<T, F8, DP>(p, tile, h, split, lds, part, &odd);
-    else many_rows<T, F8, DP>(p, tile, h, split, lds, &odd);
+    if (tile.rows <= kSplitRows) few_rows<T, F8, DP, W>(p, tile, h, split, lds, part, &odd);
+    else many_rows<T, F8, DP, W>(p, tile, h, split, lds, &odd);
 }
 
 // Join the parts of each row: one wave a row, each half of it every other
@@ -724,13 +725,21 @@ __global__ __launch_bounds__(kThreads) void attention_join_kernel(AttentionParam
     if (lane == 0 && p.lse) p.lse[row] = top == -INFINITY ? -INFINITY : (top + log2_(l)) * kLn2;
 }
 
-template <class T, bool F8> void (*attention_kernel(bool many, int head_dim))(AttentionParams) {
-    if (head_dim <= 64) return many ? attention_many_kernel<T, F8, 64> : attention_few_kernel<T, F8, 64>;
-    if constexpr (!F8) {
-        if (head_dim <= 96) return many ? attention_many_kernel<T, F8, 96> : attention_few_kernel<T, F8, 96>;
+template <class T, bool F8, int DP> void (*attention_kernel_for(int rows))(AttentionParams) {
+    if (rows == kSplitRows) return attention_few_kernel<T, F8, DP>;
+    if constexpr (DP <= 128) {
+        if (rows == kLargeRows) return attention_many_kernel<T, F8, DP, kLargeRows / 32>;
     }
-    if (head_dim <= 128) return many ? attention_many_kernel<T, F8, 128> : attention_few_kernel<T, F8, 128>;
-    return many ? attention_many_kernel<T, F8, 256> : attention_few_kernel<T, F8, 256>;
+    return attention_many_kernel<T, F8, DP, kTileRows / 32>;
+}
+
+template <class T, bool F8> auto attention_kernel(int rows, int head_dim) {
+    if (head_dim <= 64) return attention_kernel_for<T, F8, 64>(rows);
+    if constexpr (!F8) {
+        if (head_dim <= 96) return attention_kernel_for<T, F8, 96>(rows);
+    }
+    if (head_dim <= 128) return attention_kernel_for<T, F8, 128>(rows);
+    return attention_kernel_for<T, F8, 256>(rows);
 }
 
 }  // namespace
@@ -781,12 +790,12 @@ int kv_paged_attention(const kv_layout *layout, const void *d_layer, const kv_ba
     p.causal = causal != 0;
     const bool bf16 = q->dtype == KV_BF16, f8 = cache_dtype == KV_F8E4M3;
     const int d = layout->head_dim;
-    const bool many = plan.rows != tkv::kSplitRows;
-    auto kernel = bf16 ? (f8 ? tkv::attention_kernel<tkv::Bf16, true>(many, d) : tkv::attention_kernel<tkv::Bf16, false>(many, d))
-                       : (f8 ? tkv::attention_kernel<tkv::F16, true>(many, d) : tkv::attention_kernel<tkv::F16, false>(many, d));
+    auto kernel = bf16 ? (f8 ? tkv::attention_kernel<tkv::Bf16, true>(plan.rows, d) : tkv::attention_kernel<tkv::Bf16, false>(plan.rows, d))
+                       : (f8 ? tkv::attention_kernel<tkv::F16, true>(plan.rows, d) : tkv::attention_kernel<tkv::F16, false>(plan.rows, d));
+    const int threads = plan.rows == tkv::kSplitRows ? tkv::kThreads : 2 * plan.rows;
     hipStream_t s = (hipStream_t)stream;
     (void)hipGetLastError();
-    hipLaunchKernelGGL(kernel, dim3((unsigned)(plan.tiles * p.kv_heads * p.splits)), dim3(tkv::kThreads), 0, s, p);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(plan.tiles * p.kv_heads * p.splits)), dim3(threads), 0, s, p);
     if (p.splits > 1) {
         auto join = bf16 ? tkv::attention_join_kernel<tkv::Bf16> : tkv::attention_join_kernel<tkv::F16>;
         hipLaunchKernelGGL(join, dim3((unsigned)((all + tkv::kWaves - 1) / tkv::kWaves)), dim3(tkv::kThreads), 0, s, p);

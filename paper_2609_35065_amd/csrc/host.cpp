@@ -71,7 +71,7 @@ int check_rows(const kv_rows *x, int64_t num, int32_t head_dim, bool written) {
 }
 
 // Into how many parts each tile's keys are cut: enough for two workgroups on
-// each compute unit, but no part shorter than one step of its four waves.
+// each compute unit, but no part shorter than a step.
 int32_t attention_splits(int64_t tiles, int32_t kv_heads, int64_t span, int32_t step) {
     const int64_t base = tiles * kv_heads, want = 512;
     if (base <= 0 || base >= want) return 1;
@@ -88,9 +88,13 @@ int plan_attention(const kv_layout *lo, const kv_batch *b, int32_t q_heads, int3
     if (b->num_q >= (int64_t(1) << 30) / q_heads) return KV_ELIMIT;       // rows are counted in 32 bits
     int64_t span = b->max_kv_len;
     if (window > 0 && span > (int64_t)window + b->max_q_len) span = (int64_t)window + b->max_q_len;
-    plan->rows = b->max_q_len * group > kSplitRows ? kTileRows : kSplitRows;
+    // Tiles of 256 rows read K and V half as often as those of 128, but take a compute unit each: where there are four
+    // rounds of them (8 x 2,048 tokens of 32 heads: 859 against 917 us; a mixed batch of fewer: 77 against 61 us).
+    const bool many = b->max_q_len * group > kSplitRows;
+    const bool large = lo->head_dim <= 128 && b->num_q * group / kLargeRows * lo->kv_heads >= 1024;
+    plan->rows = !many ? kSplitRows : (large ? kLargeRows : kTileRows);
     plan->tiles = b->num_q * group / plan->rows + b->num_reqs;
-    plan->splits = attention_splits(plan->tiles, lo->kv_heads, span, plan->rows == kTileRows ? kTileStep : kSplitStep);
+    plan->splits = attention_splits(plan->tiles, lo->kv_heads, span, many ? kTileStep : kSplitStep);
     plan->workspace = plan->splits > 1 ? (int64_t)plan->splits * b->num_q * q_heads * (lo->head_dim + 2) * 4 : 0;
     if (plan->tiles * lo->kv_heads * plan->splits >= (int64_t(1) << 31)) return KV_ELIMIT;
     return KV_OK;

@@ -17,11 +17,11 @@ int check_layout(const kv_layout *lo);
 constexpr int kMaxHeadDim = 256, kMaxHeads = 65536, kMaxLength = 1 << 30;
 constexpr int kSplitRows = 16, kSplitStep = 128;   // rows (query, head of the group) of a small attention tile, and
                                                    // keys that its workgroup takes in one step
-constexpr int kTileRows = 128, kTileStep = 64;     // the same of a large one
+constexpr int kTileRows = 128, kLargeRows = 256, kTileStep = 64;   // the same of a tile for many rows, small or large
 constexpr int kMaxSplits = 64;
 
 struct AttentionPlan {
-    int32_t rows;         // of a tile: kSplitRows or kTileRows
+    int32_t rows;         // of a tile: kSplitRows, kTileRows or kLargeRows
     int64_t tiles;        // row tiles, each for every KV head
     int32_t splits;       // parts that a tile's keys are cut into
     int64_t workspace;    // bytes
