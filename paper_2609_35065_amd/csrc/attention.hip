@@ -358,9 +358,16 @@ template <int DP> constexpr int kKeyRow = DP * 2 + 16;     // bytes of an LDS ro
 template <int DP> constexpr int kValueRow = DP * 2 + (DP * 2 % 128 ? 0 : 64);   // of V: 4 rows, 64 bytes of each
 template <int DP> constexpr int kTileLds = 2 * kStep * (kKeyRow<DP> + kValueRow<DP>);
 
+// Where a step's keys lie (16-byte units from a plane's start), and which of
+// them are in the cache.
+struct Places {
+    uint32_t at[kStep];
+    uint64_t there;
+};
+
 template <class T, bool F8, int DP, int W>
 __device__ __forceinline__ void many_rows(const AttentionParams &p, const Tile &tile, int h, int split, char *lds,
-                                          int *odd) {
+                                          int *odd, Places *places) {
     constexpr int KS = DP / 16, DT = DP / 32, kThreads = 64 * W, kRows = 32 * W;
     constexpr int VEC = F8 ? 16 : 8, VPR = DP / VEC, kVecs = kStep * VPR, VL = (kVecs + kThreads - 1) / kThreads;
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), col = lane & 31, half = lane >> 5;
@@ -399,30 +406,32 @@ __device__ __forceinline__ void many_rows(const AttentionParams &p, const Tile &
     uint64_t there = 0, there_next = 0;        // bit k: key k of the step is in the cache
     const auto is_mixed = [&](uint64_t there, int t0) { return there != ~uint64_t(0) || t0 < tile_lo || t0 + kStep > tile_hi; };
     if (tid == 0) *odd = 0;
-    __syncthreads();
 
-    // Staging.  A lane looks up one key of a step, two steps ahead (the table's answer is not looked at before it is
-    // needed); then all load vectors x = i kThreads + tid, one step ahead.
+    // Staging.  One wave, in turn, looks up the keys of a step, a lane each, and leaves their places for all: the
+    // table's entries are asked for three steps ahead and looked at one step later.  One step ahead all load the
+    // vectors x = i kThreads + tid.
     const int32_t *const table = p.cache.bt + (int64_t)tile.req * p.cache.bt_stride;
     u32x4 kreg[VL], vreg[VL];
     int32_t id = -1;
     uint32_t id_row = 0;
-    const auto look_up = [&](int step) {
+    const auto ask = [&](int step) {
         const uint32_t t = begin + step * kStep + lane, blk = divide(t, p.cache.by_block);
         id_row = t - blk * p.cache.block_size;
         id = -1;
         if (step < step1 && t < (uint32_t)end) id = table[blk];        // t < end <= the table's span
     };
-    const auto offset = [&]() {
+    const auto leave = [&](int step) {
         const bool in = (uint32_t)id < p.cache.blocks;
-        there_next = uniform((uint64_t)__ballot(in));
-        return in ? (uint32_t)id * p.cache.block16 + id_row * p.cache.row16 : 0u;
+        const uint64_t mask = __ballot(in);
+        places[step & 3].at[lane] = in ? (uint32_t)id * p.cache.block16 + id_row * p.cache.row16 : 0u;
+        if (lane == 0) places[step & 3].there = mask;
     };
-    const auto load = [&]() {
-        const uint32_t off = offset();
+    const auto load = [&](int step) {
+        const Places &from = places[step & 3];
+        there_next = uniform(from.there);
         uint32_t at[VL];
 #pragma unroll
-        for (int i = 0; i < VL; ++i) at[i] = (uint32_t)__shfl((int)off, (i * kThreads + tid) / VPR % kStep);
+        for (int i = 0; i < VL; ++i) at[i] = from.at[(i * kThreads + tid) / VPR % kStep];
 #pragma unroll
         for (int i = 0; i < VL; ++i) {
             // (past a head narrower than DP its last vector is read again, and dropped in stage)
@@ -472,16 +481,21 @@ __device__ __forceinline__ void many_rows(const AttentionParams &p, const Tile &
         for (int e = 0; e < 16; ++e) o[i][e] = 0.0f;
     float m = -INFINITY, base = 0.0f, l = 0.0f;
 
-    look_up(step0);
-    if (step0 < step1) load();
-    look_up(step0 + 1);
+    if (wave < 3) {
+        ask(step0 + wave);
+        leave(step0 + wave);
+    }
+    __syncthreads();
+    if (step0 < step1) load(step0);
     for (int step = step0; step < step1; ++step) {
         const int buf = (step - step0) & 1, t0 = begin + step * kStep;
         stage(buf, step);
         there = there_next;
         __syncthreads();
-        if (step + 1 < step1) load();
-        look_up(step + 2);
+        if (step + 1 < step1) load(step + 1);
+        const int turn = (step - step0) % W;
+        if (wave == (turn + 2) % W && step > step0) leave(step + 2);
+        if (wave == (turn + 3) % W) ask(step + 3);
 
         // S: the reads of K are ahead of the products, of the second half among those of the first
         f32x16 s[2];
@@ -614,9 +628,10 @@ __device__ __forceinline__ void many_rows(const AttentionParams &p, const Tile &
     // other lane writes: the barrier is behind both halves' stores)
     for (int step = step0; step < step1; ++step) {
         const int t0 = begin + step * kStep;
-        look_up(step);
-        const uint32_t off = offset();
-        const uint64_t in = there_next;
+        ask(step);
+        const bool here = (uint32_t)id < p.cache.blocks;
+        const uint32_t off = here ? (uint32_t)id * p.cache.block16 + id_row * p.cache.row16 : 0u;
+        const uint64_t in = __ballot(here);
         if (!is_mixed(in, t0)) continue;
         for (int k = 0; k < kStep; ++k) {
             const char *v = vbase + ((int64_t)(uint32_t)__shfl((int)off, k) << 4);
@@ -650,12 +665,13 @@ __global__ __launch_bounds__(64 * W, DP > 128 ? 1 : 2) void attention_many_kerne
     __shared__ __align__(16) char lds[kTileLds<DP> > kSplitLds<DP, W> ? kTileLds<DP> : kSplitLds<DP, W>];
     __shared__ float part[W][16][2];
     __shared__ int odd;                        // some value that not all rows see is not finite
+    __shared__ Places places[4];
     const unsigned id = blockIdx.x;
     const int h = (int)(id % p.kv_heads), split = (int)(id / p.kv_heads % p.splits);
     const Tile tile = find_tile<32 * W>(p.cache, (int)p.tiles - 1 - (int)(id / p.kv_heads / p.splits), p.group);
     if (tile.row0 >= tile.rows) return;
     if (tile.rows <= kSplitRows) few_rows<T, F8, DP, W>(p, tile, h, split, lds, part, &odd);
-    else many_rows<T, F8, DP, W>(p, tile, h, split, lds, &odd);
+    else many_rows<T, F8, DP, W>(p, tile, h, split, lds, &odd, places);
 }
 
 // Join the parts of each row: one wave a row, each half of it every other
