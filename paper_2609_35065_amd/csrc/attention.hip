@@ -305,9 +305,10 @@ __device__ __forceinline__ void few_rows(const AttentionParams &p, const Tile &t
             }
             continue;
         }
-        const float by = mm == -INFINITY ? 0.0f : (F8 && p.v_scale ? p.v_scale[h] : 1.0f) / ll;
-        store_out(p, q, hd, d, mm == -INFINITY ? f32x4{0, 0, 0, 0} : acc * by, T::kBf16);
-        if (d == 0 && p.lse) p.lse[q * p.q_heads + hd] = mm == -INFINITY ? -INFINITY : (mm + log2_(ll)) * kLn2;
+        const bool empty = ll == 0.0f;         // (scores that are all NaN leave the maximum as it began, and a sum of NaN)
+        const float by = empty ? 0.0f : (F8 && p.v_scale ? p.v_scale[h] : 1.0f) / ll;
+        store_out(p, q, hd, d, empty ? f32x4{0, 0, 0, 0} : acc * by, T::kBf16);
+        if (d == 0 && p.lse) p.lse[q * p.q_heads + hd] = empty ? -INFINITY : (mm + log2_(ll)) * kLn2;
     }
     if (!*odd) return;
     __syncthreads();
@@ -604,8 +605,9 @@ __device__ __forceinline__ void many_rows(const AttentionParams &p, const Tile &
             ml[1] = l;
         }
     } else {
-        const float by = m == -INFINITY ? 0.0f : (F8 && p.v_scale ? p.v_scale[h] : 1.0f) / l;
-        if (m == -INFINITY)
+        const bool empty = l == 0.0f;
+        const float by = empty ? 0.0f : (F8 && p.v_scale ? p.v_scale[h] : 1.0f) / l;
+        if (empty)
 #pragma unroll
             for (int i = 0; i < DT; ++i)
 #pragma unroll
@@ -620,7 +622,7 @@ __device__ __forceinline__ void many_rows(const AttentionParams &p, const Tile &
                 const int d = i * 32 + e * 2 + half * 8;
                 if (have && d < p.head_dim) *(u32x4 *)(to + d * 2) = u32x4{a[0], b[0], a[1], b[1]};
             }
-        if (have && half == 0 && p.lse) p.lse[at] = m == -INFINITY ? -INFINITY : (m + log2_(l)) * kLn2;
+        if (have && half == 0 && p.lse) p.lse[at] = empty ? -INFINITY : (m + log2_(l)) * kLn2;
     }
     __syncthreads();
     if (!*odd) return;
@@ -731,14 +733,15 @@ __global__ __launch_bounds__(kThreads) void attention_join_kernel(AttentionParam
     }
     const int64_t q = (uint32_t)row / (uint32_t)p.q_heads;
     const int head = (int)(row - q * p.q_heads);
-    const float inv = top == -INFINITY ? 0.0f : (p.v_scale ? p.v_scale[(int)divide(head, p.by_group)] : 1.0f) / l;
+    const bool empty = l == 0.0f;
+    const float inv = empty ? 0.0f : (p.v_scale ? p.v_scale[(int)divide(head, p.by_group)] : 1.0f) / l;
     if (half == 0 && in) {
         char *to = p.out + q * p.o_ts + head * p.o_hs + d * 2;
-        if (top == -INFINITY) *(u32x4 *)to = u32x4{0, 0, 0, 0};
+        if (empty) *(u32x4 *)to = u32x4{0, 0, 0, 0};
         else *(u32x4 *)to = u32x4{pack2<T>(a[0] * inv, a[1] * inv), pack2<T>(a[2] * inv, a[3] * inv),
                                   pack2<T>(b[0] * inv, b[1] * inv), pack2<T>(b[2] * inv, b[3] * inv)};
     }
-    if (lane == 0 && p.lse) p.lse[row] = top == -INFINITY ? -INFINITY : (top + log2_(l)) * kLn2;
+    if (lane == 0 && p.lse) p.lse[row] = empty ? -INFINITY : (top + log2_(l)) * kLn2;
 }
 
 template <class T, bool F8, int DP> void (*attention_kernel_for(int rows))(AttentionParams) {

@@ -134,6 +134,16 @@ def test_what_a_row_does_not_see_does_not_reach_it(dtype, bad, new, window):
     assert bool(out[0].isfinite().all())
 
 
+@pytest.mark.parametrize("new,length", [(1, 40), (1, 4000), (64, 201), (300, 900)])
+def test_scores_that_are_all_nan_are_not_an_empty_row(new, length):
+    """A row of NaN queries sees keys: its result and its lse are NaN, and no other row's are."""
+    c = ref.Cache([length], heads=2, dim=64, seed=13)
+    q = ref.rows_of(new, 4, 64, torch.bfloat16, c.gen)
+    q[new // 2, 1] = math.nan
+    out = _check(c, [new], q, 0.125)
+    assert bool(out[new // 2, 1].isnan().all()) and int(out.isnan().sum()) == 64
+
+
 def test_extreme_scores():
     """Maxima that grow late and far, and scores that leave one key."""
     for dtype in (torch.bfloat16, torch.float16):
