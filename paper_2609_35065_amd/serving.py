@@ -1,0 +1,102 @@
+"""Serving over a paged cache: new tokens through the operators of one GPU.
+
+``ServedCache`` takes the paged tensors that a retrieve filled (or empty ones)
+and runs, for each step of a ragged batch, every layer's
+    kv_rope_append        the new tokens' rotated keys, and values, into the blocks
+    kv_paged_attention    their attention over all that the cache holds
+    kv_attention_weights  what each cached token received, accumulated
+and between steps, to hold fewer bytes, kv_evict_select and kv_evict_compact.
+A token's cache index changes when others are evicted, its rotary position
+does not, so both are counted.
+
+This module only sequences the calls and owns their buffers; it computes
+nothing itself and never waits for the GPU.
+"""
+from __future__ import annotations
+
+from typing import List, Optional, Sequence
+
+import numpy as np
+import torch
+
+from . import (KvLayout, kv_attention_weights, kv_evict_compact, kv_evict_select, kv_paged_attention,
+               kv_paged_attention_workspace, kv_rope_append, make_batch)
+
+
+class ServedCache:
+    """The cache of ``len(lengths)`` requests, which hold ``lengths`` tokens at positions 0, 1, ... at the start.
+
+    ``layers`` and ``block_tables`` (int32 [requests, n]) are the paged tensors and tables of the copies;
+    ``freqs`` (float64, on the device) and ``magnitude`` come from kv_rope_frequencies.  ``decay`` is the factor on
+    weights accumulated in earlier steps (None: weights are not kept, and nothing can be evicted); ``k_scale`` and
+    ``v_scale`` are float32 [layers, kv_heads] for an 8-bit cache."""
+
+    def __init__(self, layout: KvLayout, layers: Sequence[torch.Tensor], block_tables: torch.Tensor, lengths,
+                 q_heads: int, freqs: torch.Tensor, *, magnitude: float = 1.0, interleaved: bool = False,
+                 scale: Optional[float] = None, window: int = 0, decay: Optional[float] = 1.0,
+                 k_scale: Optional[torch.Tensor] = None, v_scale: Optional[torch.Tensor] = None):
+        self.layout, self.layers, self.block_tables = layout, list(layers), block_tables
+        self.q_heads, self.freqs, self.magnitude, self.interleaved = q_heads, freqs, magnitude, interleaved
+        self.scale = layout.head_dim ** -0.5 if scale is None else scale
+        self.window, self.decay, self.k_scale, self.v_scale = window, decay, k_scale, v_scale
+        self.dev = block_tables.device
+        self.capacity = block_tables.shape[1] * layout.block_size
+        self.lengths = np.asarray(lengths, np.int64).copy()     # tokens that the cache holds
+        self.positions = self.lengths.copy()                    # position of each request's next token
+        if self.lengths.shape != (block_tables.shape[0],) or (self.lengths < 0).any() \
+                or (self.lengths > self.capacity).any():
+            raise ValueError("lengths must hold one length per request, within its block table")
+        self.weights = None
+        if decay is not None:
+            self.weights = torch.zeros((layout.num_layers, len(self.lengths), layout.kv_heads, self.capacity),
+                                       device=self.dev)
+        self.batch, self._workspace, self._lse = None, None, None
+
+    def begin(self, new) -> None:
+        """Start a step: ``new`` tokens of each request (0, 1 or many)."""
+        new = np.asarray(new, np.int64)
+        if new.shape != self.lengths.shape or (new < 0).any() or (self.lengths + new > self.capacity).any():
+            raise ValueError("new must hold one count per request, and leave every request within its block table")
+        self.lengths += new
+        off = np.concatenate([[0], np.cumsum(new)])
+        pos = np.concatenate([np.arange(p, p + n) for p, n in zip(self.positions, new)]).astype(np.int32)
+        self.positions += new
+        up = lambda x: torch.from_numpy(x).to(self.dev)
+        self._positions = up(pos)
+        self.batch = make_batch(up(off), up(self.lengths.astype(np.int32)), self.block_tables, int(off[-1]),
+                                int(new.max(initial=0)), int(self.lengths.max(initial=0)))
+        size = kv_paged_attention_workspace(self.layout, self.batch, self.q_heads, self.window)
+        if size and (self._workspace is None or self._workspace.numel() < size):
+            self._workspace = torch.empty(size, dtype=torch.uint8, device=self.dev)
+        self._lse = torch.empty((self.batch.num_q, self.q_heads), device=self.dev)
+
+    def attend(self, layer: int, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor) -> None:
+        """One layer of the step: q [rows, q_heads, head_dim] is rotated in place, k and v go into the cache, and
+        ``out`` gets the attention of q over the cache."""
+        ks = None if self.k_scale is None else self.k_scale[layer]
+        vs = None if self.v_scale is None else self.v_scale[layer]
+        pool = self.layers[layer]
+        kv_rope_append(self.layout, pool, self.batch, q, k, v, self.freqs, interleaved=self.interleaved,
+                       magnitude=self.magnitude, positions=self._positions, k_scale=ks, v_scale=vs)
+        kv_paged_attention(self.layout, pool, self.batch, q, out, self.scale, window=self.window, lse=self._lse,
+                           k_scale=ks, v_scale=vs, workspace=self._workspace)
+        if self.weights is not None:
+            kv_attention_weights(self.layout, pool, self.batch, q, self._lse, self.weights[layer], self.scale,
+                                 window=self.window, decay=self.decay, k_scale=ks)
+
+    def evict(self, budget: int, sink: int = 0, recent: int = 0) -> List[int]:
+        """Cut every request to ``budget`` tokens per head and layer: the first ``sink``, the last ``recent``, and the
+        most attended of the rest.  Returns how many blocks of each request's table are still in use."""
+        if self.weights is None:
+            raise ValueError("nothing to choose by: this cache keeps no weights")
+        L, R, h, _ = self.weights.shape
+        keep = torch.empty((L, R, h, budget), dtype=torch.int32, device=self.dev)
+        left = torch.empty(R, dtype=torch.int32, device=self.dev)
+        size = torch.from_numpy(self.lengths.astype(np.int32)).to(self.dev)
+        kv_evict_select(self.weights, size, budget, sink, recent, keep, left)
+        kv_evict_compact(self.layout, self.layers, self.block_tables, keep, left, weights=self.weights)
+        # what lies behind the kept tokens belongs to none: new tokens start from 0
+        gone = torch.arange(self.capacity, device=self.dev) >= left[:, None]
+        self.weights.masked_fill_(gone[None, :, None], 0.0)
+        self.lengths = np.minimum(self.lengths, budget)
+        return [int(-(-n // self.layout.block_size)) for n in self.lengths]
