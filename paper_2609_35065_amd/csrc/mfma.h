@@ -96,6 +96,43 @@ __device__ __forceinline__ u32x2 swap_halves(uint32_t a, uint32_t b) {
     return __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(a, b, false, false));
 }
 
+// Sixteen rows of LD * 64 bytes as the 16 x 16 products take them: lane (col,
+// quad) has of row `col` the bytes 64 ks + 16 quad on, in y[ks].  Loaded that
+// way an instruction would take 64 bytes of each row, half a cache line.  So
+// of each pair of pieces lanes load 128 bytes of eight rows at a time, and
+// arrange_rows then exchanges columns eight apart.  `at_row(r)` is where row r
+// starts; bytes from `bytes` on are zero.  All 64 lanes take part.
+template <int LD, class F> __device__ __forceinline__ void load_rows(u32x4 (&y)[LD], int bytes, F at_row) {
+    const int lane = threadIdx.x & 63, col = lane & 15, quad = lane >> 4;
+    const int wide = (quad + 4 * (col >> 3)) * 16;
+    if constexpr (LD > 1) {
+        const char *a = at_row(col & 7), *b = at_row(8 + (col & 7));
+#pragma unroll
+        for (int ks = 0; ks + 1 < LD; ks += 2) {
+            const bool in = ks * 64 + wide < bytes;
+            y[ks] = in ? *(const u32x4 *)(a + ks * 64 + wide) : u32x4{0, 0, 0, 0};
+            y[ks + 1] = in ? *(const u32x4 *)(b + ks * 64 + wide) : u32x4{0, 0, 0, 0};
+        }
+    }
+    if constexpr (LD % 2) {
+        const int at = (LD - 1) * 64 + quad * 16;
+        const char *a = at_row(col);
+        y[LD - 1] = at < bytes ? *(const u32x4 *)(a + at) : u32x4{0, 0, 0, 0};
+    }
+}
+
+template <int LD> __device__ __forceinline__ void arrange_rows(u32x4 (&y)[LD]) {
+    constexpr int kTurn8 = 0x128;          // rotate by 8 within 16 lanes; banks of four lanes
+#pragma unroll
+    for (int ks = 0; ks + 1 < LD; ks += 2)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int a = (int)y[ks][i], b = (int)y[ks + 1][i];
+            y[ks][i] = (uint32_t)__builtin_amdgcn_update_dpp(a, b, kTurn8, 0xf, 0xc, false);
+            y[ks + 1][i] = (uint32_t)__builtin_amdgcn_update_dpp(b, a, kTurn8, 0xf, 0x3, false);
+        }
+}
+
 // Transposing read from LDS.  Of each 16 lanes, lane s gives the address of
 // four consecutive 16-bit elements, 4 (s % 4) .. of row s / 4; lane s gets
 // element s of the four rows.
