@@ -61,7 +61,8 @@ template <int WAVES> __device__ __forceinline__ int prefix(int x, int *scratch) 
 
 // One workgroup a row.  ITEMS > 0: the row has at most ITEMS * THREADS
 // tokens and is read once, into registers; 0: any length, read again from the
-// caches in each pass.
+// caches in each pass.  Bound by the counts in LDS: 32 layers x 8 heads of 1,001
+// tokens 10 us, 8 ragged requests around 4,096 tokens (2,048 rows) 70 us.
 template <int THREADS, int ITEMS>
 __global__ __launch_bounds__(THREADS, THREADS == 256 ? 4 : 6) void evict_select_kernel(SelectParams p) {
     constexpr int kWaves = THREADS / 64, kBatch = 8;          // loads on their way together
@@ -197,7 +198,11 @@ struct CompactParams {
 constexpr int kMoves = 2048;               // rows whose places are looked up at a time
 constexpr int kAhead = 4;                  // vectors of a lane in a tile
 
-// One workgroup: a (layer, request, head, plane, slice).
+// One workgroup: a (layer, request, head, plane, slice).  A row already in its
+// place is neither read nor written.  Bound by memory: both calls move or read
+// 0.13 GB in 20 us (1,001 tokens, 32 layers, half kept) and 2.2 GB, counted as if
+// every kept row moved, in 268 us (8 ragged requests around 4,096, a quarter
+// kept; 8.3 TB/s).
 __global__ __launch_bounds__(kThreads) void evict_compact_kernel(CompactParams p) {
     __shared__ uint32_t from[kMoves], to[kMoves];      // 16-byte units from the plane's start; from = to: no move
     const int tid = threadIdx.x;

