@@ -110,8 +110,8 @@ template <int DP, int W> constexpr int kSplitLds = W * 32 * (DP * 2 + 32);
 // transposed.  Waves share nothing until the end, so that there is no barrier
 // in the loop and each keeps the next step's K and V on their way.
 // Bound by the reads of the cache: 64 requests of 4,096 tokens, 8 KV heads of
-// 128, 1.07 GB in 207 us (5.2 TB/s); 8 of 32,768 in 8 bits, 0.54 GB in 126 us
-// (4.3 TB/s).  P is rounded to the type of the products, relative to the
+// 128, 1.07 GB in 207 us (5.2 TB/s); 8 of 32,768 in 8 bits, 0.54 GB in 128 us
+// (4.2 TB/s).  P is rounded to the type of the products, relative to the
 // running maximum; sums, statistics and results stay in 32 bits.
 template <class T, bool F8, int DP, int W>
 __device__ __forceinline__ void few_rows(const AttentionParams &p, const Tile &tile, int h, int split, char *lds,

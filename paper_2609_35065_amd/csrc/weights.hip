@@ -226,7 +226,7 @@ __global__ __launch_bounds__(kThreads, DP > 128 ? 1 : 2) void attention_weights_
 // Few rows (a decoded token's heads): nothing to share, so that each wave works
 // alone on 64 keys, 16 rows at a time, and all its loads are on their way at
 // once.  A lane has one key (lane % 16) and 4 of 16 rows.  Bound by the reads of
-// K: 64 requests of 4,096 tokens, 8 KV heads of 128, 0.54 GB in 125 us (4.4
+// K: 64 requests of 4,096 tokens, 8 KV heads of 128, 0.54 GB in 123 us (4.5
 // TB/s).  Keys loaded as half cache lines, without the exchange of columns,
 // take 31 against 28.7 us for 32 requests of 4,000 at head size 64, 48 against
 // 42 us at 80 and 96, 124.8 us where 128 takes 125.4.
