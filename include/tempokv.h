@@ -454,8 +454,8 @@ enum { KV_ROPE_HALF = 0,          /* element i with i + rot_dim/2 */
  *              in place; partial overlap is not allowed); both NULL: none
  *   k, v       new keys and values with kv_heads heads: k rotated, v as it
  *              is, both written to the cache at the row's cache index in
- *              cache_dtype (KV_F8E4M3: divided by the scale, rounded to
- *              nearest even, values beyond 448 become 448 with their sign,
+ *              cache_dtype (KV_F8E4M3: multiplied by the scale's reciprocal
+ *              in 32 bits, rounded to nearest even, values beyond 448 become 448 with their sign,
  *              NaN stays); both NULL: the cache is not touched, and d_layer
  *              may be NULL
  * d_freqs float64 [rot_dim/2] in device memory; rot_dim even, 0 <= rot_dim <=
@@ -523,7 +523,8 @@ int kv_attention_weights(const kv_layout *layout, const void *d_layer, const kv_
  *              in ascending order, then -1
  *   d_new_len  int32 [num_reqs]: m
  * sink, recent >= 0, sink + recent <= budget, budget > 0.  One launch.
- * Errors: KV_EINVAL, KV_EHIP. */
+ * Errors: KV_EINVAL, KV_EALIGN, KV_ELIMIT (2^31 rows of weights, or rows of
+ * more than 2^30), KV_EHIP. */
 int kv_evict_select(const float *d_weights, int64_t weight_stride, const int32_t *d_len, int32_t num_layers,
                     int32_t num_reqs, int32_t heads, int32_t budget, int32_t sink, int32_t recent, int32_t *d_keep,
                     int32_t *d_new_len, void *stream);

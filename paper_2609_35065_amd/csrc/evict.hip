@@ -290,7 +290,7 @@ int kv_evict_select(const float *d_weights, int64_t weight_stride, const int32_t
     if (((uintptr_t)d_weights & 3u) || ((uintptr_t)d_len & 3u) || ((uintptr_t)d_keep & 3u) || ((uintptr_t)d_new_len & 3u))
         return KV_EALIGN;
     const int64_t rows = (int64_t)num_layers * num_reqs;
-    if (rows >= (int64_t(1) << 31) / heads) return KV_ELIMIT;
+    if (rows >= (int64_t(1) << 31) / heads || weight_stride > (int64_t(1) << 30)) return KV_ELIMIT;   // indices and rounds in 32 bits
     if (num_reqs == 0) return KV_OK;
     const tkv::SelectParams p = {d_weights, d_len, d_keep, d_new_len, weight_stride, num_reqs, heads, budget, sink, recent};
     (void)hipGetLastError();

@@ -199,11 +199,14 @@ __global__ __launch_bounds__(kThreads) void rope_append_kernel(RopeParams p) {
         } else {
             const int first = lane / p.row_units * p.row_units;            // lane of the row's first unit
             uint16_t *mine = (uint16_t *)rows[wave] + first * 16;
+            // (the wave's own rows: its LDS accesses are in order, and the fences keep them so in the code)
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             __builtin_amdgcn_wave_barrier();
             if (u.on) {
                 *(u32x4 *)(mine + u.a * 8) = ra;
                 if (u.b >= 0) *(u32x4 *)(mine + u.b * 8) = rb;
             }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             __builtin_amdgcn_wave_barrier();
             if (turned)
 #pragma unroll

@@ -169,6 +169,10 @@ def test_select_refuses():
     assert _select(reqs=0, w=None, lens=None, keep=None, new=None) == kv.KV_OK
 
 
+def test_select_refuses_rows_past_its_indices():
+    assert _select(n=(1 << 30) + 1) == kv.KV_ELIMIT
+
+
 def _compact(lo=None, layers=(A,), bt=A, stride=4, reqs=1, heads=2, keep=A, budget=4, new=A, w=None, n=0):
     lo = lo or _layout()
     arr = (ct.c_void_p * len(layers))(*layers) if layers is not None else None
