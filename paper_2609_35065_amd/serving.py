@@ -7,7 +7,9 @@ and runs, for each step of a ragged batch, every layer's
     kv_attention_weights  what each cached token received, accumulated
 and between steps, to hold fewer bytes, kv_evict_select and kv_evict_compact.
 A token's cache index changes when others are evicted, its rotary position
-does not, so both are counted.
+does not, so both are counted.  A sliding window reaches back over positions,
+the operators' over cache indices: an eviction therefore has to leave the
+tokens that a window still reaches.
 
 This module only sequences the calls and owns their buffers; it computes
 nothing itself and never waits for the GPU.
@@ -86,9 +88,16 @@ class ServedCache:
 
     def evict(self, budget: int, sink: int = 0, recent: int = 0) -> List[int]:
         """Cut every request to ``budget`` tokens per head and layer: the first ``sink``, the last ``recent``, and the
-        most attended of the rest.  Returns how many blocks of each request's table are still in use."""
+        most attended of the rest.  Returns how many blocks of each request's table are still in use.  With a window,
+        ``recent`` must be at least ``window - 1`` where a request is cut: those tokens then lie next to one another
+        in the cache as in the text, and a window over indices is one over positions.  (Where no position will reach
+        the window, a cache without one gives the same results.)"""
         if self.weights is None:
             raise ValueError("nothing to choose by: this cache keeps no weights")
+        # (the operators take 2^30 and more as no window)
+        if 0 < self.window < 1 << 30 and recent < self.window - 1 and (self.lengths > budget).any():
+            raise ValueError(f"an eviction has to leave the last {self.window - 1} tokens, which the window reaches, "
+                             f"not {recent}")
         L, R, h, _ = self.weights.shape
         keep = torch.empty((L, R, h, budget), dtype=torch.int32, device=self.dev)
         left = torch.empty(R, dtype=torch.int32, device=self.dev)
