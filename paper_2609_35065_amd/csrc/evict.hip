@@ -233,10 +233,10 @@ __global__ __launch_bounds__(kThreads) void evict_compact_kernel(CompactParams p
             from[i] = a;
             to[i] = b;
         }
-        if (with_weights)
+        if (with_weights)                  // (a lane's places are those that it looked up above)
             for (int at = 0; at < rows; at += kThreads) {
                 const int i = row0 + at + tid;
-                const int32_t src = at + tid < rows ? keep[i] : -1;
+                const int32_t src = at + tid < rows && from[at + tid] != to[at + tid] ? keep[i] : -1;
                 const bool moves = src > i && src < p.weight_stride;
                 const float y = moves ? w[src] : 0.0f;
                 __syncthreads();
