@@ -393,7 +393,8 @@ typedef enum kv_dtype { KV_BF16 = 0, KV_F16 = 1, KV_F8E4M3 = 2 } kv_dtype;
 /* Rows [num_q][heads][head_dim] of new tokens in device memory: element x of
  * head h of token t is at element t*token_stride + h*head_stride + x.
  * d_data and both strides in bytes must be multiples of 16, so that q, k and
- * v may lie side by side as one projection leaves them. */
+ * v may lie side by side as one projection leaves them.  Rows that a call
+ * writes must not lie on one another (KV_EINVAL). */
 typedef struct kv_rows {
     const void *d_data;
     int64_t token_stride, head_stride;   /* elements */

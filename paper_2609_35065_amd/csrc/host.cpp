@@ -58,14 +58,32 @@ int check_batch(const kv_batch *b) {
     return KV_OK;
 }
 
+// Whether rows of `dim` elements at t*ts + h*hs lie on one another (t < num,
+// h < heads, strides >= 0).  Rows whose heads differ by a > 0 and tokens by b
+// the other way are |a hs - b ts| apart, which is least for the two b beside
+// a hs / ts; the usual layouts, one stride past all of the other's rows, need
+// no search.
+static bool rows_overlap(int64_t num, int64_t heads, int64_t ts, int64_t hs, int64_t dim) {
+    typedef __int128 wide;
+    if ((heads > 1 && hs < dim) || (num > 1 && ts < dim)) return true;
+    if (heads <= 1 || num <= 1) return false;
+    if ((wide)ts >= (wide)(heads - 1) * hs + dim || (wide)hs >= (wide)(num - 1) * ts + dim) return false;
+    for (int64_t a = 1; a < heads; ++a) {
+        const wide at = (wide)a * hs;
+        wide b = at / ts;
+        if (b >= num - 1) b = num - 1;
+        if (at - b * ts < dim) return true;
+        if (b + 1 < num && (b + 1) * ts - at < dim) return true;
+    }
+    return false;
+}
+
 int check_rows(const kv_rows *x, int64_t num, int32_t head_dim, bool written) {
     if (!x || x->heads <= 0 || (x->dtype != KV_BF16 && x->dtype != KV_F16)) return KV_EINVAL;
     if (num > 0 && !x->d_data) return KV_EINVAL;
     if (x->heads > kMaxHeads) return KV_ELIMIT;
     if (x->token_stride < 0 || x->head_stride < 0) return KV_EINVAL;
-    // rows that are written must not lie on one another
-    if (written && ((x->heads > 1 && x->head_stride < head_dim) || (num > 1 && x->token_stride < head_dim)))
-        return KV_EINVAL;
+    if (written && rows_overlap(num, x->heads, x->token_stride, x->head_stride, head_dim)) return KV_EINVAL;
     if (((uintptr_t)x->d_data & 15u) || x->token_stride % 8 != 0 || x->head_stride % 8 != 0) return KV_EALIGN;
     return KV_OK;
 }
