@@ -729,13 +729,19 @@ def _rows(t, num_q: int, head_dim: int, what: str) -> Tuple[bytes, int, int]:
     return _pack_rows(t.data_ptr(), ts, hs, heads, code), heads, code
 
 
-def _cache_code(cache_dtype, layout: KvLayout, dtype: int) -> int:
-    """Element type of the cache: given, or float8_e4m3fn for one byte and the queries' type for two."""
+def _cache_code(cache_dtype, layout: KvLayout, dtype: int, layer) -> int:
+    """Element type of the cache: given, or float8_e4m3fn for one byte and the queries' type for two.  A layer's tensor
+    of floating type must be of this one; integers (the bytes of the copies' pools) and addresses have none."""
     if cache_dtype is None:
-        return KV_F8E4M3 if layout.elem_bytes == 1 else dtype
-    code = _dtypes().get(cache_dtype)
-    if code is None:
-        raise ValueError(f"the cache must be bfloat16, float16 or float8_e4m3fn, got {cache_dtype}")
+        code = KV_F8E4M3 if layout.elem_bytes == 1 else dtype
+    else:
+        code = _dtypes().get(cache_dtype)
+        if code is None:
+            raise ValueError(f"the cache must be bfloat16, float16 or float8_e4m3fn, got {cache_dtype}")
+    held = getattr(layer, "dtype", None)
+    if held is not None and (_dtype_codes or _dtypes()).get(held) != code and held.is_floating_point:
+        raise ValueError(f"the cache is a tensor of {held}, and would be read as "
+                         f"{next(t for t, c in _dtypes().items() if c == code)}")
     return code
 
 
@@ -784,8 +790,9 @@ def kv_rope_append(layout: KvLayout, layer, batch: KvBatch, q, k, v, d_freqs, *,
                                 2 * d_freqs.numel(),
                                 (KV_ROPE_INTERLEAVED if interleaved else 0) | (KV_ROPE_INVERSE if inverse else 0),
                                 magnitude, None if positions is None else _dptr(positions, torch.int32, "positions"),
-                                _cache_code(cache_dtype, layout, code), _scale_ptr(k_scale, layout, "k_scale"),
-                                _scale_ptr(v_scale, layout, "v_scale"), _stream(stream)), "kv_rope_append")
+                                _cache_code(cache_dtype, layout, code, None if k is None else layer),
+                                _scale_ptr(k_scale, layout, "k_scale"), _scale_ptr(v_scale, layout, "v_scale"),
+                                _stream(stream)), "kv_rope_append")
 
 
 def kv_paged_attention_workspace(layout: KvLayout, batch: KvBatch, q_heads: int, window: int = 0) -> int:
@@ -807,7 +814,7 @@ def kv_paged_attention(layout: KvLayout, layer, batch: KvBatch, q, out, scale: f
     if lse is not None and lse.numel() != n * heads:
         raise ValueError("lse must be [rows, heads]")
     _check(lib().kv_paged_attention(ct.addressof(layout), _dptr(layer, None, "layer"), ct.addressof(batch), rq, ro,
-                                    scale, 1 if causal else 0, window, _cache_code(cache_dtype, layout, code),
+                                    scale, 1 if causal else 0, window, _cache_code(cache_dtype, layout, code, layer),
                                     _scale_ptr(k_scale, layout, "k_scale"), _scale_ptr(v_scale, layout, "v_scale"),
                                     None if lse is None else _dptr(lse, _torch().float32, "lse"), ws, size,
                                     _stream(stream)), "kv_paged_attention")
@@ -827,8 +834,9 @@ def kv_attention_weights(layout: KvLayout, layer, batch: KvBatch, q, lse, weight
         raise ValueError("weights must be [requests, kv_heads, n]")
     _check(lib().kv_attention_weights(ct.addressof(layout), _dptr(layer, None, "layer"), ct.addressof(batch),
                                       rq, _dptr(lse, torch.float32, "lse"), scale, 1 if causal else 0, window,
-                                      _cache_code(cache_dtype, layout, code), _scale_ptr(k_scale, layout, "k_scale"),
-                                      decay, _dptr(weights, torch.float32, "weights"), shape[2], _stream(stream)),
+                                      _cache_code(cache_dtype, layout, code, layer),
+                                      _scale_ptr(k_scale, layout, "k_scale"), decay,
+                                      _dptr(weights, torch.float32, "weights"), shape[2], _stream(stream)),
            "kv_attention_weights")
 
 
