@@ -59,18 +59,19 @@ class ServedCache:
         new = np.asarray(new, np.int64)
         if new.shape != self.lengths.shape or (new < 0).any() or (self.lengths + new > self.capacity).any():
             raise ValueError("new must hold one count per request, and leave every request within its block table")
-        self.lengths += new
+        # (the counts change last: a step that is refused leaves them as they were)
+        lengths = self.lengths + new
         off = np.concatenate([[0], np.cumsum(new)])
         pos = np.concatenate([np.arange(p, p + n) for p, n in zip(self.positions, new)]).astype(np.int32)
-        self.positions += new
         up = lambda x: torch.from_numpy(x).to(self.dev)
-        self._positions = up(pos)
-        self.batch = make_batch(up(off), up(self.lengths.astype(np.int32)), self.block_tables, int(off[-1]),
-                                int(new.max(initial=0)), int(self.lengths.max(initial=0)))
-        size = kv_paged_attention_workspace(self.layout, self.batch, self.q_heads, self.window)
+        batch = make_batch(up(off), up(lengths.astype(np.int32)), self.block_tables, int(off[-1]),
+                           int(new.max(initial=0)), int(lengths.max(initial=0)))
+        size = kv_paged_attention_workspace(self.layout, batch, self.q_heads, self.window)
         if size and (self._workspace is None or self._workspace.numel() < size):
             self._workspace = torch.empty(size, dtype=torch.uint8, device=self.dev)
-        self._lse = torch.empty((self.batch.num_q, self.q_heads), device=self.dev)
+        lse, positions = torch.empty((batch.num_q, self.q_heads), device=self.dev), up(pos)
+        self.batch, self._lse, self._positions = batch, lse, positions
+        self.lengths, self.positions = lengths, self.positions + new
 
     def attend(self, layer: int, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor) -> None:
         """One layer of the step: q [rows, q_heads, head_dim] is rotated in place, k and v go into the cache, and
