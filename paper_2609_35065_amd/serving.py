@@ -12,7 +12,8 @@ the operators' over cache indices: an eviction therefore has to leave the
 tokens that a window still reaches.
 
 This module only sequences the calls and owns their buffers; it computes
-nothing itself and never waits for the GPU.
+nothing itself and never waits for the GPU: what a step uploads lies in pinned
+memory, so that the host may be steps ahead.
 """
 from __future__ import annotations
 
@@ -54,6 +55,16 @@ class ServedCache:
                                        device=self.dev)
         self.batch, self._workspace, self._lse = None, None, None
 
+    def _upload(self, *arrays: np.ndarray) -> List[torch.Tensor]:
+        """Copies on the device, by one upload from pinned memory that the allocator keeps until it is done.  64-bit
+        arrays come first, so that all are aligned."""
+        ends = np.cumsum([0] + [x.nbytes for x in arrays])
+        host = torch.empty(int(ends[-1]), dtype=torch.uint8, pin_memory=self.dev.type == "cuda")
+        for x, a, b in zip(arrays, ends, ends[1:]):
+            host.numpy()[a:b] = x.view(np.uint8)
+        there = host.to(self.dev, non_blocking=True)
+        return [there[a:b].view(torch.from_numpy(x).dtype) for x, a, b in zip(arrays, ends, ends[1:])]
+
     def begin(self, new) -> None:
         """Start a step: ``new`` tokens of each request (0, 1 or many)."""
         new = np.asarray(new, np.int64)
@@ -63,14 +74,14 @@ class ServedCache:
         lengths = self.lengths + new
         off = np.concatenate([[0], np.cumsum(new)])
         pos = np.concatenate([np.arange(p, p + n) for p, n in zip(self.positions, new)]).astype(np.int32)
-        up = lambda x: torch.from_numpy(x).to(self.dev)
-        batch = make_batch(up(off), up(lengths.astype(np.int32)), self.block_tables, int(off[-1]),
-                           int(new.max(initial=0)), int(lengths.max(initial=0)))
+        d_off, d_len, d_pos = self._upload(off, lengths.astype(np.int32), pos)
+        batch = make_batch(d_off, d_len, self.block_tables, int(off[-1]), int(new.max(initial=0)),
+                           int(lengths.max(initial=0)))
         size = kv_paged_attention_workspace(self.layout, batch, self.q_heads, self.window)
         if size and (self._workspace is None or self._workspace.numel() < size):
             self._workspace = torch.empty(size, dtype=torch.uint8, device=self.dev)
-        lse, positions = torch.empty((batch.num_q, self.q_heads), device=self.dev), up(pos)
-        self.batch, self._lse, self._positions = batch, lse, positions
+        lse = torch.empty((batch.num_q, self.q_heads), device=self.dev)
+        self.batch, self._lse, self._positions = batch, lse, d_pos
         self.lengths, self.positions = lengths, self.positions + new
 
     def attend(self, layer: int, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor) -> None:
@@ -102,7 +113,7 @@ class ServedCache:
         L, R, h, _ = self.weights.shape
         keep = torch.empty((L, R, h, budget), dtype=torch.int32, device=self.dev)
         left = torch.empty(R, dtype=torch.int32, device=self.dev)
-        size = torch.from_numpy(self.lengths.astype(np.int32)).to(self.dev)
+        size, = self._upload(self.lengths.astype(np.int32))
         kv_evict_select(self.weights, size, budget, sink, recent, keep, left)
         kv_evict_compact(self.layout, self.layers, self.block_tables, keep, left, weights=self.weights)
         # what lies behind the kept tokens belongs to none: new tokens start from 0

@@ -1,4 +1,5 @@
-"""ServedCache between its calls: a step that is refused leaves it as it was."""
+"""ServedCache between its calls: a step that is refused leaves it as it was, and the
+host does not wait for the GPU."""
 import pytest
 import torch
 
@@ -21,3 +22,32 @@ def test_a_refused_step_changes_nothing():
         with pytest.raises(kv.KvError):
             s.begin([1, 2])
         assert s.lengths.tolist() == [40, 7] and s.positions.tolist() == [40, 7] and s.batch is None
+
+
+def _busy(x, n):
+    """Work of the GPU's that lasts some hundred milliseconds: n products of 8,192 a side in 32 bits."""
+    for _ in range(n):
+        torch.mm(x, x, out=x)
+
+
+def test_the_host_does_not_wait_for_the_gpu():
+    c, s = _served([40, 7], room=200)
+    x = torch.zeros(8192, 8192, device="cuda")
+    q, k, v = (ref.rows_of(2, h, 64, torch.bfloat16, c.gen).cuda() for h in (4, 2, 2))
+    out = torch.empty_like(q)
+
+    def steps():
+        for _ in range(3):
+            s.begin([1, 1])
+            s.attend(0, q, k, v, out)
+        return s.evict(40, sink=2, recent=4)
+
+    _busy(x, 1)
+    steps()
+    torch.cuda.synchronize()
+    _busy(x, 20)
+    done = torch.cuda.Event()
+    done.record()
+    assert steps() == [3, 1]
+    assert not done.query(), "the host waited"
+    torch.cuda.synchronize()
