@@ -32,7 +32,10 @@ class ServedCache:
     ``layers`` and ``block_tables`` (int32 [requests, n]) are the paged tensors and tables of the copies;
     ``freqs`` (float64, on the device) and ``magnitude`` come from kv_rope_frequencies.  ``decay`` is the factor on
     weights accumulated in earlier steps (None: weights are not kept, and nothing can be evicted); ``k_scale`` and
-    ``v_scale`` are float32 [layers, kv_heads] for an 8-bit cache."""
+    ``v_scale`` are float32 [layers, kv_heads] for an 8-bit cache.
+
+    The layers of a step share buffers, so that calls follow one another on the GPU: one that comes on another stream
+    than the last waits for that one's work.  (Not in a graph capture: its replays are the program's to order.)"""
 
     def __init__(self, layout: KvLayout, layers: Sequence[torch.Tensor], block_tables: torch.Tensor, lengths,
                  q_heads: int, freqs: torch.Tensor, *, magnitude: float = 1.0, interleaved: bool = False,
@@ -53,7 +56,20 @@ class ServedCache:
         if decay is not None:
             self.weights = torch.zeros((layout.num_layers, len(self.lengths), layout.kv_heads, self.capacity),
                                        device=self.dev)
-        self.batch, self._workspace, self._lse = None, None, None
+        self.batch, self._workspace, self._lse, self._positions = None, None, None, None
+        self._stream = torch.cuda.current_stream(self.dev) if self.dev.type == "cuda" else None
+
+    def _follow(self) -> None:
+        """Put the current stream behind the one of the last call, and keep the buffers for it."""
+        now = torch.cuda.current_stream(self.dev)
+        if now == self._stream or torch.cuda.is_current_stream_capturing():
+            return
+        now.wait_stream(self._stream)
+        self._stream = now
+        held = [self.weights, self._workspace, self._lse, self._positions]
+        for t in held + list(self.batch.tensors if self.batch else ()):
+            if t is not None:
+                t.record_stream(now)
 
     def _upload(self, *arrays: np.ndarray) -> List[torch.Tensor]:
         """Copies on the device, by one upload from pinned memory that the allocator keeps until it is done.  64-bit
@@ -70,6 +86,7 @@ class ServedCache:
         new = np.asarray(new, np.int64)
         if new.shape != self.lengths.shape or (new < 0).any() or (self.lengths + new > self.capacity).any():
             raise ValueError("new must hold one count per request, and leave every request within its block table")
+        self._follow()
         # (the counts change last: a step that is refused leaves them as they were)
         lengths = self.lengths + new
         off = np.concatenate([[0], np.cumsum(new)])
@@ -87,6 +104,7 @@ class ServedCache:
     def attend(self, layer: int, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor) -> None:
         """One layer of the step: q [rows, q_heads, head_dim] is rotated in place, k and v go into the cache, and
         ``out`` gets the attention of q over the cache."""
+        self._follow()
         ks = None if self.k_scale is None else self.k_scale[layer]
         vs = None if self.v_scale is None else self.v_scale[layer]
         pool = self.layers[layer]
@@ -110,6 +128,7 @@ class ServedCache:
         if 0 < self.window < 1 << 30 and recent < self.window - 1 and (self.lengths > budget).any():
             raise ValueError(f"an eviction has to leave the last {self.window - 1} tokens, which the window reaches, "
                              f"not {recent}")
+        self._follow()
         L, R, h, _ = self.weights.shape
         keep = torch.empty((L, R, h, budget), dtype=torch.int32, device=self.dev)
         left = torch.empty(R, dtype=torch.int32, device=self.dev)

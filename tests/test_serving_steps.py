@@ -1,5 +1,5 @@
-"""ServedCache between its calls: a step that is refused leaves it as it was, and the
-host does not wait for the GPU."""
+"""ServedCache between its calls: a step that is refused leaves it as it was, the host
+does not wait for the GPU, and calls on several streams keep their order."""
 import pytest
 import torch
 
@@ -51,3 +51,55 @@ def test_the_host_does_not_wait_for_the_gpu():
     assert steps() == [3, 1]
     assert not done.query(), "the host waited"
     torch.cuda.synchronize()
+
+
+def test_layers_on_several_streams_keep_their_order():
+    """Each layer's call comes on another stream, behind work that takes long on the first: the same results as on
+    one stream."""
+    got = []
+    for streams in (1, 2):
+        c, s = _served([500, 70], layers=2, seed=5)
+        side = [torch.cuda.Stream() for _ in range(streams)]
+        x = torch.zeros(8192, 8192, device="cuda")
+        rows = [[ref.rows_of(3, h, 64, torch.bfloat16, c.gen).cuda() for h in (4, 2, 2)] for _ in range(4)]
+        outs = [torch.empty_like(q) for q, _, _ in rows]
+        torch.cuda.synchronize()
+        for step in range(2):
+            with torch.cuda.stream(side[0]):
+                _busy(x, 4)
+                s.begin([1, 2])
+                s.attend(0, *rows[2 * step], outs[2 * step])
+            with torch.cuda.stream(side[-1]):
+                s.attend(1, *rows[2 * step + 1], outs[2 * step + 1])
+        with torch.cuda.stream(side[0]):
+            s.evict(64, sink=1, recent=8)
+        torch.cuda.synchronize()
+        got.append([t.cpu() for t in (*outs, s.weights, *c.d_pool)])
+    for a, b in zip(*got):
+        assert torch.equal(a, b)
+
+
+def test_a_captured_layer():
+    """A step's layer as a graph: captured on a stream of the graph's own, replayed against the eager call."""
+    c, s = _served([500, 70], seed=6)
+    q, k, v = (ref.rows_of(2, h, 64, torch.bfloat16, c.gen).cuda() for h in (4, 2, 2))
+    out, graph = torch.empty_like(q), torch.cuda.CUDAGraph()
+    s.begin([1, 1])
+    before = [s.weights.clone(), c.d_pool[0].clone(), q.clone()]
+
+    def restore():
+        for t, was in zip((s.weights, c.d_pool[0], q), before):
+            t.copy_(was)
+
+    s.attend(0, q, k, v, out)
+    want = [t.clone() for t in (out, s.weights, c.d_pool[0], q)]
+    restore()
+    with torch.cuda.graph(graph):
+        s.attend(0, q, k, v, out)
+    for _ in range(3):
+        restore()
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip((out, s.weights, c.d_pool[0], q), want):
+            assert torch.equal(a, b)
