@@ -104,6 +104,8 @@ class ServedCache:
     def attend(self, layer: int, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor) -> None:
         """One layer of the step: q [rows, q_heads, head_dim] is rotated in place, k and v go into the cache, and
         ``out`` gets the attention of q over the cache."""
+        if self.batch is None:
+            raise ValueError("no step: begin one first, and after an eviction")
         self._follow()
         ks = None if self.k_scale is None else self.k_scale[layer]
         vs = None if self.v_scale is None else self.v_scale[layer]
@@ -138,5 +140,5 @@ class ServedCache:
         # what lies behind the kept tokens belongs to none: new tokens start from 0
         gone = torch.arange(self.capacity, device=self.dev) >= left[:, None]
         self.weights.masked_fill_(gone[None, :, None], 0.0)
-        self.lengths = np.minimum(self.lengths, budget)
+        self.lengths, self.batch = np.minimum(self.lengths, budget), None       # the step's lengths are gone
         return [int(-(-n // self.layout.block_size)) for n in self.lengths]

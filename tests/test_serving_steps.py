@@ -103,3 +103,18 @@ def test_a_captured_layer():
         torch.cuda.synchronize()
         for a, b in zip((out, s.weights, c.d_pool[0], q), want):
             assert torch.equal(a, b)
+
+
+def test_a_step_has_to_begin_after_an_eviction():
+    c, s = _served([40, 7])
+    q, k, v = (ref.rows_of(2, h, 64, torch.bfloat16, c.gen).cuda() for h in (4, 2, 2))
+    with pytest.raises(ValueError, match="begin"):
+        s.attend(0, q, k, v, torch.empty_like(q))
+    s.begin([1, 1])
+    s.attend(0, q, k, v, torch.empty_like(q))
+    s.evict(16, sink=2, recent=4)
+    with pytest.raises(ValueError, match="begin"):
+        s.attend(0, q, k, v, torch.empty_like(q))
+    s.begin([1, 1])
+    s.attend(0, q, k, v, torch.empty_like(q))
+    torch.cuda.synchronize()
