@@ -97,6 +97,12 @@ __device__ __forceinline__ int part_of(int n, int i, int parts) {
     return uniform(parts == 1 ? n * i : (int)((uint64_t)n * i / parts));
 }
 
+// LDS that the lanes of a wave exchange without a barrier: its accesses are in order, and this keeps them so in the code.
+__device__ __forceinline__ void wave_fence() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
+    __builtin_amdgcn_wave_barrier();
+}
+
 // Bytes of LDS that a body needs.
 template <int DP, int W> constexpr int kSplitLds = W * 32 * (DP * 2 + 32);
 
@@ -205,6 +211,7 @@ __device__ __forceinline__ void few_rows(const AttentionParams &p, const Tile &t
         // A value that is not finite must reach only the rows that see its key: 0 times it is NaN.  In a step that some
         // row does not see whole, such values are staged as 0, and added below to the results that do see them.
         const bool mixed = is_mixed(there, t0);
+        wave_fence();                          // the step before is read
 #pragma unroll
         for (int i = 0; i < VL; ++i) {
             const int x = i * 64 + lane, r = x / VPR, vec = x % VPR;
@@ -221,6 +228,7 @@ __device__ __forceinline__ void few_rows(const AttentionParams &p, const Tile &t
                 *(u32x4 *)(mine + r * kRow + vec * VEC * 2 + j * 16) = y[j];
             }
         }
+        wave_fence();
         f32x4 s[2];
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
@@ -274,6 +282,7 @@ __device__ __forceinline__ void few_rows(const AttentionParams &p, const Tile &t
     l += __shfl_xor(l, 32);
 
     // join the waves' parts
+    wave_fence();
     float *po = (float *)mine;                 // [16][DP + 4]
 #pragma unroll
     for (int i = 0; i < DT; ++i) *(f32x4 *)(po + col * (DP + 4) + i * 16 + quad * 4) = o[i];
