@@ -409,14 +409,15 @@ typedef struct kv_rows {
  * d_block_tables[r*bt_stride + t / B].  A block id outside [0, num_blocks) is
  * a missing block, and indices past the table are missing too: nothing is
  * written there, and attention does not see them.  n_r may be 0, 1 or
- * thousands in one batch.  max_q_len and max_kv_len are the largest n_r and
+ * thousands in one batch.  Rows before d_q_off[0] belong to no request: they
+ * are not appended (and rotated at d_positions, or else at -1).  max_q_len and max_kv_len are the largest n_r and
  * d_kv_len[r] as far as the host knows: they choose launch shapes, results do
  * not depend on them.  The struct lives in host memory and is read during the
  * call. */
 typedef struct kv_batch {
     int32_t num_reqs;
     int32_t bt_stride;
-    int64_t num_q;                   /* rows in all: d_q_off[num_reqs] */
+    int64_t num_q;                   /* rows of the tensors: d_q_off[num_reqs] */
     int32_t max_q_len, max_kv_len;
     const int64_t *d_q_off;          /* [num_reqs+1], non-decreasing */
     const int32_t *d_kv_len;         /* [num_reqs] */

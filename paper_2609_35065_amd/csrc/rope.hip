@@ -129,7 +129,7 @@ __global__ __launch_bounds__(kThreads) void rope_append_kernel(RopeParams p) {
             if (c < 64) break;
         }
         if (lane == 0) {
-            const bool known = r < p.cache.num_reqs;
+            const bool known = r < p.cache.num_reqs && p.cache.q_off[r] <= t0 + i;     // (of no request: the rows before the first)
             const int32_t index = known ? p.cache.kv_len[r] - (int32_t)(p.cache.q_off[r + 1] - (t0 + i)) : -1;
             uint32_t row = 0;
             const int32_t id = index >= 0 ? block_of(p.cache, r, (uint32_t)index, row) : -1;
