@@ -410,10 +410,11 @@ typedef struct kv_rows {
  * a missing block, and indices past the table are missing too: nothing is
  * written there, and attention does not see them.  n_r may be 0, 1 or
  * thousands in one batch.  Rows before d_q_off[0] belong to no request: they
- * are not appended (and rotated at d_positions, or else at -1).  max_q_len and max_kv_len are the largest n_r and
- * d_kv_len[r] as far as the host knows: they choose launch shapes, results do
- * not depend on them.  The struct lives in host memory and is read during the
- * call. */
+ * are not appended (and rotated at d_positions, or else at -1), and their
+ * results of attention are left alone.  max_q_len and max_kv_len are the
+ * largest n_r and d_kv_len[r] as far as the host knows: they choose launch
+ * shapes, results do not depend on them.  The struct lives in host memory and
+ * is read during the call. */
 typedef struct kv_batch {
     int32_t num_reqs;
     int32_t bt_stride;

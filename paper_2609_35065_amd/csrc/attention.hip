@@ -701,6 +701,8 @@ __global__ __launch_bounds__(kThreads) void attention_join_kernel(AttentionParam
     const int lane = threadIdx.x & 63, half = lane >> 5, d = (lane & 31) * 8;
     const int64_t all = p.cache.num_q * p.q_heads, row = (int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6);
     if (row >= all) return;
+    const int64_t q = (uint32_t)row / (uint32_t)p.q_heads;
+    const bool ours = q >= p.cache.q_off[0] && q < p.cache.q_off[p.cache.num_reqs];   // no part holds rows of no request
     f32x2 ml = {-INFINITY, 0.0f};
     if (lane < p.splits) ml = *(const f32x2 *)(p.part_ml + (lane * all + row) * 2);
     const float *at = p.part_o + row * p.head_dim + d;
@@ -749,7 +751,7 @@ __global__ __launch_bounds__(kThreads) void attention_join_kernel(AttentionParam
         a[e] = u[0] + u[1];
         b[e] = v[0] + v[1];
     }
-    const int64_t q = (uint32_t)row / (uint32_t)p.q_heads;
+    if (!ours) return;
     const int head = (int)(row - q * p.q_heads);
     const bool empty = l == 0.0f;
     const float inv = empty ? 0.0f : (p.v_scale ? p.v_scale[(int)divide(head, p.by_group)] : 1.0f) / l;
