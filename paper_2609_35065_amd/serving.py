@@ -55,7 +55,7 @@ class ServedCache:
         self.weights = None
         if decay is not None:
             self.weights = torch.zeros((layout.num_layers, len(self.lengths), layout.kv_heads, self.capacity),
-                                       device=self.dev)
+                                       dtype=torch.float32, device=self.dev)
         self.batch, self._workspace, self._lse, self._positions = None, None, None, None
         self._stream = torch.cuda.current_stream(self.dev) if self.dev.type == "cuda" else None
 
@@ -97,7 +97,7 @@ class ServedCache:
         size = kv_paged_attention_workspace(self.layout, batch, self.q_heads, self.window)
         if size and (self._workspace is None or self._workspace.numel() < size):
             self._workspace = torch.empty(size, dtype=torch.uint8, device=self.dev)
-        lse = torch.empty((batch.num_q, self.q_heads), device=self.dev)
+        lse = torch.empty((batch.num_q, self.q_heads), dtype=torch.float32, device=self.dev)
         self.batch, self._lse, self._positions = batch, lse, d_pos
         self.lengths, self.positions = lengths, self.positions + new
 

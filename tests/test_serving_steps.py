@@ -118,3 +118,20 @@ def test_a_step_has_to_begin_after_an_eviction():
     s.begin([1, 1])
     s.attend(0, q, k, v, torch.empty_like(q))
     torch.cuda.synchronize()
+
+
+def test_another_default_type():
+    """A program may have torch make bfloat16 tensors by default: sums stay in 32 bits."""
+    c = ref.Cache([104, 71], heads=2, dim=64).device()
+    freqs = torch.from_numpy(FREQS).cuda()
+    q, k, v = (ref.rows_of(2, h, 64, torch.bfloat16, c.gen).cuda() for h in (4, 2, 2))
+    torch.set_default_dtype(torch.bfloat16)
+    try:
+        s = ServedCache(c.layout, c.d_pool, c.d_bt, [40, 7], 4, freqs)
+        s.begin([1, 1])
+        s.attend(0, q, k, v, torch.empty_like(q))
+        assert s.weights.dtype == torch.float32
+        s.evict(16, recent=4)
+    finally:
+        torch.set_default_dtype(torch.float32)
+    torch.cuda.synchronize()
