@@ -117,8 +117,10 @@ template <int DP, int W> constexpr int kSplitLds = W * 32 * (DP * 2 + 32);
 // in the loop and each keeps the next step's K and V on their way.
 // Bound by the reads of the cache: 64 requests of 4,096 tokens, 8 KV heads of
 // 128, 1.07 GB in 207 us (5.2 TB/s); 8 of 32,768 in 8 bits, 0.54 GB in 128 us
-// (4.2 TB/s).  P is rounded to the type of the products, relative to the
-// running maximum; sums, statistics and results stay in 32 bits.
+// (4.2 TB/s).  P is rounded to the type of the products, as the matrix units
+// take it: relative to the running maximum, after its sum.  That adds 12 to 19 %
+// to the error of results that are rounded to bf16 alone (0.0017 to 0.0020 of
+// their size; chunks 0.0023).  Sums and statistics stay in 32 bits.
 template <class T, bool F8, int DP, int W>
 __device__ __forceinline__ void few_rows(const AttentionParams &p, const Tile &tile, int h, int split, char *lds,
                                          float (*part)[16][2], int *odd) {
@@ -362,8 +364,10 @@ __device__ __forceinline__ void few_rows(const AttentionParams &p, const Tile &t
 // one row's scores for half of the keys, so that a row's maximum and sum need
 // one exchange between lanes.  Steps are bound by the issue of exponentials,
 // LDS reads and products beside one another: 8 chunks of 2,048 tokens over
-// 4,096, 32 heads on 8 of 128, 825 GFLOP in 853 us (967 TFLOP/s); head size 80
-// with a window of 1,024, ragged, 62 us (343 TFLOP/s of what the rows see).
+// 4,096, 32 heads on 8 of 128, 825 GFLOP in 848 to 897 us (920 to 973 TFLOP/s,
+// by card), the matrix units busy for 43 % of the time, the vector units for 45 %;
+// head size 80 with a window of 1,024, ragged, 61 to 65 us (330 to 350 TFLOP/s of
+// what the rows see).
 //
 // The running maximum may lag: o and l are only scaled when some row's
 // maximum has grown by more than 2^kLag since it was last taken.  Until then
@@ -695,7 +699,7 @@ __global__ __launch_bounds__(64 * W, DP > 128 ? 1 : 2) void attention_many_kerne
 
 // Join the parts of each row: one wave a row, each half of it every other
 // part, eight elements a lane; the parts' sums and values are loaded together.
-// Bound by latency: 4.4 us for the parts of few rows.
+// Bound by latency: 3.5 to 5.5 us for the parts of few rows.
 template <class T>
 __global__ __launch_bounds__(kThreads) void attention_join_kernel(AttentionParams p) {
     const int lane = threadIdx.x & 63, half = lane >> 5, d = (lane & 31) * 8;

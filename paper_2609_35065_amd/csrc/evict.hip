@@ -61,8 +61,11 @@ template <int WAVES> __device__ __forceinline__ int prefix(int x, int *scratch) 
 
 // One workgroup a row.  ITEMS > 0: the row has at most ITEMS * THREADS
 // tokens and is read once, into registers; 0: any length, read again from the
-// caches in each pass.  Bound by the counts in LDS: 32 layers x 8 heads of 1,001
-// tokens 10 us, 8 ragged requests around 4,096 tokens (2,048 rows) 70 us.
+// caches in each pass.  Reading is an eighth of it: 8 ragged requests around 4,096
+// tokens (2,048 rows, 46 MB) take 62 us, 32 layers x 8 heads of 1,001 tokens 9.4
+// us.  Vector instructions are busy for 48 % of that, LDS for 26 % (a third of it
+// conflicts between lanes that count one bin); the rest are the waits between the
+// passes, which depend on one another.
 template <int THREADS, int ITEMS>
 __global__ __launch_bounds__(THREADS, THREADS == 256 ? 4 : 6) void evict_select_kernel(SelectParams p) {
     constexpr int kWaves = THREADS / 64, kBatch = 8;          // loads on their way together
@@ -199,10 +202,11 @@ constexpr int kMoves = 2048;               // rows whose places are looked up at
 constexpr int kAhead = 4;                  // vectors of a lane in a tile
 
 // One workgroup: a (layer, request, head, plane, slice).  A row already in its
-// place is neither read nor written.  Bound by memory: both calls move or read
-// 0.13 GB in 20 us (1,001 tokens, 32 layers, half kept) and 2.2 GB, counted as if
-// every kept row moved, in 268 us (8 ragged requests around 4,096, a quarter
-// kept; 8.3 TB/s).
+// place is neither read nor written.  Bound by memory, and by the two barriers
+// of a tile, at which its workgroup has only the next tile's reads on their way:
+// 8 ragged requests around 4,096 tokens, 32 layers, a quarter kept, 2.16 GB read
+// and written in 458 us (4.7 TB/s) where nearly all kept rows move; 1,001 tokens,
+// half kept, 0.13 GB in 30 us (4.4 TB/s).
 __global__ __launch_bounds__(kThreads) void evict_compact_kernel(CompactParams p) {
     __shared__ uint32_t from[kMoves], to[kMoves];      // 16-byte units from the plane's start; from = to: no move
     const int tid = threadIdx.x;

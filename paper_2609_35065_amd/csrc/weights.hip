@@ -44,10 +44,12 @@ struct __align__(16) RowInfo {
 template <int DP> constexpr int kQueryRow = DP * 2 + 16;     // bytes of an LDS row: 8 rows on different banks
 
 // The four waves take KW groups of 64 keys and 4 / KW groups of 32 rows at a
-// time; the rows go through LDS, one step ahead, for all of them.  Bound by the
-// products and as many exponentials as scores: chunks of 1,000 tokens over
-// 4,000 in 4 requests, 32 heads on 8 of 128, 115 GFLOP in 169 us (679
-// TFLOP/s).
+// time; the rows go through LDS, one step ahead, for all of them.  Chunks of
+// 1,000 tokens over 4,000 in 4 requests, 32 heads on 8 of 128, 115 GFLOP in 168 to
+// 176 us (650 to 680 TFLOP/s).  A wave's products and exponentials take turns,
+// with two waves on each SIMD to overlap them: the matrix units are busy for 27 %
+// of the time, the vector units for 44 %.  And all 512 workgroups run at once,
+// those of the last quarter of the keys with half the rows.
 template <class T, bool F8, int DP, int KW>
 __global__ __launch_bounds__(kThreads, DP > 128 ? 1 : 2) void attention_weights_kernel(WeightParams p) {
     constexpr int KS = DP / 16, RW = kWaves / KW, RT = KW > 1 ? 2 : 1, kRows = 32 * RW * RT, VPR = DP / 8, VL = kRows * VPR / kThreads;
