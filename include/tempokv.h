@@ -473,6 +473,57 @@ int kv_rope_append(const kv_layout *layout, void *d_layer, const kv_batch *batch
                    int32_t flags, float magnitude, const int32_t *d_positions, int32_t cache_dtype,
                    const float *d_k_scale, const float *d_v_scale, void *stream);
 
+/* Largest number of axes of a position. */
+enum { KV_MAX_AXES = 8 };
+
+/* Which axis the pairs of a row take (kv_rope_axes). */
+typedef enum kv_axes_order {
+    KV_AXES_SECTIONS = 0,   /* the first sections[0] pairs axis 0, the next sections[1] axis 1, ... */
+    KV_AXES_IN_TURN = 1     /* the axes in turn, pair by pair; one whose pairs are all placed is left out from there on */
+} kv_axes_order;
+
+/* The axis of each pair, in host memory, for kv_rope_append_axes: axis a gets
+ * h_sections[a] pairs (0 or more), sum(h_sections) = rot_dim/2 in all, in the
+ * given kv_axes_order.  Errors: KV_EINVAL, KV_ELIMIT (more than 128 pairs). */
+int kv_rope_axes(int32_t num_axes, const int32_t *h_sections, int32_t order, uint8_t *h_axis);
+
+/* kv_rope_append for positions with several axes (time, height and width of
+ * an image's or a video's patch; text has the same position on all): pair i of
+ * row t is turned by
+ *     u = d_positions[h_axis[i] * position_stride + t] * d_freqs[i]
+ * and all else is as there.  d_positions int32, at least num_q apart from one
+ * axis to the next; 1 to KV_MAX_AXES axes; h_axis uint8 [rot_dim/2] in host
+ * memory, read during the call.  K and V go to the row's cache index, whatever
+ * its positions.  Errors: those of kv_rope_append, KV_EINVAL for an axis that
+ * is none of num_axes. */
+int kv_rope_append_axes(const kv_layout *layout, void *d_layer, const kv_batch *batch, const kv_rows *q,
+                        const kv_rows *q_out, const kv_rows *k, const kv_rows *v, const double *d_freqs,
+                        int32_t rot_dim, int32_t flags, float magnitude, const int32_t *d_positions,
+                        int64_t position_stride, int32_t num_axes, const uint8_t *h_axis, int32_t cache_dtype,
+                        const float *d_k_scale, const float *d_v_scale, void *stream);
+
+/* Turn keys that lie in the cache to other positions, in place: for every
+ * layer l, request r, head h and cache index j < min(d_len[r], shift_stride),
+ * pair (a, b) of index i < rot_dim/2 of the key becomes
+ *     (a cos u - b sin u, a sin u + b cos u),
+ *     u = d_shift[l][r][h][j] * d_freqs[i]   (l, h: 0 where layers, heads are 1),
+ * so that a key rotated for position p is one rotated for p + shift (of any
+ * number of axes that all move by the same).  Keys whose shift is 0, and those
+ * in a missing block, stay as they are, bit by bit; others are rounded to the
+ * cache's type once more (KV_F8E4M3 as in kv_rope_append; scales do not matter
+ * to a rotation).  V is not touched.
+ *   d_shift   int32 [layers][num_reqs][heads][shift_stride]; layers is 1 or
+ *             num_layers, heads 1 or kv_heads
+ *   max_len   the largest d_len[r] as far as the host knows (launch shape only)
+ *   flags     how pairs are formed and turned, as in kv_rope_append
+ * Requests must not share blocks whose keys turn.  One launch.  Errors:
+ * KV_EINVAL, KV_EALIGN, KV_ELIMIT (as kv_rope_append, and 2^31 workgroups or
+ * more), KV_EHIP. */
+int kv_rope_shift(const kv_layout *layout, void *const *h_layer_ptrs, const int32_t *d_block_tables,
+                  int32_t bt_stride, int32_t num_reqs, const int32_t *d_len, int32_t max_len, int32_t layers,
+                  int32_t heads, const int32_t *d_shift, int64_t shift_stride, const double *d_freqs,
+                  int32_t rot_dim, int32_t flags, int32_t cache_dtype, void *stream);
+
 /* Bytes of device scratch that kv_paged_attention needs for a batch (0 when
  * it splits no request's keys): depends on the shapes and the host's hints
  * alone, so a program can keep one buffer of the largest.  Errors: KV_EINVAL,
@@ -502,6 +553,19 @@ int kv_paged_attention(const kv_layout *layout, const void *d_layer, const kv_ba
                        const float *d_k_scale, const float *d_v_scale, float *d_lse, void *d_workspace,
                        int64_t workspace_bytes, void *stream);
 
+/* kv_paged_attention with a sliding window and sinks: the first `sink` tokens
+ * of each request, which stay visible however far the window has moved.  Row i
+ * at cache index p_i sees key j when j < d_kv_len[r], j's block is not missing,
+ * j <= p_i if `causal`, and j > p_i - window or j < sink (window 0: every key).
+ * Keys that no row sees cost nothing.  sink >= 0; all else, and the errors, as
+ * there; the workspace is that of kv_sink_attention_workspace. */
+int kv_sink_attention_workspace(const kv_layout *layout, const kv_batch *batch, int32_t q_heads, int32_t window,
+                                int32_t sink, int64_t *bytes);
+int kv_sink_attention(const kv_layout *layout, const void *d_layer, const kv_batch *batch, const kv_rows *q,
+                      const kv_rows *out, float scale, int32_t causal, int32_t window, int32_t sink,
+                      int32_t cache_dtype, const float *d_k_scale, const float *d_v_scale, float *d_lse,
+                      void *d_workspace, int64_t workspace_bytes, void *stream);
+
 /* Attention weight that each cached token received from the batch's new
  * tokens, accumulated over calls: for request r, KV head h and cache index
  * j < d_kv_len[r],
@@ -516,6 +580,18 @@ int kv_paged_attention(const kv_layout *layout, const void *d_layer, const kv_ba
 int kv_attention_weights(const kv_layout *layout, const void *d_layer, const kv_batch *batch, const kv_rows *q,
                          const float *d_lse, float scale, int32_t causal, int32_t window, int32_t cache_dtype,
                          const float *d_k_scale, float decay, float *d_weights, int64_t weight_stride, void *stream);
+
+/* kv_attention_weights by the rule of kv_sink_attention.  At most two
+ * launches, deterministic; d_workspace as there, of
+ * kv_sink_weights_workspace's size.  Errors: those of kv_attention_weights,
+ * KV_EINVAL without a workspace where one is needed, KV_ELIMIT for one that
+ * is too small. */
+int kv_sink_weights_workspace(const kv_layout *layout, const kv_batch *batch, int32_t q_heads, int32_t window,
+                              int32_t sink, int64_t *bytes);
+int kv_sink_weights(const kv_layout *layout, const void *d_layer, const kv_batch *batch, const kv_rows *q,
+                    const float *d_lse, float scale, int32_t causal, int32_t window, int32_t sink,
+                    int32_t cache_dtype, const float *d_k_scale, float decay, float *d_weights,
+                    int64_t weight_stride, void *d_workspace, int64_t workspace_bytes, void *stream);
 
 /* Which cached tokens to keep, for every layer, request and head of
  * accumulated weights float32 [num_layers][num_reqs][heads][weight_stride]

@@ -32,6 +32,8 @@ SIM_TRACE_KINDS = ["arrive", "admit", "commit", "ordinary", "ready", "stageready
 KV_BF16, KV_F16, KV_F8E4M3 = range(3)
 KV_ROPE_PLAIN, KV_ROPE_LINEAR, KV_ROPE_BASE, KV_ROPE_RAMP = range(4)
 KV_ROPE_HALF, KV_ROPE_INTERLEAVED, KV_ROPE_INVERSE = 0, 1, 2
+KV_AXES_SECTIONS, KV_AXES_IN_TURN = range(2)
+KV_MAX_AXES = 8
 KV_MAX_LAYERS = 128
 HASH_BLOCK_TOKENS = 16
 
@@ -45,12 +47,15 @@ EXPORTS = ["kv_hash_prefix", "kv_index_create", "kv_index_destroy", "kv_index_in
            "kv_pipeline_create", "kv_pipeline_destroy", "kv_retrieve_pipelined", "kv_decide_claims",
            "kv_build_jobs_routed", "kv_ttr_static", "kv_ttr_state_aware", "kv_chunk_keys", "kv_validate_jobs_device",
            "kv_probe_mixed_traffic", "kv_rope_frequencies", "kv_rope_append", "kv_paged_attention_workspace",
-           "kv_paged_attention", "kv_attention_weights", "kv_evict_select", "kv_evict_compact"]
+           "kv_paged_attention", "kv_attention_weights", "kv_evict_select", "kv_evict_compact",
+           "kv_rope_axes", "kv_rope_append_axes", "kv_rope_shift", "kv_sink_attention_workspace", "kv_sink_attention",
+           "kv_sink_weights_workspace", "kv_sink_weights"]
 # the calls that run on the host only (host.cpp, controller.cpp)
 HOST_CALLS = ["kv_build_jobs", "kv_build_jobs_routed", "kv_decide_claims", "kv_group_jobs_by_slot",
               "kv_validate_jobs", "kv_commit_should_stage", "kv_commit_should_stage_n", "kv_retrieve_plan",
               "kv_strerror", "kv_version", "kv_sim_run", "kv_ttr_static", "kv_ttr_state_aware", "kv_chunk_keys",
-              "kv_rope_frequencies", "kv_paged_attention_workspace"]
+              "kv_rope_frequencies", "kv_paged_attention_workspace", "kv_rope_axes", "kv_sink_attention_workspace",
+              "kv_sink_weights_workspace"]
 
 
 class KvError(RuntimeError):
@@ -148,6 +153,14 @@ SIGNATURES = {
     "kv_attention_weights": [_vp, _vp, _vp, _vp, _vp, _flt, _i32, _i32, _i32, _vp, _flt, _vp, _i64, _vp],
     "kv_evict_select": [_vp, _i64, _vp, _i32, _i32, _i32, _i32, _i32, _i32, _vp, _vp, _vp],
     "kv_evict_compact": [_vp, _vp, _vp, _i32, _i32, _i32, _vp, _i32, _vp, _vp, _i64, _vp],
+    "kv_rope_axes": [_i32, _vp, _i32, _vp],
+    "kv_rope_append_axes": [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i32, _i32, _flt, _vp, _i64, _i32, _vp, _i32, _vp, _vp,
+                            _vp],
+    "kv_rope_shift": [_vp, _vp, _vp, _i32, _i32, _vp, _i32, _i32, _i32, _vp, _i64, _vp, _i32, _i32, _i32, _vp],
+    "kv_sink_attention_workspace": [ct.POINTER(KvLayout), ct.POINTER(KvBatch), _i32, _i32, _i32, ct.POINTER(_i64)],
+    "kv_sink_attention": [_vp, _vp, _vp, _vp, _vp, _flt, _i32, _i32, _i32, _i32, _vp, _vp, _vp, _vp, _i64, _vp],
+    "kv_sink_weights_workspace": [ct.POINTER(KvLayout), ct.POINTER(KvBatch), _i32, _i32, _i32, ct.POINTER(_i64)],
+    "kv_sink_weights": [_vp, _vp, _vp, _vp, _vp, _flt, _i32, _i32, _i32, _i32, _vp, _flt, _vp, _i64, _vp, _i64, _vp],
 }
 
 
@@ -769,7 +782,22 @@ def kv_rope_append(layout: KvLayout, layer, batch: KvBatch, q, k, v, d_freqs, *,
     """Rotate q into q_out (default: in place) and append rotated k, and v, to the cache.  q, or both k and v, may be
     None; layer may be None without k and v."""
     torch = _torch()
-    n, d = batch.num_q, layout.head_dim
+    n = batch.num_q
+    rq, ro, rk, rv, code = _append_rows(n, layout.head_dim, q, q_out, k, v)
+    if positions is not None and not isinstance(positions, int) and positions.numel() != n:
+        raise ValueError("positions must hold one position per row")
+    _check(lib().kv_rope_append(ct.addressof(layout), None if layer is None else _dptr(layer, None, "layer"),
+                                ct.addressof(batch), rq, ro, rk, rv, _dptr(d_freqs, torch.float64, "freqs"),
+                                2 * d_freqs.numel(),
+                                (KV_ROPE_INTERLEAVED if interleaved else 0) | (KV_ROPE_INVERSE if inverse else 0),
+                                magnitude, None if positions is None else _dptr(positions, torch.int32, "positions"),
+                                _cache_code(cache_dtype, layout, code, None if k is None else layer),
+                                _scale_ptr(k_scale, layout, "k_scale"), _scale_ptr(v_scale, layout, "v_scale"),
+                                _stream(stream)), "kv_rope_append")
+
+
+def _append_rows(n: int, d: int, q, q_out, k, v):
+    """(kv_rows of q, q_out, k and v, kv_dtype) of an append."""
     rq = ro = rk = rv = None
     code = -1
     if q is not None:
@@ -783,16 +811,73 @@ def kv_rope_append(layout: KvLayout, layer, batch: KvBatch, q, k, v, d_freqs, *,
         raise ValueError("k and v go together")
     if code < 0:
         raise ValueError("nothing to do: q and k are both None")
-    if positions is not None and not isinstance(positions, int) and positions.numel() != n:
-        raise ValueError("positions must hold one position per row")
-    _check(lib().kv_rope_append(ct.addressof(layout), None if layer is None else _dptr(layer, None, "layer"),
-                                ct.addressof(batch), rq, ro, rk, rv, _dptr(d_freqs, torch.float64, "freqs"),
-                                2 * d_freqs.numel(),
-                                (KV_ROPE_INTERLEAVED if interleaved else 0) | (KV_ROPE_INVERSE if inverse else 0),
-                                magnitude, None if positions is None else _dptr(positions, torch.int32, "positions"),
-                                _cache_code(cache_dtype, layout, code, None if k is None else layer),
-                                _scale_ptr(k_scale, layout, "k_scale"), _scale_ptr(v_scale, layout, "v_scale"),
-                                _stream(stream)), "kv_rope_append")
+    return rq, ro, rk, rv, code
+
+
+def kv_rope_axes(sections: Sequence[int], interleaved: bool = False) -> np.ndarray:
+    """The axis of each pair (uint8) for kv_rope_append_axes: ``sections[a]`` pairs of axis a, one axis's after
+    another's, or (interleaved) the axes in turn as long as they have pairs left."""
+    s = np.ascontiguousarray(sections, np.int32)
+    out = np.zeros(min(max(int(s.clip(min=0).sum(dtype=np.int64)), 0), 128), np.uint8)
+    _check(host_lib().kv_rope_axes(s.size, _hdata(s), KV_AXES_IN_TURN if interleaved else KV_AXES_SECTIONS,
+                                   out.ctypes.data), "kv_rope_axes")
+    return out
+
+
+def kv_rope_append_axes(layout: KvLayout, layer, batch: KvBatch, q, k, v, d_freqs, axes: np.ndarray, positions, *,
+                        q_out=None, interleaved: bool = False, inverse: bool = False, magnitude: float = 1.0,
+                        k_scale=None, v_scale=None, cache_dtype=None, stream=None) -> None:
+    """kv_rope_append at positions with several axes: int32 [axes, rows] on the device, and the axis of each pair
+    (kv_rope_axes)."""
+    torch = _torch()
+    n, half = batch.num_q, d_freqs.numel()
+    rq, ro, rk, rv, code = _append_rows(n, layout.head_dim, q, q_out, k, v)
+    if axes.dtype != np.uint8 or axes.shape != (half,) or not axes.flags.c_contiguous:
+        raise ValueError("axes must hold the axis of each pair, uint8")
+    shape = positions.shape
+    if len(shape) != 2 or shape[1] != n:
+        raise ValueError("positions must be [axes, rows]")
+    if not positions.is_cuda or positions.dtype != torch.int32:
+        raise ValueError("positions must be an int32 device tensor")
+    apart, dense = positions.stride()
+    if (dense != 1 and n > 1) or (apart < n and shape[0] > 1):
+        raise ValueError("positions must hold each axis's rows next to one another")
+    _check(lib().kv_rope_append_axes(ct.addressof(layout), None if layer is None else _dptr(layer, None, "layer"),
+                                     ct.addressof(batch), rq, ro, rk, rv, _dptr(d_freqs, torch.float64, "freqs"),
+                                     2 * half,
+                                     (KV_ROPE_INTERLEAVED if interleaved else 0) | (KV_ROPE_INVERSE if inverse else 0),
+                                     magnitude, positions.data_ptr(), max(apart, n), shape[0], _hdata(axes),
+                                     _cache_code(cache_dtype, layout, code, None if k is None else layer),
+                                     _scale_ptr(k_scale, layout, "k_scale"), _scale_ptr(v_scale, layout, "v_scale"),
+                                     _stream(stream)), "kv_rope_append_axes")
+
+
+def kv_rope_shift(layout: KvLayout, layers: Sequence, d_block_tables, d_len, max_len: int, d_shift, d_freqs, *,
+                  interleaved: bool = False, inverse: bool = False, cache_dtype=None, stream=None) -> None:
+    """Turn the cached keys by d_shift positions (int32 [layers or 1, requests, heads or 1, n]), in place, in every
+    layer; ``max_len`` is the largest of d_len (int32 [requests]) as far as the host knows."""
+    torch = _torch()
+    R = d_len.numel()
+    if len(layers) != layout.num_layers:
+        raise ValueError("one paged tensor per layer is required")
+    if d_block_tables.dim() != 2 or d_block_tables.shape[0] != R:
+        raise ValueError("block_tables must hold one row per request")
+    if d_shift.dim() != 4 or d_shift.shape[1] != R:
+        raise ValueError("shift must be [layers or 1, requests, heads or 1, n]")
+    if cache_dtype is None and layout.elem_bytes == 2:
+        cache_dtype = next((t.dtype for t in layers if not isinstance(t, int) and t.is_floating_point()), None)
+        if cache_dtype is None:
+            raise ValueError("cache_dtype is needed for a cache of bytes")
+    for t in layers:
+        code = _cache_code(cache_dtype, layout, KV_BF16, t)
+    lp = _layer_array(layers)   # alive during the call
+    _check(lib().kv_rope_shift(ct.addressof(layout), lp.buffer_info()[0],
+                               _dptr(d_block_tables, torch.int32, "block_tables"), max(1, d_block_tables.shape[1]), R,
+                               _dptr(d_len, torch.int32, "len"), max_len, d_shift.shape[0], d_shift.shape[2],
+                               _dptr(d_shift, torch.int32, "shift"), d_shift.shape[3],
+                               _dptr(d_freqs, torch.float64, "freqs"), 2 * d_freqs.numel(),
+                               (KV_ROPE_INTERLEAVED if interleaved else 0) | (KV_ROPE_INVERSE if inverse else 0), code,
+                               _stream(stream)), "kv_rope_shift")
 
 
 def kv_paged_attention_workspace(layout: KvLayout, batch: KvBatch, q_heads: int, window: int = 0) -> int:
@@ -818,6 +903,60 @@ def kv_paged_attention(layout: KvLayout, layer, batch: KvBatch, q, out, scale: f
                                     _scale_ptr(k_scale, layout, "k_scale"), _scale_ptr(v_scale, layout, "v_scale"),
                                     None if lse is None else _dptr(lse, _torch().float32, "lse"), ws, size,
                                     _stream(stream)), "kv_paged_attention")
+
+
+def kv_sink_attention_workspace(layout: KvLayout, batch: KvBatch, q_heads: int, window: int, sink: int) -> int:
+    """Bytes of device scratch that kv_sink_attention needs for this batch."""
+    n = _i64(0)
+    _check(host_lib().kv_sink_attention_workspace(ct.byref(layout), ct.byref(batch), q_heads, window, sink, ct.byref(n)),
+           "kv_sink_attention_workspace")
+    return n.value
+
+
+def kv_sink_attention(layout: KvLayout, layer, batch: KvBatch, q, out, scale: float, window: int, sink: int, *,
+                      causal: bool = True, lse=None, k_scale=None, v_scale=None, cache_dtype=None, workspace=None,
+                      stream=None) -> None:
+    """kv_paged_attention where each row sees the last ``window`` tokens and the first ``sink`` of its request."""
+    n, d = batch.num_q, layout.head_dim
+    rq, heads, code = _rows(q, n, d, "q")
+    ro = _rows(out, n, d, "out")[0]
+    ws, size = (None, 0) if workspace is None else (_dptr(workspace, None, "workspace"), workspace.nbytes)
+    if lse is not None and lse.numel() != n * heads:
+        raise ValueError("lse must be [rows, heads]")
+    _check(lib().kv_sink_attention(ct.addressof(layout), _dptr(layer, None, "layer"), ct.addressof(batch), rq, ro,
+                                   scale, 1 if causal else 0, window, sink,
+                                   _cache_code(cache_dtype, layout, code, layer),
+                                   _scale_ptr(k_scale, layout, "k_scale"), _scale_ptr(v_scale, layout, "v_scale"),
+                                   None if lse is None else _dptr(lse, _torch().float32, "lse"), ws, size,
+                                   _stream(stream)), "kv_sink_attention")
+
+
+def kv_sink_weights_workspace(layout: KvLayout, batch: KvBatch, q_heads: int, window: int, sink: int) -> int:
+    """Bytes of device scratch that kv_sink_weights needs for this batch."""
+    n = _i64(0)
+    _check(host_lib().kv_sink_weights_workspace(ct.byref(layout), ct.byref(batch), q_heads, window, sink, ct.byref(n)),
+           "kv_sink_weights_workspace")
+    return n.value
+
+
+def kv_sink_weights(layout: KvLayout, layer, batch: KvBatch, q, lse, weights, scale: float, window: int, sink: int, *,
+                    causal: bool = True, decay: float = 1.0, k_scale=None, cache_dtype=None, workspace=None,
+                    stream=None) -> None:
+    """kv_attention_weights where each row sees the last ``window`` tokens and the first ``sink`` of its request."""
+    torch = _torch()
+    rq, heads, code = _rows(q, batch.num_q, layout.head_dim, "q")
+    if lse.numel() != batch.num_q * heads:
+        raise ValueError("lse must be [rows, heads]")
+    shape = weights.shape
+    if len(shape) != 3 or shape[0] != batch.num_reqs or shape[1] != layout.kv_heads:
+        raise ValueError("weights must be [requests, kv_heads, n]")
+    ws, size = (None, 0) if workspace is None else (_dptr(workspace, None, "workspace"), workspace.nbytes)
+    _check(lib().kv_sink_weights(ct.addressof(layout), _dptr(layer, None, "layer"), ct.addressof(batch), rq,
+                                 _dptr(lse, torch.float32, "lse"), scale, 1 if causal else 0, window, sink,
+                                 _cache_code(cache_dtype, layout, code, layer),
+                                 _scale_ptr(k_scale, layout, "k_scale"), decay,
+                                 _dptr(weights, torch.float32, "weights"), shape[2], ws, size, _stream(stream)),
+           "kv_sink_weights")
 
 
 def kv_attention_weights(layout: KvLayout, layer, batch: KvBatch, q, lse, weights, scale: float, *,

@@ -35,7 +35,7 @@ struct AttentionParams {
     float scale;                       // times log2 e
     Divider by_group;
     int32_t q_heads, kv_heads, group, head_dim;
-    int32_t splits, window;
+    int32_t splits, window, sink;
     bool causal;
 };
 
@@ -103,6 +103,19 @@ __device__ __forceinline__ void wave_fence() {
     __builtin_amdgcn_wave_barrier();
 }
 
+// The keys that the rows of a tile see with a window and sinks: the request's first `sink` and, from the first key of
+// the first row's window on, all up to the last row's last.  A body passes them as one run of places, so that the keys
+// between cost no steps and neither range is rounded to whole steps: key t is place t below `sink` and place t - gap
+// behind the gap, which is empty where the window begins among the sinks.
+struct Run {
+    int sink, gap;
+};
+
+__device__ __forceinline__ Run find_run(int sink, int first) { return {sink, max(0, first - sink)}; }
+// The key at a place, and of a row's bound (its first key in the window, or one past its last) the place.
+__device__ __forceinline__ int key_at(const Run &x, int place) { return place + (place < x.sink ? 0 : x.gap); }
+__device__ __forceinline__ int place_of(const Run &x, int key) { return max(key - x.gap, min(key, x.sink)); }
+
 // Bytes of LDS that a body needs.
 template <int DP, int W> constexpr int kSplitLds = W * 32 * (DP * 2 + 32);
 
@@ -121,7 +134,7 @@ template <int DP, int W> constexpr int kSplitLds = W * 32 * (DP * 2 + 32);
 // take it: relative to the running maximum, after its sum.  That adds 12 to 19 %
 // to the error of results that are rounded to bf16 alone (0.0017 to 0.0020 of
 // their size; chunks 0.0023).  Sums and statistics stay in 32 bits.
-template <class T, bool F8, int DP, int W>
+template <class T, bool F8, int DP, int W, bool SINK>
 __device__ __forceinline__ void few_rows(const AttentionParams &p, const Tile &tile, int h, int split, char *lds,
                                          float (*part)[16][2], int *odd) {
     constexpr int KS = DP / 32, LD = F8 ? KS / 2 : KS, DT = DP / 16;
@@ -144,11 +157,18 @@ __device__ __forceinline__ void few_rows(const AttentionParams &p, const Tile &t
     const int64_t pos_last = ahead + divide(min(tile.row0 + 15, tile.rows - 1), p.by_group);
     // keys this lane's row sees: lo <= j < hi; and those that some or all rows of the tile see
     const int64_t hi64 = p.causal ? min(len, pos + 1) : len, lo64 = p.window > 0 ? max((int64_t)0, pos - p.window + 1) : 0;
-    const int hi = have ? (int)max((int64_t)0, hi64) : 0, lo = (int)lo64;
-    const int end = (int)max((int64_t)0, p.causal ? min(len, pos_last + 1) : len);
-    const int begin = (int)(p.window > 0 ? max((int64_t)0, pos_first - p.window + 1) : 0) & ~(kWide - 1);
-    const int all_hi = (int)max((int64_t)0, p.causal ? min(len, pos_first + 1) : len);
-    const int all_lo = (int)(p.window > 0 ? max((int64_t)0, pos_last - p.window + 1) : 0);
+    int hi = have ? (int)max((int64_t)0, hi64) : 0, lo = (int)lo64;
+    int end = (int)max((int64_t)0, p.causal ? min(len, pos_last + 1) : len);
+    int begin = (int)(p.window > 0 ? max((int64_t)0, pos_first - p.window + 1) : 0);
+    int all_hi = (int)max((int64_t)0, p.causal ? min(len, pos_first + 1) : len);
+    int all_lo = (int)(p.window > 0 ? max((int64_t)0, pos_last - p.window + 1) : 0);
+    Run run = {0, 0};
+    if constexpr (SINK) {                      // from here on all of these, and t, are places
+        run = find_run(p.sink, begin);
+        hi = place_of(run, hi), lo -= run.gap, end = place_of(run, end);
+        all_hi = place_of(run, all_hi), all_lo -= run.gap, begin = 0;
+    }
+    begin &= ~(kWide - 1);
     const int steps = end > begin ? (end - begin + kWide - 1) / kWide : 0;
     const int step0 = part_of(steps, split, p.splits), step1 = part_of(steps, split + 1, p.splits);
 
@@ -156,7 +176,9 @@ __device__ __forceinline__ void few_rows(const AttentionParams &p, const Tile &t
     const char *kbase = p.cache.layer + (int64_t)h * p.cache.head_bytes;
     const char *vbase = kbase + p.cache.kv_stride;
     char *mine = lds + wave * 32 * kRow;
-    const auto is_mixed = [&](uint32_t there, int t0) { return there != 0xffffffffu || t0 < all_lo || t0 + 32 > all_hi; };
+    const auto is_mixed = [&](uint32_t there, int t0) {
+        return there != 0xffffffffu || (t0 < all_lo && !(SINK && t0 + 32 <= run.sink)) || t0 + 32 > all_hi;
+    };
     if (threadIdx.x == 0) *odd = 0;
     __syncthreads();
 
@@ -167,7 +189,7 @@ __device__ __forceinline__ void few_rows(const AttentionParams &p, const Tile &t
     u32x4 kreg[2 * NS][LD], vreg[VL * NS];
     const auto look_up = [&](int step) {
         const int t = begin + step * kWide + (lane & (kWide - 1));
-        id = step < step1 && t < end ? block_of(p.cache, tile.req, (uint32_t)t, id_row) : -1;
+        id = step < step1 && t < end ? block_of(p.cache, tile.req, (uint32_t)(SINK ? key_at(run, t) : t), id_row) : -1;
     };
     const auto offset = [&]() { return id < 0 ? 0u : (uint32_t)id * p.cache.block16 + id_row * p.cache.row16; };
     const auto load = [&]() {
@@ -251,7 +273,7 @@ __device__ __forceinline__ void few_rows(const AttentionParams &p, const Tile &t
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int k = x * 16 + quad * 4 + i;
-                const bool see = !mixed || (((there >> k) & 1) && t0 + k >= lo && t0 + k < hi);
+                const bool see = !mixed || (((there >> k) & 1) && (t0 + k >= lo || (SINK && t0 + k < run.sink)) && t0 + k < hi);
                 s[x][i] = see ? s[x][i] * c : -INFINITY;
                 top = fmaxf(top, s[x][i]);
             }
@@ -341,7 +363,9 @@ __device__ __forceinline__ void few_rows(const AttentionParams &p, const Tile &t
             for (int x = threadIdx.x; x < 16 * p.head_dim; x += (64 * W)) {
                 const int r = x / p.head_dim, d = x - r * p.head_dim, row = tile.row0 + r, tok = (int)divide(row, p.by_group);
                 const int64_t at = ahead + tok;
-                if (row >= tile.rows || (p.causal && t0 + k > at) || (p.window > 0 && t0 + k <= at - p.window)) continue;
+                const int t = SINK ? key_at(run, t0 + k) : t0 + k;
+                if (row >= tile.rows || (p.causal && t > at)) continue;
+                if (p.window > 0 && t <= at - p.window && !(SINK && t < p.sink)) continue;
                 const float y = load_one<T, F8>(v, d);
                 if (fabsf(y) < INFINITY) continue;
                 const int64_t q = tile.first + tok;
@@ -387,7 +411,7 @@ struct Places {
     uint64_t there;
 };
 
-template <class T, bool F8, int DP, int W>
+template <class T, bool F8, int DP, int W, bool SINK>
 __device__ __forceinline__ void many_rows(const AttentionParams &p, const Tile &tile, int h, int split, char *lds,
                                           int *odd, Places *places) {
     constexpr int KS = DP / 16, DT = DP / 32, kThreads = 64 * W, kRows = 32 * W;
@@ -406,11 +430,19 @@ __device__ __forceinline__ void many_rows(const AttentionParams &p, const Tile &
     const auto hi_of = [&](int tok) { return max(0, p.causal ? min(len, ahead + tok + 1) : len); };
     const auto lo_of = [&](int tok) { return p.window > 0 ? max(0, ahead + tok - p.window + 1) : 0; };
     const auto token_of = [&](int row) { return uniform((int)divide(min(row, last_row), p.by_group)); };
-    const int hi = have ? hi_of(token) : 0, lo = lo_of(token);
+    int hi = have ? hi_of(token) : 0, lo = lo_of(token);
     const int wfirst = token_of(wrow), wlast = token_of(wrow + 31), first = token_of(tile.row0), last = token_of(tile.row0 + kRows - 1);
-    const int all_hi = uniform(hi_of(wfirst)), all_lo = uniform(lo_of(wlast));
-    const int tile_hi = uniform(hi_of(first)), tile_lo = uniform(lo_of(last));
-    const int end = uniform(hi_of(last)), begin = uniform(lo_of(first) & ~(kStep - 1));
+    int all_hi = uniform(hi_of(wfirst)), all_lo = uniform(lo_of(wlast));
+    int tile_hi = uniform(hi_of(first)), tile_lo = uniform(lo_of(last));
+    int end = uniform(hi_of(last)), begin = uniform(lo_of(first));
+    Run run = {0, 0};
+    if constexpr (SINK) {                      // from here on all of these, and t, are places
+        run = find_run(p.sink, begin);
+        hi = place_of(run, hi), lo -= run.gap, end = place_of(run, end);
+        all_hi = place_of(run, all_hi), all_lo -= run.gap;
+        tile_hi = place_of(run, tile_hi), tile_lo -= run.gap, begin = 0;
+    }
+    begin &= ~(kStep - 1);
     const int steps = end > begin ? (end - begin + kStep - 1) / kStep : 0;
     const int step0 = part_of(steps, split, p.splits), step1 = part_of(steps, split + 1, p.splits);
 
@@ -426,7 +458,9 @@ __device__ __forceinline__ void many_rows(const AttentionParams &p, const Tile &
     const char *vbase = kbase + p.cache.kv_stride;
 
     uint64_t there = 0, there_next = 0;        // bit k: key k of the step is in the cache
-    const auto is_mixed = [&](uint64_t there, int t0) { return there != ~uint64_t(0) || t0 < tile_lo || t0 + kStep > tile_hi; };
+    const auto is_mixed = [&](uint64_t there, int t0) {
+        return there != ~uint64_t(0) || (t0 < tile_lo && !(SINK && t0 + kStep <= run.sink)) || t0 + kStep > tile_hi;
+    };
     if (tid == 0) *odd = 0;
 
     // Staging.  One wave, in turn, looks up the keys of a step, a lane each, and leaves their places for all: the
@@ -437,8 +471,8 @@ __device__ __forceinline__ void many_rows(const AttentionParams &p, const Tile &
     int32_t id = -1;
     uint32_t id_row = 0;
     const auto ask = [&](int step) {
-        const uint32_t t = begin + step * kStep + lane, blk = divide(t, p.cache.by_block);
-        id_row = t - blk * p.cache.block_size;
+        const uint32_t t = begin + step * kStep + lane, key = SINK ? key_at(run, t) : t, blk = divide(key, p.cache.by_block);
+        id_row = key - blk * p.cache.block_size;
         id = -1;
         if (step < step1 && t < (uint32_t)end) id = table[blk];        // t < end <= the table's span
     };
@@ -551,11 +585,16 @@ __device__ __forceinline__ void many_rows(const AttentionParams &p, const Tile &
         };
         read_v(0);
         __builtin_amdgcn_sched_barrier(0);
-        if (there != ~uint64_t(0) || t0 < all_lo || t0 + kStep > all_hi) {
+        if (there != ~uint64_t(0) || (t0 < all_lo && !(SINK && t0 + kStep <= run.sink)) || t0 + kStep > all_hi) {
             // bit k: this lane's row sees key 4 half + k, for the k below (x = 32, 8 and 1 times the indices)
             const int from = min(max(lo - t0, 0), kStep), to = min(max(hi - t0, 0), kStep);
             uint64_t see = there;
-            see = from < kStep ? see & (~uint64_t(0) << from) : 0;
+            uint64_t seen = from < kStep ? ~uint64_t(0) << from : 0;
+            if constexpr (SINK) {
+                const int sinks = max(run.sink - t0, 0);
+                seen |= sinks < kStep ? (uint64_t(1) << sinks) - 1 : ~uint64_t(0);
+            }
+            see &= seen;
             see = to < kStep ? see & ((uint64_t(1) << to) - 1) : see;
             see >>= 4 * half;
 #pragma unroll
@@ -658,7 +697,7 @@ __device__ __forceinline__ void many_rows(const AttentionParams &p, const Tile &
         if (!is_mixed(in, t0)) continue;
         for (int k = 0; k < kStep; ++k) {
             const char *v = vbase + ((int64_t)(uint32_t)__shfl((int)off, k) << 4);
-            if (!((in >> k) & 1) || !have || t0 + k < lo || t0 + k >= hi) continue;
+            if (!((in >> k) & 1) || !have || (t0 + k < lo && !(SINK && t0 + k < run.sink)) || t0 + k >= hi) continue;
             for (int d = half; d < p.head_dim; d += 2) {
                 const float x = load_one<T, F8>(v, d);
                 if (fabsf(x) < INFINITY) continue;
@@ -670,7 +709,7 @@ __device__ __forceinline__ void many_rows(const AttentionParams &p, const Tile &
 }
 
 // Every request in tiles of 16 rows.
-template <class T, bool F8, int DP>
+template <class T, bool F8, int DP, bool SINK>
 __global__ __launch_bounds__(kThreads) void attention_few_kernel(AttentionParams p) {
     __shared__ __align__(16) char lds[kSplitLds<DP, kWaves>];
     __shared__ float part[kWaves][16][2];
@@ -678,12 +717,12 @@ __global__ __launch_bounds__(kThreads) void attention_few_kernel(AttentionParams
     const unsigned id = blockIdx.x;
     const int h = (int)(id % p.kv_heads), split = (int)(id / p.kv_heads % p.splits);
     const Tile tile = find_tile<kSplitRows>(p.cache, (int)(id / p.kv_heads / p.splits), p.group);
-    if (tile.row0 < tile.rows) few_rows<T, F8, DP, kWaves>(p, tile, h, split, lds, part, &odd);
+    if (tile.row0 < tile.rows) few_rows<T, F8, DP, kWaves, SINK>(p, tile, h, split, lds, part, &odd);
 }
 
 // Large tiles, from the last to the first (a request's last rows see most
 // keys); a request with no more than 16 rows in all takes the other body.
-template <class T, bool F8, int DP, int W>
+template <class T, bool F8, int DP, int W, bool SINK>
 __global__ __launch_bounds__(64 * W, DP > 128 ? 1 : 2) void attention_many_kernel(AttentionParams p) {
     __shared__ __align__(16) char lds[kTileLds<DP> > kSplitLds<DP, W> ? kTileLds<DP> : kSplitLds<DP, W>];
     __shared__ float part[W][16][2];
@@ -693,8 +732,8 @@ __global__ __launch_bounds__(64 * W, DP > 128 ? 1 : 2) void attention_many_kerne
     const int h = (int)(id % p.kv_heads), split = (int)(id / p.kv_heads % p.splits);
     const Tile tile = find_tile<32 * W>(p.cache, (int)p.tiles - 1 - (int)(id / p.kv_heads / p.splits), p.group);
     if (tile.row0 >= tile.rows) return;
-    if (tile.rows <= kSplitRows) few_rows<T, F8, DP, W>(p, tile, h, split, lds, part, &odd);
-    else many_rows<T, F8, DP, W>(p, tile, h, split, lds, &odd, places);
+    if (tile.rows <= kSplitRows) few_rows<T, F8, DP, W, SINK>(p, tile, h, split, lds, part, &odd);
+    else many_rows<T, F8, DP, W, SINK>(p, tile, h, split, lds, &odd, places);
 }
 
 // Join the parts of each row: one wave a row, each half of it every other
@@ -768,21 +807,83 @@ __global__ __launch_bounds__(kThreads) void attention_join_kernel(AttentionParam
     if (lane == 0 && p.lse) p.lse[row] = empty ? -INFINITY : (top + log2_(l)) * kLn2;
 }
 
-template <class T, bool F8, int DP> void (*attention_kernel_for(int rows))(AttentionParams) {
-    if (rows == kSplitRows) return attention_few_kernel<T, F8, DP>;
+template <class T, bool F8, bool SINK, int DP> void (*attention_kernel_for(int rows))(AttentionParams) {
+    if (rows == kSplitRows) return attention_few_kernel<T, F8, DP, SINK>;
     if constexpr (DP <= 128) {
-        if (rows == kLargeRows) return attention_many_kernel<T, F8, DP, kLargeRows / 32>;
+        if (rows == kLargeRows) return attention_many_kernel<T, F8, DP, kLargeRows / 32, SINK>;
     }
-    return attention_many_kernel<T, F8, DP, kTileRows / 32>;
+    return attention_many_kernel<T, F8, DP, kTileRows / 32, SINK>;
 }
 
-template <class T, bool F8> auto attention_kernel(int rows, int head_dim) {
-    if (head_dim <= 64) return attention_kernel_for<T, F8, 64>(rows);
+template <class T, bool F8, bool SINK> auto attention_kernel(int rows, int head_dim) {
+    if (head_dim <= 64) return attention_kernel_for<T, F8, SINK, 64>(rows);
     if constexpr (!F8) {
-        if (head_dim <= 96) return attention_kernel_for<T, F8, 96>(rows);
+        if (head_dim <= 96) return attention_kernel_for<T, F8, SINK, 96>(rows);
     }
-    if (head_dim <= 128) return attention_kernel_for<T, F8, 128>(rows);
-    return attention_kernel_for<T, F8, 256>(rows);
+    if (head_dim <= 128) return attention_kernel_for<T, F8, SINK, 128>(rows);
+    return attention_kernel_for<T, F8, SINK, 256>(rows);
+}
+
+template <bool SINK> auto attention_kernel(bool bf16, bool f8, int rows, int d) {
+    return bf16 ? (f8 ? attention_kernel<Bf16, true, SINK>(rows, d) : attention_kernel<Bf16, false, SINK>(rows, d))
+                : (f8 ? attention_kernel<F16, true, SINK>(rows, d) : attention_kernel<F16, false, SINK>(rows, d));
+}
+
+int attention(const kv_layout *layout, const void *d_layer, const kv_batch *batch, const kv_rows *q, const kv_rows *out,
+              float scale, int32_t causal, int32_t window, int32_t sink, int32_t cache_dtype, const float *d_k_scale,
+              const float *d_v_scale, float *d_lse, void *d_workspace, int64_t workspace_bytes, void *stream) {
+    int rc = check_cache(layout, cache_dtype);
+    if (rc == KV_OK) rc = check_batch(batch);
+    if (rc == KV_OK) rc = check_rows(q, batch->num_q, layout->head_dim, false);
+    if (rc == KV_OK) rc = check_rows(out, batch->num_q, layout->head_dim, true);
+    if (rc != KV_OK) return rc;
+    if (!d_layer || out->dtype != q->dtype || out->heads != q->heads) return KV_EINVAL;
+    if (cache_dtype != KV_F8E4M3 && cache_dtype != q->dtype) return KV_EINVAL;
+    if (!(scale > 0.0f) || !isfinite(scale)) return KV_EINVAL;
+    if (((uintptr_t)d_layer & 15u) || ((uintptr_t)d_lse & 3u) || ((uintptr_t)d_workspace & 15u)) return KV_EALIGN;
+    AttentionPlan plan;
+    rc = plan_attention(layout, batch, q->heads, window, sink, &plan);
+    if (rc != KV_OK) return rc;
+    if (plan.workspace > 0 && !d_workspace) return KV_EINVAL;
+    if (plan.workspace > workspace_bytes) return KV_ELIMIT;
+    if (batch->num_q == 0) return KV_OK;
+    const int64_t all = batch->num_q * q->heads;
+    AttentionParams p;
+    p.cache = make_paged(layout, d_layer, batch);
+    p.q = (const char *)q->d_data;
+    p.out = (char *)const_cast<void *>(out->d_data);
+    p.q_ts = q->token_stride * 2, p.q_hs = q->head_stride * 2;
+    p.o_ts = out->token_stride * 2, p.o_hs = out->head_stride * 2;
+    p.lse = d_lse;
+    p.part_o = (float *)d_workspace;
+    p.part_ml = p.part_o ? p.part_o + (int64_t)plan.splits * all * layout->head_dim : nullptr;
+    p.k_scale = cache_dtype == KV_F8E4M3 ? d_k_scale : nullptr;
+    p.v_scale = cache_dtype == KV_F8E4M3 ? d_v_scale : nullptr;
+    p.tiles = plan.tiles;
+    p.scale = scale * kLog2e;
+    p.q_heads = q->heads;
+    p.kv_heads = layout->kv_heads;
+    p.group = q->heads / layout->kv_heads;
+    p.by_group = make_divider((uint32_t)p.group);
+    p.head_dim = layout->head_dim;
+    p.splits = plan.splits;
+    p.window = window < kMaxLength ? window : 0;
+    p.sink = sink < kMaxLength ? sink : kMaxLength;
+    p.causal = causal != 0;
+    const bool bf16 = q->dtype == KV_BF16, f8 = cache_dtype == KV_F8E4M3;
+    const int d = layout->head_dim;
+    // (without a window every key is in it)
+    auto kernel = p.sink > 0 && p.window > 0 ? attention_kernel<true>(bf16, f8, plan.rows, d)
+                                             : attention_kernel<false>(bf16, f8, plan.rows, d);
+    const int threads = plan.rows == kSplitRows ? kThreads : 2 * plan.rows;
+    hipStream_t s = (hipStream_t)stream;
+    (void)hipGetLastError();
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(plan.tiles * p.kv_heads * p.splits)), dim3(threads), 0, s, p);
+    if (p.splits > 1) {
+        auto join = bf16 ? attention_join_kernel<Bf16> : attention_join_kernel<F16>;
+        hipLaunchKernelGGL(join, dim3((unsigned)((all + kWaves - 1) / kWaves)), dim3(kThreads), 0, s, p);
+    }
+    return hipGetLastError() == hipSuccess ? KV_OK : KV_EHIP;
 }
 
 }  // namespace
@@ -794,56 +895,16 @@ int kv_paged_attention(const kv_layout *layout, const void *d_layer, const kv_ba
                        const kv_rows *out, float scale, int32_t causal, int32_t window, int32_t cache_dtype,
                        const float *d_k_scale, const float *d_v_scale, float *d_lse, void *d_workspace,
                        int64_t workspace_bytes, void *stream) {
-    int rc = tkv::check_cache(layout, cache_dtype);
-    if (rc == KV_OK) rc = tkv::check_batch(batch);
-    if (rc == KV_OK) rc = tkv::check_rows(q, batch->num_q, layout->head_dim, false);
-    if (rc == KV_OK) rc = tkv::check_rows(out, batch->num_q, layout->head_dim, true);
-    if (rc != KV_OK) return rc;
-    if (!d_layer || out->dtype != q->dtype || out->heads != q->heads) return KV_EINVAL;
-    if (cache_dtype != KV_F8E4M3 && cache_dtype != q->dtype) return KV_EINVAL;
-    if (!(scale > 0.0f) || !isfinite(scale)) return KV_EINVAL;
-    if (((uintptr_t)d_layer & 15u) || ((uintptr_t)d_lse & 3u) || ((uintptr_t)d_workspace & 15u)) return KV_EALIGN;
-    tkv::AttentionPlan plan;
-    rc = tkv::plan_attention(layout, batch, q->heads, window, &plan);
-    if (rc != KV_OK) return rc;
-    if (plan.workspace > 0 && !d_workspace) return KV_EINVAL;
-    if (plan.workspace > workspace_bytes) return KV_ELIMIT;
-    if (batch->num_q == 0) return KV_OK;
-    const int64_t all = batch->num_q * q->heads;
-    tkv::AttentionParams p;
-    p.cache = tkv::make_paged(layout, d_layer, batch);
-    p.q = (const char *)q->d_data;
-    p.out = (char *)const_cast<void *>(out->d_data);
-    p.q_ts = q->token_stride * 2, p.q_hs = q->head_stride * 2;
-    p.o_ts = out->token_stride * 2, p.o_hs = out->head_stride * 2;
-    p.lse = d_lse;
-    p.part_o = (float *)d_workspace;
-    p.part_ml = p.part_o ? p.part_o + (int64_t)plan.splits * all * layout->head_dim : nullptr;
-    p.k_scale = cache_dtype == KV_F8E4M3 ? d_k_scale : nullptr;
-    p.v_scale = cache_dtype == KV_F8E4M3 ? d_v_scale : nullptr;
-    p.tiles = plan.tiles;
-    p.scale = scale * tkv::kLog2e;
-    p.q_heads = q->heads;
-    p.kv_heads = layout->kv_heads;
-    p.group = q->heads / layout->kv_heads;
-    p.by_group = tkv::make_divider((uint32_t)p.group);
-    p.head_dim = layout->head_dim;
-    p.splits = plan.splits;
-    p.window = window < tkv::kMaxLength ? window : 0;
-    p.causal = causal != 0;
-    const bool bf16 = q->dtype == KV_BF16, f8 = cache_dtype == KV_F8E4M3;
-    const int d = layout->head_dim;
-    auto kernel = bf16 ? (f8 ? tkv::attention_kernel<tkv::Bf16, true>(plan.rows, d) : tkv::attention_kernel<tkv::Bf16, false>(plan.rows, d))
-                       : (f8 ? tkv::attention_kernel<tkv::F16, true>(plan.rows, d) : tkv::attention_kernel<tkv::F16, false>(plan.rows, d));
-    const int threads = plan.rows == tkv::kSplitRows ? tkv::kThreads : 2 * plan.rows;
-    hipStream_t s = (hipStream_t)stream;
-    (void)hipGetLastError();
-    hipLaunchKernelGGL(kernel, dim3((unsigned)(plan.tiles * p.kv_heads * p.splits)), dim3(threads), 0, s, p);
-    if (p.splits > 1) {
-        auto join = bf16 ? tkv::attention_join_kernel<tkv::Bf16> : tkv::attention_join_kernel<tkv::F16>;
-        hipLaunchKernelGGL(join, dim3((unsigned)((all + tkv::kWaves - 1) / tkv::kWaves)), dim3(tkv::kThreads), 0, s, p);
-    }
-    return hipGetLastError() == hipSuccess ? KV_OK : KV_EHIP;
+    return tkv::attention(layout, d_layer, batch, q, out, scale, causal, window, 0, cache_dtype, d_k_scale, d_v_scale, d_lse,
+                          d_workspace, workspace_bytes, stream);
+}
+
+int kv_sink_attention(const kv_layout *layout, const void *d_layer, const kv_batch *batch, const kv_rows *q,
+                      const kv_rows *out, float scale, int32_t causal, int32_t window, int32_t sink,
+                      int32_t cache_dtype, const float *d_k_scale, const float *d_v_scale, float *d_lse,
+                      void *d_workspace, int64_t workspace_bytes, void *stream) {
+    return tkv::attention(layout, d_layer, batch, q, out, scale, causal, window, sink, cache_dtype, d_k_scale, d_v_scale,
+                          d_lse, d_workspace, workspace_bytes, stream);
 }
 
 }  // extern "C"

@@ -105,12 +105,13 @@ int32_t attention_splits(int64_t tiles, int32_t num_reqs, int32_t kv_heads, int6
     return parts < 1 ? 1 : (int32_t)parts;
 }
 
-int plan_attention(const kv_layout *lo, const kv_batch *b, int32_t q_heads, int32_t window, AttentionPlan *plan) {
-    if (q_heads <= 0 || q_heads % lo->kv_heads != 0 || window < 0) return KV_EINVAL;
+int plan_attention(const kv_layout *lo, const kv_batch *b, int32_t q_heads, int32_t window, int32_t sink,
+                   AttentionPlan *plan) {
+    if (q_heads <= 0 || q_heads % lo->kv_heads != 0 || window < 0 || sink < 0) return KV_EINVAL;
     const int64_t group = q_heads / lo->kv_heads;
     if (b->num_q >= (int64_t(1) << 30) / q_heads) return KV_ELIMIT;       // rows are counted in 32 bits
     int64_t span = b->max_kv_len;
-    if (window > 0 && span > (int64_t)window + b->max_q_len) span = (int64_t)window + b->max_q_len;
+    if (window > 0 && span > (int64_t)window + b->max_q_len + sink) span = (int64_t)window + b->max_q_len + sink;
     // Tiles of 256 rows read K and V half as often as those of 128, but take a compute unit each: where there are four
     // rounds of them (8 x 2,048 tokens of 32 heads: 859 against 917 us; a mixed batch of fewer: 77 against 61 us).
     const bool many = b->max_q_len * group > kSplitRows;
@@ -122,6 +123,35 @@ int plan_attention(const kv_layout *lo, const kv_batch *b, int32_t q_heads, int3
     plan->splits = attention_splits(real, b->num_reqs, lo->kv_heads, span, many ? kTileStep : kSplitStep);
     plan->workspace = plan->splits > 1 ? (int64_t)plan->splits * b->num_q * q_heads * (lo->head_dim + 2) * 4 : 0;
     if (plan->tiles * lo->kv_heads * plan->splits >= (int64_t(1) << 31)) return KV_ELIMIT;
+    return KV_OK;
+}
+
+// sink < 0: the rule without sinks.
+int plan_weights(const kv_layout *lo, const kv_batch *b, int32_t q_heads, int32_t window, int32_t sink, WeightPlan *plan) {
+    const int64_t heads = (int64_t)b->num_reqs * lo->kv_heads, group = q_heads / lo->kv_heads;
+    if (heads >= (int64_t(1) << 31) || b->num_q >= (int64_t(1) << 30) / q_heads) return KV_ELIMIT;
+    plan->windowed = sink >= 0 && window > 0 && window < kMaxLength;
+    // Keys of a workgroup: 256, each wave 64 of its own, or 64, with the waves sharing the rows, where that is needed to
+    // give each compute unit two workgroups.  Up to 16 rows take a kernel of their own.
+    plan->few = b->max_q_len * group <= 16;
+    int64_t span = b->max_kv_len;
+    if (plan->windowed && span > (int64_t)window + b->max_q_len) span = (int64_t)window + b->max_q_len;
+    plan->keys = !plan->few && heads * ((span + 255) / 256) < 512 ? 64 : 256;
+    plan->sink_tiles = plan->parts = 0;
+    if (plan->windowed && !plan->few) {
+        // A sink's rows are all of a chunk's, a key's those of a window: as many parts as that is longer.  (Sums of
+        // parts need memory for each sink: more than 1,024 are not cut.)
+        int64_t tiles = ((int64_t)sink + 63) / 64, parts = (b->max_q_len + (int64_t)window + 255) / ((int64_t)window + 256);
+        parts = parts < 1 || tiles > 16 ? 1 : (parts > 64 ? 64 : parts);
+        plan->sink_tiles = (int32_t)(tiles > 256 ? 256 : tiles);
+        plan->parts = (int32_t)parts;
+    }
+    plan->workspace = plan->parts > 1 ? heads * plan->sink_tiles * plan->parts * 64 * 4 : 0;
+    // (few rows: the sinks lie next to the window's keys)
+    if (plan->windowed && plan->few) span += sink;
+    if (span > b->max_kv_len) span = b->max_kv_len;
+    int64_t tiles = (span + plan->keys - 1) / plan->keys;
+    plan->tiles = tiles < 1 ? 1 : (tiles > 32768 ? 32768 : tiles);
     return KV_OK;
 }
 
@@ -159,14 +189,55 @@ int kv_rope_frequencies(int32_t rot_dim, double base, int32_t scaling, double fa
     return KV_OK;
 }
 
+int kv_rope_axes(int32_t num_axes, const int32_t *h_sections, int32_t order, uint8_t *h_axis) {
+    if (num_axes <= 0 || num_axes > KV_MAX_AXES || !h_sections) return KV_EINVAL;
+    if (order != KV_AXES_SECTIONS && order != KV_AXES_IN_TURN) return KV_EINVAL;
+    int64_t pairs = 0;
+    int32_t longest = 0;
+    for (int32_t a = 0; a < num_axes; ++a) {
+        if (h_sections[a] < 0) return KV_EINVAL;
+        pairs += h_sections[a];
+        if (h_sections[a] > longest) longest = h_sections[a];
+    }
+    if (pairs > tkv::kMaxHeadDim / 2) return KV_ELIMIT;
+    if (pairs > 0 && !h_axis) return KV_EINVAL;
+    if (order == KV_AXES_SECTIONS) {
+        for (int32_t a = 0; a < num_axes; ++a)
+            for (int32_t i = 0; i < h_sections[a]; ++i) *h_axis++ = (uint8_t)a;
+    } else {
+        for (int32_t i = 0; i < longest; ++i)
+            for (int32_t a = 0; a < num_axes; ++a)
+                if (i < h_sections[a]) *h_axis++ = (uint8_t)a;
+    }
+    return KV_OK;
+}
+
 int kv_paged_attention_workspace(const kv_layout *layout, const kv_batch *batch, int32_t q_heads, int32_t window,
                                  int64_t *bytes) {
+    return kv_sink_attention_workspace(layout, batch, q_heads, window, 0, bytes);
+}
+
+int kv_sink_attention_workspace(const kv_layout *layout, const kv_batch *batch, int32_t q_heads, int32_t window,
+                                int32_t sink, int64_t *bytes) {
     int rc = check_layout(layout);
     if (rc == KV_OK) rc = tkv::check_batch(batch);
     if (rc != KV_OK) return rc;
     if (!bytes) return KV_EINVAL;
     tkv::AttentionPlan plan;
-    rc = tkv::plan_attention(layout, batch, q_heads, window, &plan);
+    rc = tkv::plan_attention(layout, batch, q_heads, window, sink, &plan);
+    if (rc != KV_OK) return rc;
+    *bytes = plan.workspace;
+    return KV_OK;
+}
+
+int kv_sink_weights_workspace(const kv_layout *layout, const kv_batch *batch, int32_t q_heads, int32_t window,
+                              int32_t sink, int64_t *bytes) {
+    int rc = check_layout(layout);
+    if (rc == KV_OK) rc = tkv::check_batch(batch);
+    if (rc != KV_OK) return rc;
+    if (!bytes || q_heads <= 0 || q_heads % layout->kv_heads != 0 || window < 0 || sink < 0) return KV_EINVAL;
+    tkv::WeightPlan plan;
+    rc = tkv::plan_weights(layout, batch, q_heads, window, sink, &plan);
     if (rc != KV_OK) return rc;
     *bytes = plan.workspace;
     return KV_OK;

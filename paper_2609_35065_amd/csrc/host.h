@@ -27,10 +27,21 @@ struct AttentionPlan {
     int64_t workspace;    // bytes
 };
 
+struct WeightPlan {
+    bool windowed;        // the kernels that know which keys a window leaves out
+    bool few;             // no request has more than 16 rows a head
+    int32_t keys;         // of a workgroup's tile of many rows: 64 or 256
+    int64_t tiles;        // workgroups for keys, each for every request and KV head
+    int32_t sink_tiles;   // and for 64 sinks each,
+    int32_t parts;        // times the parts that their rows are cut into
+    int64_t workspace;    // bytes
+};
+
 int check_cache(const kv_layout *lo, int32_t cache_dtype);
 int check_span(const kv_layout *lo);
 int check_batch(const kv_batch *b);
 int check_rows(const kv_rows *x, int64_t num, int32_t head_dim, bool written);
-int plan_attention(const kv_layout *lo, const kv_batch *b, int32_t q_heads, int32_t window, AttentionPlan *plan);
+int plan_attention(const kv_layout *lo, const kv_batch *b, int32_t q_heads, int32_t window, int32_t sink, AttentionPlan *plan);
+int plan_weights(const kv_layout *lo, const kv_batch *b, int32_t q_heads, int32_t window, int32_t sink, WeightPlan *plan);
 
 }  // namespace tkv

@@ -5,6 +5,7 @@
 // The angle needs more than 32 bits (position 100,000 times 1 radian leaves
 // 2^-7 radians of a float's mantissa), so the product and its remainder by a
 // turn are formed in 64 bits, once per (token, pair), and shared by all heads.
+// With several axes p is the row's position on the pair's axis.
 
 #include "paged.h"
 
@@ -20,6 +21,7 @@ struct RopeParams {
     int64_t q_ts, q_hs, o_ts, o_hs, k_ts, k_hs, v_ts, v_hs;   // bytes
     const double *freqs;
     const int32_t *positions;
+    int64_t position_stride;                                  // between the positions of one axis and the next
     const float *k_scale, *v_scale;
     int32_t q_heads, kv_heads;
     Divider by_token, by_row, by_half;
@@ -28,6 +30,7 @@ struct RopeParams {
     int32_t row_units, token_units;
     int32_t per_block;     // tokens a workgroup takes
     float magnitude, sign;
+    uint8_t axis[kMaxHeadDim / 2];                            // of each pair
 };
 
 template <bool BF16> __device__ __forceinline__ float to_f32(uint32_t bits16) {
@@ -68,7 +71,7 @@ __device__ __forceinline__ uint32_t pack4_f8(float a, float b, float c, float d)
 // 53 us (4.6 TB/s).
 enum Pairing { HALF, INTERLEAVED, ODD };
 
-template <bool BF16, bool F8, Pairing PAIR>
+template <bool BF16, bool F8, Pairing PAIR, bool AXES>
 __global__ __launch_bounds__(kThreads) void rope_append_kernel(RopeParams p) {
     extern __shared__ __align__(16) float trig[];                       // [per_block][half4] cos, then sin
     __shared__ int32_t where_index[kMaxTokens];
@@ -141,7 +144,9 @@ __global__ __launch_bounds__(kThreads) void rope_append_kernel(RopeParams p) {
     __syncthreads();
     for (int x = tid; x < n * p.half; x += kThreads) {
         const int i = (int)divide(x, p.by_half), j = x - i * p.half;
-        const double pos = p.positions ? p.positions[t0 + i] : where_index[i];
+        double pos;
+        if constexpr (AXES) pos = p.positions[p.axis[j] * p.position_stride + t0 + i];
+        else pos = p.positions ? p.positions[t0 + i] : where_index[i];
         double angle = pos * p.freqs[j];
         angle -= rint(angle * 0.15915494309189533577) * 6.283185307179586476925;
         float s, c;
@@ -254,9 +259,90 @@ __global__ __launch_bounds__(kThreads) void rope_append_kernel(RopeParams p) {
     }
 }
 
-template <bool BF16, bool F8> auto rope_kernel(Pairing pair) {
-    return pair == HALF ? rope_append_kernel<BF16, F8, HALF>
-                        : (pair == INTERLEAVED ? rope_append_kernel<BF16, F8, INTERLEAVED> : rope_append_kernel<BF16, F8, ODD>);
+template <bool BF16, bool F8, bool AXES> auto rope_kernel(Pairing pair) {
+    return pair == HALF ? rope_append_kernel<BF16, F8, HALF, AXES>
+                        : (pair == INTERLEAVED ? rope_append_kernel<BF16, F8, INTERLEAVED, AXES>
+                                               : rope_append_kernel<BF16, F8, ODD, AXES>);
+}
+
+template <bool AXES> auto rope_kernel(bool bf16, bool f8, Pairing pair) {
+    return bf16 ? (f8 ? rope_kernel<true, true, AXES>(pair) : rope_kernel<true, false, AXES>(pair))
+                : (f8 ? rope_kernel<false, true, AXES>(pair) : rope_kernel<false, false, AXES>(pair));
+}
+
+// The append with one position a row (num_axes 0), or several and the axis of each pair.
+int rope_append(const kv_layout *layout, void *d_layer, const kv_batch *batch, const kv_rows *q, const kv_rows *q_out,
+                const kv_rows *k, const kv_rows *v, const double *d_freqs, int32_t rot_dim, int32_t flags,
+                float magnitude, const int32_t *d_positions, int64_t position_stride, int32_t num_axes,
+                const uint8_t *h_axis, int32_t cache_dtype, const float *d_k_scale, const float *d_v_scale,
+                void *stream) {
+    int rc = check_cache(layout, cache_dtype);
+    if (rc == KV_OK) rc = check_batch(batch);
+    if (rc != KV_OK) return rc;
+    const int32_t d = layout->head_dim;
+    if ((!q && !k) || !q != !q_out || !k != !v || (k && !d_layer)) return KV_EINVAL;
+    if (q && ((rc = check_rows(q, batch->num_q, d, false)) != KV_OK ||
+              (rc = check_rows(q_out, batch->num_q, d, true)) != KV_OK))
+        return rc;
+    if (k && ((rc = check_rows(k, batch->num_q, d, false)) != KV_OK ||
+              (rc = check_rows(v, batch->num_q, d, false)) != KV_OK))
+        return rc;
+    const int32_t dtype = q ? q->dtype : k->dtype;
+    if (q && (q_out->dtype != dtype || q_out->heads != q->heads)) return KV_EINVAL;
+    if (k && (k->dtype != dtype || v->dtype != dtype || k->heads != layout->kv_heads || v->heads != layout->kv_heads))
+        return KV_EINVAL;
+    if (k && cache_dtype != KV_F8E4M3 && cache_dtype != dtype) return KV_EINVAL;
+    if (rot_dim < 0 || rot_dim % 2 != 0 || rot_dim > d || (rot_dim > 0 && !d_freqs)) return KV_EINVAL;
+    if (flags & ~(KV_ROPE_INTERLEAVED | KV_ROPE_INVERSE)) return KV_EINVAL;
+    RopeParams p;
+    if (num_axes > 0) {
+        if (rot_dim > 0 && !h_axis) return KV_EINVAL;
+        for (int32_t i = 0; i < rot_dim / 2; ++i) {
+            if (h_axis[i] >= num_axes) return KV_EINVAL;
+            p.axis[i] = h_axis[i];
+        }
+        if (batch->num_q > 0 && rot_dim > 0 && (!d_positions || position_stride < batch->num_q)) return KV_EINVAL;
+    }
+    if (((uintptr_t)d_layer & 15u) || ((uintptr_t)d_freqs & 7u) || ((uintptr_t)d_positions & 3u)) return KV_EALIGN;
+    if (batch->num_q == 0) return KV_OK;
+    p.cache = make_paged(layout, d_layer, batch);
+    p.q = q ? (const char *)q->d_data : nullptr;
+    p.q_out = q ? (char *)const_cast<void *>(q_out->d_data) : nullptr;
+    p.k = k ? (const char *)k->d_data : nullptr;
+    p.v = k ? (const char *)v->d_data : nullptr;
+    p.q_ts = q ? q->token_stride * 2 : 0, p.q_hs = q ? q->head_stride * 2 : 0;
+    p.o_ts = q ? q_out->token_stride * 2 : 0, p.o_hs = q ? q_out->head_stride * 2 : 0;
+    p.k_ts = k ? k->token_stride * 2 : 0, p.k_hs = k ? k->head_stride * 2 : 0;
+    p.v_ts = k ? v->token_stride * 2 : 0, p.v_hs = k ? v->head_stride * 2 : 0;
+    p.freqs = d_freqs;
+    p.positions = d_positions;
+    p.position_stride = position_stride;
+    p.k_scale = d_k_scale;
+    p.v_scale = d_v_scale;
+    p.q_heads = q ? q->heads : 0;
+    p.kv_heads = layout->kv_heads;
+    p.vecs = d / 8;
+    p.half = rot_dim / 2;
+    p.magnitude = magnitude;
+    p.sign = (flags & KV_ROPE_INVERSE) ? -1.0f : 1.0f;
+    const Pairing pair = (flags & KV_ROPE_INTERLEAVED) ? INTERLEAVED : (p.half % 8 ? ODD : HALF);
+    const int hv = pair == HALF ? p.half / 8 : 0;
+    p.row_units = hv + (p.vecs - 2 * hv + 1) / 2;
+    p.token_units = p.row_units * (p.q_heads + (k ? 2 * p.kv_heads : 0));
+    p.by_row = make_divider((uint32_t)p.row_units);
+    p.by_token = make_divider((uint32_t)p.token_units);
+    p.by_half = make_divider((uint32_t)(p.half ? p.half : 1));
+    // Four tokens share a workgroup's start where there are workgroups enough; few tokens take one each.
+    const int64_t share = batch->num_q / 1024;
+    p.per_block = share < 1 ? 1 : (share > kMaxTokens ? kMaxTokens : (int)share);
+    const int64_t blocks = (batch->num_q + p.per_block - 1) / p.per_block;
+    if (blocks >= (int64_t(1) << 31)) return KV_ELIMIT;
+    const size_t lds = (size_t)p.per_block * ((p.half + 3) & ~3) * 2 * sizeof(float);
+    const bool f8 = cache_dtype == KV_F8E4M3;
+    auto kernel = num_axes > 0 ? rope_kernel<true>(dtype == KV_BF16, f8, pair) : rope_kernel<false>(dtype == KV_BF16, f8, pair);
+    (void)hipGetLastError();
+    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(kThreads), lds, (hipStream_t)stream, p);
+    return hipGetLastError() == hipSuccess ? KV_OK : KV_EHIP;
 }
 
 }  // namespace
@@ -268,65 +354,18 @@ int kv_rope_append(const kv_layout *layout, void *d_layer, const kv_batch *batch
                    const kv_rows *q_out, const kv_rows *k, const kv_rows *v, const double *d_freqs, int32_t rot_dim,
                    int32_t flags, float magnitude, const int32_t *d_positions, int32_t cache_dtype,
                    const float *d_k_scale, const float *d_v_scale, void *stream) {
-    int rc = tkv::check_cache(layout, cache_dtype);
-    if (rc == KV_OK) rc = tkv::check_batch(batch);
-    if (rc != KV_OK) return rc;
-    const int32_t d = layout->head_dim;
-    if ((!q && !k) || !q != !q_out || !k != !v || (k && !d_layer)) return KV_EINVAL;
-    if (q && ((rc = tkv::check_rows(q, batch->num_q, d, false)) != KV_OK ||
-              (rc = tkv::check_rows(q_out, batch->num_q, d, true)) != KV_OK))
-        return rc;
-    if (k && ((rc = tkv::check_rows(k, batch->num_q, d, false)) != KV_OK ||
-              (rc = tkv::check_rows(v, batch->num_q, d, false)) != KV_OK))
-        return rc;
-    const int32_t dtype = q ? q->dtype : k->dtype;
-    if (q && (q_out->dtype != dtype || q_out->heads != q->heads)) return KV_EINVAL;
-    if (k && (k->dtype != dtype || v->dtype != dtype || k->heads != layout->kv_heads || v->heads != layout->kv_heads))
-        return KV_EINVAL;
-    if (k && cache_dtype != KV_F8E4M3 && cache_dtype != dtype) return KV_EINVAL;
-    if (rot_dim < 0 || rot_dim % 2 != 0 || rot_dim > d || (rot_dim > 0 && !d_freqs)) return KV_EINVAL;
-    if (flags & ~(KV_ROPE_INTERLEAVED | KV_ROPE_INVERSE)) return KV_EINVAL;
-    if (((uintptr_t)d_layer & 15u) || ((uintptr_t)d_freqs & 7u) || ((uintptr_t)d_positions & 3u)) return KV_EALIGN;
-    if (batch->num_q == 0) return KV_OK;
-    tkv::RopeParams p;
-    p.cache = tkv::make_paged(layout, d_layer, batch);
-    p.q = q ? (const char *)q->d_data : nullptr;
-    p.q_out = q ? (char *)const_cast<void *>(q_out->d_data) : nullptr;
-    p.k = k ? (const char *)k->d_data : nullptr;
-    p.v = k ? (const char *)v->d_data : nullptr;
-    p.q_ts = q ? q->token_stride * 2 : 0, p.q_hs = q ? q->head_stride * 2 : 0;
-    p.o_ts = q ? q_out->token_stride * 2 : 0, p.o_hs = q ? q_out->head_stride * 2 : 0;
-    p.k_ts = k ? k->token_stride * 2 : 0, p.k_hs = k ? k->head_stride * 2 : 0;
-    p.v_ts = k ? v->token_stride * 2 : 0, p.v_hs = k ? v->head_stride * 2 : 0;
-    p.freqs = d_freqs;
-    p.positions = d_positions;
-    p.k_scale = d_k_scale;
-    p.v_scale = d_v_scale;
-    p.q_heads = q ? q->heads : 0;
-    p.kv_heads = layout->kv_heads;
-    p.vecs = d / 8;
-    p.half = rot_dim / 2;
-    p.magnitude = magnitude;
-    p.sign = (flags & KV_ROPE_INVERSE) ? -1.0f : 1.0f;
-    const tkv::Pairing pair = (flags & KV_ROPE_INTERLEAVED) ? tkv::INTERLEAVED : (p.half % 8 ? tkv::ODD : tkv::HALF);
-    const int hv = pair == tkv::HALF ? p.half / 8 : 0;
-    p.row_units = hv + (p.vecs - 2 * hv + 1) / 2;
-    p.token_units = p.row_units * (p.q_heads + (k ? 2 * p.kv_heads : 0));
-    p.by_row = tkv::make_divider((uint32_t)p.row_units);
-    p.by_token = tkv::make_divider((uint32_t)p.token_units);
-    p.by_half = tkv::make_divider((uint32_t)(p.half ? p.half : 1));
-    // Four tokens share a workgroup's start where there are workgroups enough; few tokens take one each.
-    const int64_t share = batch->num_q / 1024;
-    p.per_block = share < 1 ? 1 : (share > tkv::kMaxTokens ? tkv::kMaxTokens : (int)share);
-    const int64_t blocks = (batch->num_q + p.per_block - 1) / p.per_block;
-    if (blocks >= (int64_t(1) << 31)) return KV_ELIMIT;
-    const size_t lds = (size_t)p.per_block * ((p.half + 3) & ~3) * 2 * sizeof(float);
-    const bool f8 = cache_dtype == KV_F8E4M3;
-    auto kernel = dtype == KV_BF16 ? (f8 ? tkv::rope_kernel<true, true>(pair) : tkv::rope_kernel<true, false>(pair))
-                                   : (f8 ? tkv::rope_kernel<false, true>(pair) : tkv::rope_kernel<false, false>(pair));
-    (void)hipGetLastError();
-    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(tkv::kThreads), lds, (hipStream_t)stream, p);
-    return hipGetLastError() == hipSuccess ? KV_OK : KV_EHIP;
+    return tkv::rope_append(layout, d_layer, batch, q, q_out, k, v, d_freqs, rot_dim, flags, magnitude, d_positions, 0, 0,
+                            nullptr, cache_dtype, d_k_scale, d_v_scale, stream);
+}
+
+int kv_rope_append_axes(const kv_layout *layout, void *d_layer, const kv_batch *batch, const kv_rows *q,
+                        const kv_rows *q_out, const kv_rows *k, const kv_rows *v, const double *d_freqs,
+                        int32_t rot_dim, int32_t flags, float magnitude, const int32_t *d_positions,
+                        int64_t position_stride, int32_t num_axes, const uint8_t *h_axis, int32_t cache_dtype,
+                        const float *d_k_scale, const float *d_v_scale, void *stream) {
+    if (num_axes <= 0 || num_axes > KV_MAX_AXES) return KV_EINVAL;
+    return tkv::rope_append(layout, d_layer, batch, q, q_out, k, v, d_freqs, rot_dim, flags, magnitude, d_positions,
+                            position_stride, num_axes, h_axis, cache_dtype, d_k_scale, d_v_scale, stream);
 }
 
 }  // extern "C"

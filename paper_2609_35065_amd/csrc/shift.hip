@@ -1,0 +1,278 @@
+// shift.hip -- keys that lie in the paged cache turned to other positions.
+//
+// Rotations add: a key turned by p f_i that is turned again by s f_i is one of
+// position p + s.  Pair (a, b) becomes (a cos u - b sin u, a sin u + b cos u),
+// u = s f_i, the product and its remainder by a turn in 64 bits.
+
+#include "mfma.h"
+#include "paged.h"
+
+namespace tkv {
+namespace {
+
+constexpr int kThreads = 256, kWaves = kThreads / 64;
+constexpr int kTokens = 64, kHeads = 16;       // of a workgroup's tile
+constexpr int kPairs = 8;                      // of a lane's unit
+
+struct ShiftParams {
+    Paged cache;
+    char *layers[KV_MAX_LAYERS];
+    const int32_t *len, *shift;
+    int64_t shift_stride;
+    const double *freqs;
+    int32_t shift_layers, shift_heads;         // 1: one shift for all
+    int32_t kv_heads, groups;                  // groups of kHeads heads
+    int32_t half, units;                       // pairs of a row, and units
+    Divider by_heads;                          // of a full group
+    float sign;
+};
+
+// Elements at any alignment.
+typedef u32x4 __attribute__((aligned(1))) u32x4_any;
+typedef u32x2 __attribute__((aligned(1))) u32x2_any;
+
+// N elements of the cache's type, and as 32-bit values.
+template <class T, bool F8, int N> struct Elements {
+    uint32_t raw[F8 ? N / 4 : N / 2];
+    __device__ __forceinline__ void load(const char *at) {
+        constexpr int kWords = F8 ? N / 4 : N / 2;
+        if constexpr (kWords == 2) {
+            const u32x2 x = *(const u32x2_any *)at;
+            raw[0] = x[0], raw[1] = x[1];
+        } else {
+#pragma unroll
+            for (int i = 0; i < kWords; i += 4) {
+                const u32x4 x = *(const u32x4_any *)(at + i * 4);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) raw[i + e] = x[e];
+            }
+        }
+    }
+    __device__ __forceinline__ void store(char *at) const {
+        constexpr int kWords = F8 ? N / 4 : N / 2;
+        if constexpr (kWords == 2) {
+            *(u32x2_any *)at = u32x2{raw[0], raw[1]};
+        } else {
+#pragma unroll
+            for (int i = 0; i < kWords; i += 4) *(u32x4_any *)(at + i * 4) = u32x4{raw[i], raw[i + 1], raw[i + 2], raw[i + 3]};
+        }
+    }
+    __device__ __forceinline__ void get(float (&x)[N]) const {
+#pragma unroll
+        for (int i = 0; i < N; i += 2) {
+            if constexpr (F8) {
+                const uint32_t y = i & 2 ? T::from_f8(raw[i / 4], true) : T::from_f8(raw[i / 4], false);
+                x[i] = T::to_f32(y & 0xffffu), x[i + 1] = T::to_f32(y >> 16);
+            } else {
+                x[i] = T::to_f32(raw[i / 2] & 0xffffu), x[i + 1] = T::to_f32(raw[i / 2] >> 16);
+            }
+        }
+    }
+    // rounded once, to nearest even; in 8 bits values beyond 448 become 448, NaN stays
+    __device__ __forceinline__ void set(const float (&x)[N]) {
+        if constexpr (F8) {
+            const auto clamp = [](float y) { return y != y ? y : fminf(fmaxf(y, -448.0f), 448.0f); };
+#pragma unroll
+            for (int i = 0; i < N; i += 4) {
+                const int y = __builtin_amdgcn_cvt_pk_fp8_f32(clamp(x[i]), clamp(x[i + 1]), 0, false);
+                raw[i / 4] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(clamp(x[i + 2]), clamp(x[i + 3]), y, true);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; i += 2) raw[i / 2] = pack2<T>(x[i], x[i + 1]);
+        }
+    }
+};
+
+// One workgroup: a layer, a request, up to 16 heads and 64 tokens.  Where the
+// tokens lie and their shifts go to LDS first.  A lane takes eight pairs of a
+// row, always the same ones, so that it holds their frequencies; a row's last
+// unit ends at its last pair and may overlap the one before.  A row lies in one
+// wave, which reads all of it before it writes.
+template <class T, bool F8, bool INTERLEAVED>
+__global__ __launch_bounds__(kThreads) void rope_shift_kernel(ShiftParams p) {
+    constexpr int kElem = F8 ? 1 : 2, kAhead = 4;
+    __shared__ uint32_t where[kTokens];            // 16-byte units from the plane's start
+    __shared__ int32_t by[kHeads][kTokens];        // 0: left as it is
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int group = (int)(blockIdx.x % p.groups);
+    const int64_t lr = blockIdx.x / p.groups;
+    const int r = (int)(lr % p.cache.num_reqs), l = (int)(lr / p.cache.num_reqs);
+    const int head0 = group * kHeads, heads = min(kHeads, p.kv_heads - head0);
+    const int64_t len = min((int64_t)max(p.len[r], 0), p.shift_stride);
+    const int32_t *shift = p.shift + ((int64_t)(p.shift_layers > 1 ? l : 0) * p.cache.num_reqs + r) * p.shift_heads * p.shift_stride;
+    char *base = p.layers[l];
+
+    const int slot = lane / p.units, unit = lane - slot * p.units, rows = 64 / p.units;     // of a wave
+    const bool on = slot < rows;
+    const int pair0 = min(unit * kPairs, p.half - kPairs);
+    double f[kPairs];                              // turns a position
+#pragma unroll
+    for (int i = 0; i < kPairs; ++i) f[i] = p.freqs[pair0 + i] * 0.15915494309189533577;
+    const int first = (INTERLEAVED ? 2 * pair0 : pair0) * kElem, second = (p.half + pair0) * kElem;     // bytes
+
+    for (int64_t t0 = (int64_t)blockIdx.y * kTokens; t0 < len; t0 += (int64_t)gridDim.y * kTokens) {
+        const int n = (int)min((int64_t)kTokens, len - t0);
+        __syncthreads();                           // the tile before is done
+        for (int x = tid; x < heads * kTokens; x += kThreads) {
+            const int t = x % kTokens, h = x / kTokens;
+            uint32_t row = 0;
+            const int32_t id = t < n ? block_of(p.cache, r, (uint32_t)(t0 + t), row) : -1;
+            if (h == 0) where[t] = id < 0 ? 0u : (uint32_t)id * p.cache.block16 + row * p.cache.row16;
+            by[h][t] = id < 0 ? 0 : shift[(p.shift_heads > 1 ? (int64_t)(head0 + h) * p.shift_stride : 0) + t0 + t];
+        }
+        __syncthreads();
+        const int total = n * heads, step = kWaves * rows;
+        for (int x0 = wave * rows; x0 < total; x0 += kAhead * step) {
+            Elements<T, F8, INTERLEAVED ? 16 : 8> a[kAhead], b[kAhead];
+            int s[kAhead];
+            char *at[kAhead];
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                const int x = x0 + i * step + slot;
+                s[i] = 0;
+                if (!on || x >= total) continue;
+                const int t = heads == kHeads ? x / kHeads : (int)divide(x, p.by_heads), h = x - t * heads;
+                s[i] = by[h][t];
+                at[i] = base + ((int64_t)where[t] << 4) + (int64_t)(head0 + h) * p.cache.head_bytes;
+                if (s[i] == 0) continue;
+                a[i].load(at[i] + first);
+                if constexpr (!INTERLEAVED) b[i].load(at[i] + second);
+            }
+            // units of a row overlap, in the same instructions of a wave: all are read here
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                if (s[i] == 0) continue;
+                float xa[INTERLEAVED ? 16 : 8], xb[8];
+                a[i].get(xa);
+                if constexpr (!INTERLEAVED) b[i].get(xb);
+#pragma unroll
+                for (int e = 0; e < kPairs; ++e) {
+                    const double turns = s[i] * f[e];
+                    const float u = (float)(turns - rint(turns));
+                    const float c = __builtin_amdgcn_cosf(u), si = __builtin_amdgcn_sinf(u) * p.sign;
+                    float &ra = xa[INTERLEAVED ? 2 * e : e], &rb = INTERLEAVED ? xa[(2 * e + 1) % (INTERLEAVED ? 16 : 8)] : xb[e];
+                    const float va = ra, vb = rb;
+                    ra = __builtin_fmaf(va, c, -vb * si);
+                    rb = __builtin_fmaf(va, si, vb * c);
+                }
+                a[i].set(xa);
+                a[i].store(at[i] + first);
+                if constexpr (!INTERLEAVED) {
+                    b[i].set(xb);
+                    b[i].store(at[i] + second);
+                }
+            }
+        }
+    }
+}
+
+// Rows of fewer than eight pairs: a lane takes one.
+template <class T, bool F8, bool INTERLEAVED>
+__global__ __launch_bounds__(kThreads) void rope_shift_short_kernel(ShiftParams p) {
+    const int64_t lr = blockIdx.x / p.groups;
+    const int r = (int)(lr % p.cache.num_reqs), l = (int)(lr / p.cache.num_reqs), head0 = (int)(blockIdx.x % p.groups) * kHeads;
+    const int heads = min(kHeads, p.kv_heads - head0), per_token = heads * p.half;
+    const int64_t len = min((int64_t)max(p.len[r], 0), p.shift_stride);
+    const int32_t *shift = p.shift + ((int64_t)(p.shift_layers > 1 ? l : 0) * p.cache.num_reqs + r) * p.shift_heads * p.shift_stride;
+    for (int64_t t0 = (int64_t)blockIdx.y * kTokens; t0 < len; t0 += (int64_t)gridDim.y * kTokens) {
+        const int n = (int)min((int64_t)kTokens, len - t0);
+        for (int x = threadIdx.x; x < n * per_token; x += kThreads) {
+            const int t = x / per_token, y = x - t * per_token, h = y / p.half, i = y - h * p.half;
+            uint32_t row = 0;
+            const int32_t id = block_of(p.cache, r, (uint32_t)(t0 + t), row);
+            const int s = id < 0 ? 0 : shift[(p.shift_heads > 1 ? (int64_t)(head0 + h) * p.shift_stride : 0) + t0 + t];
+            if (s == 0) continue;
+            char *at = p.layers[l] + ((int64_t)((uint32_t)id * p.cache.block16 + row * p.cache.row16) << 4) +
+                       (int64_t)(head0 + h) * p.cache.head_bytes;
+            const int ia = INTERLEAVED ? 2 * i : i, ib = INTERLEAVED ? 2 * i + 1 : i + p.half;
+            const double turns = s * (p.freqs[i] * 0.15915494309189533577);
+            const float u = (float)(turns - rint(turns));
+            const float c = __builtin_amdgcn_cosf(u), si = __builtin_amdgcn_sinf(u) * p.sign;
+            Elements<T, F8, 4> one;
+            float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+            float w[4];
+            if constexpr (F8) {
+                one.raw[0] = ((const uint8_t *)at)[ia] | (uint32_t)((const uint8_t *)at)[ib] << 8;
+            } else {
+                one.raw[0] = ((const uint16_t *)at)[ia] | (uint32_t)((const uint16_t *)at)[ib] << 16;
+                one.raw[1] = 0;
+            }
+            one.get(w);
+            v[0] = __builtin_fmaf(w[0], c, -w[1] * si);
+            v[1] = __builtin_fmaf(w[0], si, w[1] * c);
+            one.set(v);
+            if constexpr (F8) {
+                ((uint8_t *)at)[ia] = (uint8_t)one.raw[0];
+                ((uint8_t *)at)[ib] = (uint8_t)(one.raw[0] >> 8);
+            } else {
+                ((uint16_t *)at)[ia] = (uint16_t)one.raw[0];
+                ((uint16_t *)at)[ib] = (uint16_t)(one.raw[0] >> 16);
+            }
+        }
+    }
+}
+
+template <class T, bool F8> void (*shift_kernel(bool interleaved, bool small))(ShiftParams) {
+    if (small) return interleaved ? rope_shift_short_kernel<T, F8, true> : rope_shift_short_kernel<T, F8, false>;
+    return interleaved ? rope_shift_kernel<T, F8, true> : rope_shift_kernel<T, F8, false>;
+}
+
+}  // namespace
+}  // namespace tkv
+
+extern "C" {
+
+int kv_rope_shift(const kv_layout *layout, void *const *h_layer_ptrs, const int32_t *d_block_tables, int32_t bt_stride,
+                  int32_t num_reqs, const int32_t *d_len, int32_t max_len, int32_t layers, int32_t heads,
+                  const int32_t *d_shift, int64_t shift_stride, const double *d_freqs, int32_t rot_dim, int32_t flags,
+                  int32_t cache_dtype, void *stream) {
+    int rc = tkv::check_cache(layout, cache_dtype);
+    if (rc != KV_OK) return rc;
+    if (!h_layer_ptrs || bt_stride <= 0 || num_reqs < 0 || max_len < 0 || shift_stride < 0) return KV_EINVAL;
+    if ((layers != 1 && layers != layout->num_layers) || (heads != 1 && heads != layout->kv_heads)) return KV_EINVAL;
+    if (rot_dim < 0 || rot_dim % 2 != 0 || rot_dim > layout->head_dim || (rot_dim > 0 && !d_freqs)) return KV_EINVAL;
+    if (flags & ~(KV_ROPE_INTERLEAVED | KV_ROPE_INVERSE)) return KV_EINVAL;
+    if (num_reqs > 0 && (!d_block_tables || !d_len || (!d_shift && shift_stride > 0))) return KV_EINVAL;
+    if (((uintptr_t)d_block_tables & 3u) || ((uintptr_t)d_len & 3u) || ((uintptr_t)d_shift & 3u) || ((uintptr_t)d_freqs & 7u))
+        return KV_EALIGN;
+    tkv::ShiftParams p;
+    for (int l = 0; l < layout->num_layers; ++l) {
+        if (!h_layer_ptrs[l]) return KV_EINVAL;
+        if ((uintptr_t)h_layer_ptrs[l] & 15u) return KV_EALIGN;
+        p.layers[l] = (char *)h_layer_ptrs[l];
+    }
+    p.groups = (layout->kv_heads + tkv::kHeads - 1) / tkv::kHeads;
+    if (layout->kv_heads > tkv::kMaxHeads || (int64_t)layout->num_layers * num_reqs >= (int64_t(1) << 31) / p.groups) return KV_ELIMIT;
+    if (num_reqs == 0 || shift_stride == 0 || rot_dim == 0) return KV_OK;
+    kv_batch b = {};
+    b.num_reqs = num_reqs;
+    b.bt_stride = bt_stride;
+    b.d_block_tables = d_block_tables;
+    p.cache = tkv::make_paged(layout, nullptr, &b);
+    p.len = d_len;
+    p.shift = d_shift;
+    p.shift_stride = shift_stride;
+    p.freqs = d_freqs;
+    p.shift_layers = layers;
+    p.shift_heads = heads;
+    p.kv_heads = layout->kv_heads;
+    p.half = rot_dim / 2;
+    p.units = (p.half + tkv::kPairs - 1) / tkv::kPairs;
+    p.by_heads = tkv::make_divider((uint32_t)(layout->kv_heads % tkv::kHeads ? layout->kv_heads % tkv::kHeads : tkv::kHeads));
+    p.sign = (flags & KV_ROPE_INVERSE) ? -1.0f : 1.0f;
+    const bool small = p.half < tkv::kPairs, inter = flags & KV_ROPE_INTERLEAVED;
+    auto kernel = cache_dtype == KV_F8E4M3 ? tkv::shift_kernel<tkv::Bf16, true>(inter, small)
+                                           : (cache_dtype == KV_BF16 ? tkv::shift_kernel<tkv::Bf16, false>(inter, small)
+                                                                     : tkv::shift_kernel<tkv::F16, false>(inter, small));
+    int64_t tiles = ((int64_t)max_len + tkv::kTokens - 1) / tkv::kTokens;
+    tiles = tiles < 1 ? 1 : (tiles > 65535 ? 65535 : tiles);
+    (void)hipGetLastError();
+    hipLaunchKernelGGL(kernel, dim3((unsigned)((int64_t)layout->num_layers * num_reqs * p.groups), (unsigned)tiles),
+                       dim3(tkv::kThreads), 0, (hipStream_t)stream, p);
+    return hipGetLastError() == hipSuccess ? KV_OK : KV_EHIP;
+}
+
+}  // extern "C"
