@@ -1,0 +1,189 @@
+"""kv_rope_append_axes against the definition in 64 bits, and against kv_rope_append where all axes have one position."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paged_ref as ref
+import paper_2609_35065_amd as kv
+import stream_ref
+
+pytestmark = pytest.mark.gpu
+F8 = torch.float8_e4m3fn
+
+
+def _case(new, lengths, sections, order=False, hq=4, heads=2, dim=64, dtype=torch.bfloat16, cache=None, interleaved=False,
+          magnitude=1.0, block=16, layout="kv_first", seed=0, in_place=False, inverse=False, top=5000, gap=2, pos_gap=0,
+          with_q=True, with_kv=True):
+    c = ref.Cache(lengths, heads=heads, dim=dim, dtype=cache or dtype, block=block, layout=layout, seed=seed, q_dtype=dtype,
+                  pad=32)
+    n, half = sum(new), sum(sections)
+    q, k, v = (ref.rows_of(n, h, dim, dtype, c.gen, 1.0, gap) for h in (hq, heads, heads))
+    freqs = kv.kv_rope_frequencies(2 * half)[0]
+    axes = kv.kv_rope_axes(sections, interleaved=order)
+    rng = np.random.default_rng(seed)
+    pos = rng.integers(-top, top, (len(sections), n)).astype(np.int32)
+    index = np.concatenate([np.arange(t - a, t) for a, t in zip(new, lengths)]) if n else np.zeros(0, int)
+    req = np.repeat(np.arange(len(new)), new)
+    c.device()
+
+    def dev(x):
+        return torch.empty_strided(x.shape, x.stride(), dtype=x.dtype, device="cuda").copy_(x)
+
+    dq = dev(q) if with_q else None
+    q_out = None if in_place or not with_q else torch.full((n, hq, dim), 9.0, dtype=dtype, device="cuda")
+    d_pos = torch.full((len(sections), n + pos_gap), 1 << 29, dtype=torch.int32, device="cuda")[:, :n]
+    d_pos.copy_(torch.from_numpy(pos))
+    kv.kv_rope_append_axes(c.layout, c.d_pool[0] if with_kv else None, c.batch(new), dq, dev(k) if with_kv else None,
+                           dev(v) if with_kv else None, torch.from_numpy(freqs).cuda(), axes, d_pos, q_out=q_out,
+                           interleaved=interleaved, inverse=inverse, magnitude=magnitude, k_scale=c.d_scales[0],
+                           v_scale=c.d_scales[1])
+    torch.cuda.synchronize()
+    # the axis of each pair, from the definition
+    if order:
+        left, want_axes = list(sections), []
+        while len(want_axes) < half:
+            for a in range(len(sections)):
+                if left[a]:
+                    want_axes.append(a)
+                    left[a] -= 1
+    else:
+        want_axes = [a for a, s in enumerate(sections) for _ in range(s)]
+    assert axes.tolist() == want_axes
+    at = pos[want_axes].T[:, None].reshape(n, 1, half)
+    u, tiny = ref.UNIT[dtype], 2.0 ** -24
+    if with_q:
+        want, err = stream_ref.turn(q, at, freqs, interleaved, magnitude, inverse)
+        ref.assert_within(dq if in_place else q_out, want, u * want.abs() * 1.001 + err + tiny, "q")
+    before = c.pool[0].clone()
+    c.pool[0] = c.d_pool[0].cpu()
+    old = ref.Cache.__new__(ref.Cache)
+    old.__dict__.update(c.__dict__)
+    old.pool = [before]
+    kw, kerr = stream_ref.turn(k, at, freqs, interleaved, magnitude, inverse)
+    for plane, x, e in ((0, kw, kerr), (1, v.double(), torch.zeros(v.shape).double())):
+        if c.scales is not None:
+            s = c.scales[plane].double()[None, :, None]
+            x, e = x / s, e / s + (x / s).abs() * 2.0 ** -22
+        got, was = (y.view(plane).view(torch.uint8) if c.elem == 1 else y.view(plane) for y in (c, old))
+        for i in range(n if with_kv else 0):
+            blk = c.bt[req[i], index[i] // block] if 0 <= index[i] and index[i] // block < c.bt.shape[1] else -1
+            if not 0 <= blk < c.num_blocks:
+                continue
+            y = got[int(blk), int(index[i]) % block]
+            y = (y.view(c.dtype) if c.elem == 1 else y).double()
+            w = x[i]
+            if c.elem == 1:
+                w = w.clamp(-ref.F8_MAX, ref.F8_MAX)
+                tol = w.abs() * 2.0 ** -4 + 2.0 ** -10 + e[i]
+            else:
+                tol = torch.zeros_like(w) if plane else u * w.abs() * 1.001 + e[i] + tiny
+            ref.assert_within(y, w, tol, f"plane {plane} row {i}")
+            got[int(blk), int(index[i]) % block] = was[int(blk), int(index[i]) % block]
+    assert torch.equal(c.pool[0].view(torch.uint8), before.view(torch.uint8)), "bytes beside the appended rows changed"
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("order", [False, True], ids=["sections", "in-turn"])
+@pytest.mark.parametrize("dim,sections", [(64, [8, 12, 12]), (64, [32]), (64, [1]), (64, [3, 0, 6]), (80, [12, 8]), (96, [1, 2, 3, 4]),
+                                          (128, [16, 24, 24]), (128, [24, 20, 20]), (8, [2, 2]), (72, [5, 5, 7]), (256, [40, 44, 41]),
+                                          (256, [16] * 8), (40, [3, 3, 3, 3])])
+def test_sections(dim, sections, order, interleaved):
+    _case([7, 1, 0, 20], [7, 30, 5, 45], sections, order, dim=dim, interleaved=interleaved, seed=dim + len(sections))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16], ids=["bf16", "f16"])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("sections", [[8, 12], [10, 16, 4]])
+def test_eight_bit_cache(dtype, interleaved, sections):
+    _case([9, 33], [50, 33], sections, True, dim=80, cache=F8, dtype=dtype, interleaved=interleaved, seed=3, magnitude=1.2,
+          layout="block_first", block=20)
+
+
+@pytest.mark.parametrize("kw", [dict(in_place=True), dict(inverse=True), dict(with_kv=False), dict(with_q=False), dict(pos_gap=5),
+                                dict(top=1 << 24), dict(gap=0, hq=1, heads=1)], ids=str)
+def test_forms(kw):
+    _case([9, 33], [50, 33], [8, 12, 12], dtype=torch.float16, seed=4, **kw)
+
+
+@pytest.mark.parametrize("rows", [1, 2049, 4099])
+@pytest.mark.parametrize("sections,interleaved", [([8, 12, 12], False), ([12, 8], True), ([9, 9], False)])
+def test_many_tokens(rows, sections, interleaved):
+    rng = np.random.default_rng(rows)
+    new = rng.multinomial(rows, np.ones(20) / 20)
+    _case(new.tolist(), (new + rng.integers(0, 30, 20)).tolist(), sections, True, hq=3, heads=1, interleaved=interleaved, seed=rows)
+
+
+def test_one_position_on_all_axes_is_kv_rope_append():
+    """Bit by bit; also text's positions far beyond what 32 bits resolve."""
+    for dtype, cache in ((torch.bfloat16, None), (torch.float16, F8)):
+        for rot, interleaved in ((64, False), (36, False), (40, True)):
+            c = ref.Cache([70, 90], heads=2, dim=64, dtype=cache or dtype, q_dtype=dtype, seed=rot)
+            q, k, v = (ref.rows_of(45, h, 64, dtype, c.gen).cuda() for h in (4, 2, 2))
+            freqs = torch.from_numpy(kv.kv_rope_frequencies(rot)[0]).cuda()
+            pos = torch.from_numpy(np.random.default_rng(1).integers(-1 << 31, 1 << 31, 45).astype(np.int32)).cuda()
+            got = []
+            for axes in (None, kv.kv_rope_axes([3, rot // 2 - 10, 7])):
+                c.device()
+                out = torch.empty_like(q)
+                call = kv.kv_rope_append if axes is None else kv.kv_rope_append_axes
+                more = (freqs,) if axes is None else (freqs, axes, pos.repeat(3, 1))
+                call(c.layout, c.d_pool[0], c.batch([12, 33]), q, k, v, *more, q_out=out, interleaved=interleaved, k_scale=c.d_scales[0],
+                     v_scale=c.d_scales[1], **({"positions": pos} if axes is None else {}))
+                got.append((out, c.d_pool[0].view(torch.uint8)))
+            torch.cuda.synchronize()
+            assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])
+
+
+def test_the_inverse_is_the_gradient():
+    """Of sum(w * rotated(q)) by q: the formula's, by autograd in 64 bits, and differences of that."""
+    freqs, axes = kv.kv_rope_frequencies(32)[0], kv.kv_rope_axes([6, 5, 5])
+    gen = torch.Generator().manual_seed(1)
+    q, w = (torch.randn(11, 3, 40, generator=gen).half() for _ in range(2))
+    pos = torch.randint(0, 900, (3, 11), generator=gen).int()
+    at = pos.numpy()[axes].T[:, None]
+    x = q.double().requires_grad_()
+
+    def total(y):
+        u = torch.from_numpy(at * freqs)
+        a, b = y[..., :16], y[..., 16:32]
+        z = torch.cat([a * u.cos() - b * u.sin(), a * u.sin() + b * u.cos(), y[..., 32:]], -1) * torch.tensor([1.5] * 32 + [1.0] * 8)
+        return (z * w.double()).sum()
+    total(x).backward()
+    h = 1e-4
+    for place in ((0, 0, 0), (3, 1, 20), (10, 2, 39)):
+        d = torch.zeros_like(x)
+        d[place] = h
+        assert math.isclose((total(x + d) - total(x - d)).item() / (2 * h), x.grad[place].item(), rel_tol=1e-7, abs_tol=1e-9)
+    c = ref.Cache([11], heads=3, dim=40, dtype=torch.float16).device()
+    out = torch.empty(11, 3, 40, dtype=torch.float16, device="cuda")
+    kv.kv_rope_append_axes(c.layout, None, c.batch([11]), w.cuda(), None, None, torch.from_numpy(freqs).cuda(), axes, pos.cuda(),
+                           q_out=out, inverse=True, magnitude=1.5)
+    err = (w.double()[..., :16].abs() + w.double()[..., 16:32].abs()) * 1.5 * 2.0 ** -20
+    tol = 2.0 ** -11 * x.grad.abs() * 1.001 + 2.0 ** -24
+    tol[..., :16] += err
+    tol[..., 16:32] += err
+    ref.assert_within(out, x.grad, tol, "gradient")
+
+
+def test_graph_replays():
+    c = ref.Cache([90, 40], heads=2, dim=64, seed=6).device()
+    b = c.batch([1, 30])
+    q, k, v = (ref.rows_of(31, h, 64, torch.bfloat16, c.gen).cuda() for h in (4, 2, 2))
+    freqs, axes = torch.from_numpy(kv.kv_rope_frequencies(64)[0]).cuda(), kv.kv_rope_axes([8, 12, 12])
+    pos = torch.zeros(3, 31, dtype=torch.int32, device="cuda")
+    out, g = torch.empty_like(q), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        kv.kv_rope_append_axes(c.layout, c.d_pool[0], b, q, k, v, freqs, axes, pos, q_out=out)
+    axes[:] = 0                                            # read during the call
+    start = c.d_pool[0].clone()
+    for x in range(3):
+        pos.random_(0, 1000, generator=torch.Generator("cuda").manual_seed(x))
+        kv.kv_rope_append_axes(c.layout, c.d_pool[0], b, q, k, v, freqs, kv.kv_rope_axes([8, 12, 12]), pos, q_out=out)
+        want = out.clone(), c.d_pool[0].clone()
+        out.zero_()
+        c.d_pool[0].copy_(start)
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want[0]) and torch.equal(c.d_pool[0], want[1]), x
