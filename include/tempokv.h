@@ -517,8 +517,8 @@ int kv_rope_append_axes(const kv_layout *layout, void *d_layer, const kv_batch *
  *   max_len   the largest d_len[r] as far as the host knows (launch shape only)
  *   flags     how pairs are formed and turned, as in kv_rope_append
  * Requests must not share blocks whose keys turn.  One launch.  Errors:
- * KV_EINVAL, KV_EALIGN, KV_ELIMIT (as kv_rope_append, and 2^31 workgroups or
- * more), KV_EHIP. */
+ * KV_EINVAL, KV_EALIGN, KV_ELIMIT (as kv_rope_append, and 2^23 or more of
+ * num_layers * num_reqs * ceil(kv_heads / 16)), KV_EHIP. */
 int kv_rope_shift(const kv_layout *layout, void *const *h_layer_ptrs, const int32_t *d_block_tables,
                   int32_t bt_stride, int32_t num_reqs, const int32_t *d_len, int32_t max_len, int32_t layers,
                   int32_t heads, const int32_t *d_shift, int64_t shift_stride, const double *d_freqs,

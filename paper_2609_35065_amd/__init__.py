@@ -868,7 +868,8 @@ def kv_rope_shift(layout: KvLayout, layers: Sequence, d_block_tables, d_len, max
         cache_dtype = next((t.dtype for t in layers if not isinstance(t, int) and t.is_floating_point()), None)
         if cache_dtype is None:
             raise ValueError("cache_dtype is needed for a cache of bytes")
-    for t in layers:
+    # one check for each type among the layers (the types by the C accessor: 32 layers take 2 us)
+    for t in {getattr(x, "dtype", None): x for x in layers}.values():
         code = _cache_code(cache_dtype, layout, KV_BF16, t)
     lp = _layer_array(layers)   # alive during the call
     _check(lib().kv_rope_shift(ct.addressof(layout), lp.buffer_info()[0],

@@ -13,6 +13,7 @@ namespace {
 constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr int kTokens = 64, kHeads = 16;       // of a workgroup's tile
 constexpr int kPairs = 8;                      // of a lane's unit
+constexpr int64_t kMaxBlocks = 1 << 23;        // of a launch, which may have 2^32 lanes
 
 struct ShiftParams {
     Paged cache;
@@ -23,9 +24,27 @@ struct ShiftParams {
     int32_t shift_layers, shift_heads;         // 1: one shift for all
     int32_t kv_heads, groups;                  // groups of kHeads heads
     int32_t half, units;                       // pairs of a row, and units
-    Divider by_heads;                          // of a full group
-    float sign;
+    int32_t tiles;                             // of a request's tokens: workgroups for each layer, request and group
+    Divider by_heads;                          // of a group that is not full
+    double sign;
 };
+
+// What a workgroup takes.  Tiles of one request are next to one another: they go to all XCDs in turn, where ragged
+// requests side by side left some of them idle.
+struct Place {
+    int l, r, head0;
+    int64_t tile;
+};
+
+__device__ __forceinline__ Place find_place(const ShiftParams &p) {
+    const uint32_t x = blockIdx.x / (uint32_t)p.tiles, lr = x / (uint32_t)p.groups;
+    Place y;
+    y.tile = blockIdx.x - x * p.tiles;
+    y.head0 = (int)(x - lr * p.groups) * kHeads;
+    y.l = (int)(lr / (uint32_t)p.cache.num_reqs);
+    y.r = (int)(lr - (uint32_t)y.l * p.cache.num_reqs);
+    return y;
+}
 
 // Elements at any alignment.
 typedef u32x4 __attribute__((aligned(1))) u32x4_any;
@@ -61,21 +80,21 @@ template <class T, bool F8, int N> struct Elements {
 #pragma unroll
         for (int i = 0; i < N; i += 2) {
             if constexpr (F8) {
-                const uint32_t y = i & 2 ? T::from_f8(raw[i / 4], true) : T::from_f8(raw[i / 4], false);
-                x[i] = T::to_f32(y & 0xffffu), x[i + 1] = T::to_f32(y >> 16);
+                const f32x2 y = i & 2 ? __builtin_amdgcn_cvt_pk_f32_fp8((int)raw[i / 4], true)
+                                      : __builtin_amdgcn_cvt_pk_f32_fp8((int)raw[i / 4], false);
+                x[i] = y[0], x[i + 1] = y[1];
             } else {
                 x[i] = T::to_f32(raw[i / 2] & 0xffffu), x[i + 1] = T::to_f32(raw[i / 2] >> 16);
             }
         }
     }
-    // rounded once, to nearest even; in 8 bits values beyond 448 become 448, NaN stays
+    // rounded once, to nearest even; in 8 bits (saturating, see saturate_f8) values beyond 448 become 448, NaN stays
     __device__ __forceinline__ void set(const float (&x)[N]) {
         if constexpr (F8) {
-            const auto clamp = [](float y) { return y != y ? y : fminf(fmaxf(y, -448.0f), 448.0f); };
 #pragma unroll
             for (int i = 0; i < N; i += 4) {
-                const int y = __builtin_amdgcn_cvt_pk_fp8_f32(clamp(x[i]), clamp(x[i + 1]), 0, false);
-                raw[i / 4] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(clamp(x[i + 2]), clamp(x[i + 3]), y, true);
+                const int y = __builtin_amdgcn_cvt_pk_fp8_f32(x[i], x[i + 1], 0, false);
+                raw[i / 4] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x[i + 2], x[i + 3], y, true);
             }
         } else {
 #pragma unroll
@@ -83,6 +102,43 @@ template <class T, bool F8, int N> struct Elements {
         }
     }
 };
+
+// From here on the wave's conversions to 8 bits give the largest value, 448, for finite values beyond it (the mode
+// register's bit 23; infinities, which an 8-bit cache does not hold, would become NaN).  As a clamp, with NaN kept, it
+// would be three instructions an element.
+__device__ __forceinline__ void saturate_f8() { __builtin_amdgcn_s_setreg(1 | 23 << 6, 1); }
+
+// Sine and cosine of the angles s f_i, f in turns below 1/2 in size.  Added to 1.5 x 2^20 in 64 bits, a number of turns
+// leaves its fraction in the low 32 bits, in units of 2^-32: one operation for the product and the remainder, where the
+// turns stay below 2^19.  The sines of the unit are off by up to 1.3e-7 (2^-22.9) of their size-1 range.
+template <int N> __device__ __forceinline__ void sincos_turns(int s, const double (&f)[N], float (&c)[N], float (&si)[N]) {
+    float u[N];
+    if (__any((uint32_t)(s + (1 << 20)) >= 1u << 21)) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const double turns = s * f[i];
+            u[i] = (float)(turns - rint(turns));
+        }
+    } else {
+        const double x = s;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const double y = __builtin_fma(x, f[i], 0x1.8p20);
+            u[i] = (float)(int32_t)__builtin_bit_cast(uint64_t, y) * 0x1p-32f;
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        c[i] = __builtin_amdgcn_cosf(u[i]);
+        si[i] = __builtin_amdgcn_sinf(u[i]);
+    }
+}
+
+// A frequency in turns a position, without its whole turns (a shift is a whole number), backwards if asked.
+__device__ __forceinline__ double to_turns(const ShiftParams &p, int pair) {
+    const double f = p.freqs[pair] * 0.15915494309189533577;
+    return (f - rint(f)) * p.sign;
+}
 
 // One workgroup: a layer, a request, up to 16 heads and 64 tokens.  Where the
 // tokens lie and their shifts go to LDS first.  A lane takes eight pairs of a
@@ -95,10 +151,8 @@ __global__ __launch_bounds__(kThreads) void rope_shift_kernel(ShiftParams p) {
     __shared__ uint32_t where[kTokens];            // 16-byte units from the plane's start
     __shared__ int32_t by[kHeads][kTokens];        // 0: left as it is
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int group = (int)(blockIdx.x % p.groups);
-    const int64_t lr = blockIdx.x / p.groups;
-    const int r = (int)(lr % p.cache.num_reqs), l = (int)(lr / p.cache.num_reqs);
-    const int head0 = group * kHeads, heads = min(kHeads, p.kv_heads - head0);
+    const Place at0 = find_place(p);
+    const int r = at0.r, l = at0.l, head0 = at0.head0, heads = min(kHeads, p.kv_heads - head0);
     const int64_t len = min((int64_t)max(p.len[r], 0), p.shift_stride);
     const int32_t *shift = p.shift + ((int64_t)(p.shift_layers > 1 ? l : 0) * p.cache.num_reqs + r) * p.shift_heads * p.shift_stride;
     char *base = p.layers[l];
@@ -106,12 +160,13 @@ __global__ __launch_bounds__(kThreads) void rope_shift_kernel(ShiftParams p) {
     const int slot = lane / p.units, unit = lane - slot * p.units, rows = 64 / p.units;     // of a wave
     const bool on = slot < rows;
     const int pair0 = min(unit * kPairs, p.half - kPairs);
-    double f[kPairs];                              // turns a position
+    double f[kPairs];
 #pragma unroll
-    for (int i = 0; i < kPairs; ++i) f[i] = p.freqs[pair0 + i] * 0.15915494309189533577;
+    for (int i = 0; i < kPairs; ++i) f[i] = to_turns(p, pair0 + i);
+    if constexpr (F8) saturate_f8();
     const int first = (INTERLEAVED ? 2 * pair0 : pair0) * kElem, second = (p.half + pair0) * kElem;     // bytes
 
-    for (int64_t t0 = (int64_t)blockIdx.y * kTokens; t0 < len; t0 += (int64_t)gridDim.y * kTokens) {
+    for (int64_t t0 = at0.tile * kTokens; t0 < len; t0 += (int64_t)p.tiles * kTokens) {
         const int n = (int)min((int64_t)kTokens, len - t0);
         __syncthreads();                           // the tile before is done
         for (int x = tid; x < heads * kTokens; x += kThreads) {
@@ -145,18 +200,16 @@ __global__ __launch_bounds__(kThreads) void rope_shift_kernel(ShiftParams p) {
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) {
                 if (s[i] == 0) continue;
-                float xa[INTERLEAVED ? 16 : 8], xb[8];
+                float xa[INTERLEAVED ? 16 : 8], xb[8], c[kPairs], si[kPairs];
+                sincos_turns(s[i], f, c, si);
                 a[i].get(xa);
                 if constexpr (!INTERLEAVED) b[i].get(xb);
 #pragma unroll
                 for (int e = 0; e < kPairs; ++e) {
-                    const double turns = s[i] * f[e];
-                    const float u = (float)(turns - rint(turns));
-                    const float c = __builtin_amdgcn_cosf(u), si = __builtin_amdgcn_sinf(u) * p.sign;
                     float &ra = xa[INTERLEAVED ? 2 * e : e], &rb = INTERLEAVED ? xa[(2 * e + 1) % (INTERLEAVED ? 16 : 8)] : xb[e];
                     const float va = ra, vb = rb;
-                    ra = __builtin_fmaf(va, c, -vb * si);
-                    rb = __builtin_fmaf(va, si, vb * c);
+                    ra = __builtin_fmaf(va, c[e], -vb * si[e]);
+                    rb = __builtin_fmaf(va, si[e], vb * c[e]);
                 }
                 a[i].set(xa);
                 a[i].store(at[i] + first);
@@ -172,12 +225,13 @@ __global__ __launch_bounds__(kThreads) void rope_shift_kernel(ShiftParams p) {
 // Rows of fewer than eight pairs: a lane takes one.
 template <class T, bool F8, bool INTERLEAVED>
 __global__ __launch_bounds__(kThreads) void rope_shift_short_kernel(ShiftParams p) {
-    const int64_t lr = blockIdx.x / p.groups;
-    const int r = (int)(lr % p.cache.num_reqs), l = (int)(lr / p.cache.num_reqs), head0 = (int)(blockIdx.x % p.groups) * kHeads;
+    const Place at0 = find_place(p);
+    const int r = at0.r, l = at0.l, head0 = at0.head0;
+    if constexpr (F8) saturate_f8();
     const int heads = min(kHeads, p.kv_heads - head0), per_token = heads * p.half;
     const int64_t len = min((int64_t)max(p.len[r], 0), p.shift_stride);
     const int32_t *shift = p.shift + ((int64_t)(p.shift_layers > 1 ? l : 0) * p.cache.num_reqs + r) * p.shift_heads * p.shift_stride;
-    for (int64_t t0 = (int64_t)blockIdx.y * kTokens; t0 < len; t0 += (int64_t)gridDim.y * kTokens) {
+    for (int64_t t0 = at0.tile * kTokens; t0 < len; t0 += (int64_t)p.tiles * kTokens) {
         const int n = (int)min((int64_t)kTokens, len - t0);
         for (int x = threadIdx.x; x < n * per_token; x += kThreads) {
             const int t = x / per_token, y = x - t * per_token, h = y / p.half, i = y - h * p.half;
@@ -188,9 +242,9 @@ __global__ __launch_bounds__(kThreads) void rope_shift_short_kernel(ShiftParams 
             char *at = p.layers[l] + ((int64_t)((uint32_t)id * p.cache.block16 + row * p.cache.row16) << 4) +
                        (int64_t)(head0 + h) * p.cache.head_bytes;
             const int ia = INTERLEAVED ? 2 * i : i, ib = INTERLEAVED ? 2 * i + 1 : i + p.half;
-            const double turns = s * (p.freqs[i] * 0.15915494309189533577);
-            const float u = (float)(turns - rint(turns));
-            const float c = __builtin_amdgcn_cosf(u), si = __builtin_amdgcn_sinf(u) * p.sign;
+            const double f[1] = {to_turns(p, i)};
+            float c[1], si[1];
+            sincos_turns(s, f, c, si);
             Elements<T, F8, 4> one;
             float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
             float w[4];
@@ -201,8 +255,8 @@ __global__ __launch_bounds__(kThreads) void rope_shift_short_kernel(ShiftParams 
                 one.raw[1] = 0;
             }
             one.get(w);
-            v[0] = __builtin_fmaf(w[0], c, -w[1] * si);
-            v[1] = __builtin_fmaf(w[0], si, w[1] * c);
+            v[0] = __builtin_fmaf(w[0], c[0], -w[1] * si[0]);
+            v[1] = __builtin_fmaf(w[0], si[0], w[1] * c[0]);
             one.set(v);
             if constexpr (F8) {
                 ((uint8_t *)at)[ia] = (uint8_t)one.raw[0];
@@ -245,7 +299,8 @@ int kv_rope_shift(const kv_layout *layout, void *const *h_layer_ptrs, const int3
         p.layers[l] = (char *)h_layer_ptrs[l];
     }
     p.groups = (layout->kv_heads + tkv::kHeads - 1) / tkv::kHeads;
-    if (layout->kv_heads > tkv::kMaxHeads || (int64_t)layout->num_layers * num_reqs >= (int64_t(1) << 31) / p.groups) return KV_ELIMIT;
+    const int64_t places = (int64_t)layout->num_layers * num_reqs * p.groups;
+    if (layout->kv_heads > tkv::kMaxHeads || places >= tkv::kMaxBlocks) return KV_ELIMIT;
     if (num_reqs == 0 || shift_stride == 0 || rot_dim == 0) return KV_OK;
     kv_batch b = {};
     b.num_reqs = num_reqs;
@@ -262,16 +317,16 @@ int kv_rope_shift(const kv_layout *layout, void *const *h_layer_ptrs, const int3
     p.half = rot_dim / 2;
     p.units = (p.half + tkv::kPairs - 1) / tkv::kPairs;
     p.by_heads = tkv::make_divider((uint32_t)(layout->kv_heads % tkv::kHeads ? layout->kv_heads % tkv::kHeads : tkv::kHeads));
-    p.sign = (flags & KV_ROPE_INVERSE) ? -1.0f : 1.0f;
+    p.sign = (flags & KV_ROPE_INVERSE) ? -1.0 : 1.0;
     const bool small = p.half < tkv::kPairs, inter = flags & KV_ROPE_INTERLEAVED;
     auto kernel = cache_dtype == KV_F8E4M3 ? tkv::shift_kernel<tkv::Bf16, true>(inter, small)
                                            : (cache_dtype == KV_BF16 ? tkv::shift_kernel<tkv::Bf16, false>(inter, small)
                                                                      : tkv::shift_kernel<tkv::F16, false>(inter, small));
     int64_t tiles = ((int64_t)max_len + tkv::kTokens - 1) / tkv::kTokens;
-    tiles = tiles < 1 ? 1 : (tiles > 65535 ? 65535 : tiles);
+    const int64_t most = tkv::kMaxBlocks / places;
+    p.tiles = (int32_t)(tiles < 1 ? 1 : (tiles > most ? most : tiles));
     (void)hipGetLastError();
-    hipLaunchKernelGGL(kernel, dim3((unsigned)((int64_t)layout->num_layers * num_reqs * p.groups), (unsigned)tiles),
-                       dim3(tkv::kThreads), 0, (hipStream_t)stream, p);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(places * p.tiles)), dim3(tkv::kThreads), 0, (hipStream_t)stream, p);
     return hipGetLastError() == hipSuccess ? KV_OK : KV_EHIP;
 }
 
