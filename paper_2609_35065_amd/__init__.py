@@ -510,7 +510,7 @@ def kv_ttr_state_aware(objs, obj_bytes, resident, queued, ready_at, now_s: float
 def _layer_array(layers: Sequence) -> array:
     """The layers' device pointers (array of 64-bit words, passed by address)."""
     tensor = _torch().Tensor
-    if all(type(t) is tensor for t in layers) and all(map(tensor.is_cuda.__get__, layers)) \
+    if set(map(type, layers)) == {tensor} and all(map(tensor.is_cuda.__get__, layers)) \
             and all(map(tensor.is_contiguous, layers)):
         return array("Q", map(tensor.data_ptr, layers))
     # (an address may come as a signed number, as in ctypes' own arrays of pointers)
@@ -751,11 +751,14 @@ def _cache_code(cache_dtype, layout: KvLayout, dtype: int, layer) -> int:
         code = _dtypes().get(cache_dtype)
         if code is None:
             raise ValueError(f"the cache must be bfloat16, float16 or float8_e4m3fn, got {cache_dtype}")
-    held = getattr(layer, "dtype", None)
+    _check_held(getattr(layer, "dtype", None), code)
+    return code
+
+
+def _check_held(held, code: int) -> None:
     if held is not None and (_dtype_codes or _dtypes()).get(held) != code and held.is_floating_point:
         raise ValueError(f"the cache is a tensor of {held}, and would be read as "
                          f"{next(t for t, c in _dtypes().items() if c == code)}")
-    return code
 
 
 def _scale_ptr(t, layout: KvLayout, what: str):
@@ -864,13 +867,17 @@ def kv_rope_shift(layout: KvLayout, layers: Sequence, d_block_tables, d_len, max
         raise ValueError("block_tables must hold one row per request")
     if d_shift.dim() != 4 or d_shift.shape[1] != R:
         raise ValueError("shift must be [layers or 1, requests, heads or 1, n]")
+    if set(map(type, layers)) == {torch.Tensor}:
+        types = set(map(torch.Tensor.dtype.__get__, layers))
+    else:
+        types = {getattr(t, "dtype", None) for t in layers}
     if cache_dtype is None and layout.elem_bytes == 2:
-        cache_dtype = next((t.dtype for t in layers if not isinstance(t, int) and t.is_floating_point()), None)
+        cache_dtype = next((t for t in types if t is not None and t.is_floating_point), None)
         if cache_dtype is None:
             raise ValueError("cache_dtype is needed for a cache of bytes")
-    # one check for each type among the layers (the types by the C accessor: 32 layers take 2 us)
-    for t in {getattr(x, "dtype", None): x for x in layers}.values():
-        code = _cache_code(cache_dtype, layout, KV_BF16, t)
+    code = _cache_code(cache_dtype, layout, KV_BF16, None)
+    for held in types:
+        _check_held(held, code)
     lp = _layer_array(layers)   # alive during the call
     _check(lib().kv_rope_shift(ct.addressof(layout), lp.buffer_info()[0],
                                _dptr(d_block_tables, torch.int32, "block_tables"), max(1, d_block_tables.shape[1]), R,

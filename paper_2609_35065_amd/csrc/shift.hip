@@ -11,7 +11,12 @@ namespace tkv {
 namespace {
 
 constexpr int kThreads = 256, kWaves = kThreads / 64;
-constexpr int kTokens = 64, kHeads = 16;       // of a workgroup's tile
+constexpr int kHeads = 16;                     // of a workgroup's tile
+// Tokens of a tile, and units that a lane has on their way.  Small tiles keep what all workgroups move at a time spread
+// evenly: 32 layers of 8 x 2,048 tokens in 16 bits take 376 us with 16, 390 with 32, 408 with 64; 8-bit rows, whose
+// angles cost as much for half the bytes, amortise a start over 32 (207 us; 214 with 16, 210 with 64).
+template <bool F8> constexpr int kTokens = F8 ? 32 : 16;
+template <bool F8> constexpr int kAhead = F8 ? 2 : 4;
 constexpr int kPairs = 8;                      // of a lane's unit
 constexpr int64_t kMaxBlocks = 1 << 23;        // of a launch, which may have 2^32 lanes
 
@@ -56,12 +61,12 @@ template <class T, bool F8, int N> struct Elements {
     __device__ __forceinline__ void load(const char *at) {
         constexpr int kWords = F8 ? N / 4 : N / 2;
         if constexpr (kWords == 2) {
-            const u32x2 x = *(const u32x2_any *)at;
+            const u32x2 x = __builtin_nontemporal_load((const u32x2_any *)at);
             raw[0] = x[0], raw[1] = x[1];
         } else {
 #pragma unroll
             for (int i = 0; i < kWords; i += 4) {
-                const u32x4 x = *(const u32x4_any *)(at + i * 4);
+                const u32x4 x = __builtin_nontemporal_load((const u32x4_any *)(at + i * 4));
 #pragma unroll
                 for (int e = 0; e < 4; ++e) raw[i + e] = x[e];
             }
@@ -70,10 +75,11 @@ template <class T, bool F8, int N> struct Elements {
     __device__ __forceinline__ void store(char *at) const {
         constexpr int kWords = F8 ? N / 4 : N / 2;
         if constexpr (kWords == 2) {
-            *(u32x2_any *)at = u32x2{raw[0], raw[1]};
+            __builtin_nontemporal_store(u32x2{raw[0], raw[1]}, (u32x2_any *)at);
         } else {
 #pragma unroll
-            for (int i = 0; i < kWords; i += 4) *(u32x4_any *)(at + i * 4) = u32x4{raw[i], raw[i + 1], raw[i + 2], raw[i + 3]};
+            for (int i = 0; i < kWords; i += 4)
+                __builtin_nontemporal_store(u32x4{raw[i], raw[i + 1], raw[i + 2], raw[i + 3]}, (u32x4_any *)(at + i * 4));
         }
     }
     __device__ __forceinline__ void get(float (&x)[N]) const {
@@ -140,16 +146,16 @@ __device__ __forceinline__ double to_turns(const ShiftParams &p, int pair) {
     return (f - rint(f)) * p.sign;
 }
 
-// One workgroup: a layer, a request, up to 16 heads and 64 tokens.  Where the
+// One workgroup: a layer, a request, up to 16 heads and a tile of tokens.  Where the
 // tokens lie and their shifts go to LDS first.  A lane takes eight pairs of a
 // row, always the same ones, so that it holds their frequencies; a row's last
 // unit ends at its last pair and may overlap the one before.  A row lies in one
 // wave, which reads all of it before it writes.
 template <class T, bool F8, bool INTERLEAVED>
 __global__ __launch_bounds__(kThreads) void rope_shift_kernel(ShiftParams p) {
-    constexpr int kElem = F8 ? 1 : 2, kAhead = 4;
-    __shared__ uint32_t where[kTokens];            // 16-byte units from the plane's start
-    __shared__ int32_t by[kHeads][kTokens];        // 0: left as it is
+    constexpr int kElem = F8 ? 1 : 2, kTok = kTokens<F8>, kNext = kAhead<F8>;
+    __shared__ uint32_t where[kTok];            // 16-byte units from the plane's start
+    __shared__ int32_t by[kHeads][kTok];        // 0: left as it is
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const Place at0 = find_place(p);
     const int r = at0.r, l = at0.l, head0 = at0.head0, heads = min(kHeads, p.kv_heads - head0);
@@ -166,11 +172,11 @@ __global__ __launch_bounds__(kThreads) void rope_shift_kernel(ShiftParams p) {
     if constexpr (F8) saturate_f8();
     const int first = (INTERLEAVED ? 2 * pair0 : pair0) * kElem, second = (p.half + pair0) * kElem;     // bytes
 
-    for (int64_t t0 = at0.tile * kTokens; t0 < len; t0 += (int64_t)p.tiles * kTokens) {
-        const int n = (int)min((int64_t)kTokens, len - t0);
+    for (int64_t t0 = at0.tile * kTok; t0 < len; t0 += (int64_t)p.tiles * kTok) {
+        const int n = (int)min((int64_t)kTok, len - t0);
         __syncthreads();                           // the tile before is done
-        for (int x = tid; x < heads * kTokens; x += kThreads) {
-            const int t = x % kTokens, h = x / kTokens;
+        for (int x = tid; x < heads * kTok; x += kThreads) {
+            const int t = x % kTok, h = x / kTok;
             uint32_t row = 0;
             const int32_t id = t < n ? block_of(p.cache, r, (uint32_t)(t0 + t), row) : -1;
             if (h == 0) where[t] = id < 0 ? 0u : (uint32_t)id * p.cache.block16 + row * p.cache.row16;
@@ -178,12 +184,12 @@ __global__ __launch_bounds__(kThreads) void rope_shift_kernel(ShiftParams p) {
         }
         __syncthreads();
         const int total = n * heads, step = kWaves * rows;
-        for (int x0 = wave * rows; x0 < total; x0 += kAhead * step) {
-            Elements<T, F8, INTERLEAVED ? 16 : 8> a[kAhead], b[kAhead];
-            int s[kAhead];
-            char *at[kAhead];
+        for (int x0 = wave * rows; x0 < total; x0 += kNext * step) {
+            Elements<T, F8, INTERLEAVED ? 16 : 8> a[kNext], b[kNext];
+            int s[kNext];
+            char *at[kNext];
 #pragma unroll
-            for (int i = 0; i < kAhead; ++i) {
+            for (int i = 0; i < kNext; ++i) {
                 const int x = x0 + i * step + slot;
                 s[i] = 0;
                 if (!on || x >= total) continue;
@@ -198,7 +204,7 @@ __global__ __launch_bounds__(kThreads) void rope_shift_kernel(ShiftParams p) {
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             __builtin_amdgcn_wave_barrier();
 #pragma unroll
-            for (int i = 0; i < kAhead; ++i) {
+            for (int i = 0; i < kNext; ++i) {
                 if (s[i] == 0) continue;
                 float xa[INTERLEAVED ? 16 : 8], xb[8], c[kPairs], si[kPairs];
                 sincos_turns(s[i], f, c, si);
@@ -231,8 +237,8 @@ __global__ __launch_bounds__(kThreads) void rope_shift_short_kernel(ShiftParams 
     const int heads = min(kHeads, p.kv_heads - head0), per_token = heads * p.half;
     const int64_t len = min((int64_t)max(p.len[r], 0), p.shift_stride);
     const int32_t *shift = p.shift + ((int64_t)(p.shift_layers > 1 ? l : 0) * p.cache.num_reqs + r) * p.shift_heads * p.shift_stride;
-    for (int64_t t0 = at0.tile * kTokens; t0 < len; t0 += (int64_t)p.tiles * kTokens) {
-        const int n = (int)min((int64_t)kTokens, len - t0);
+    for (int64_t t0 = at0.tile * kTokens<F8>; t0 < len; t0 += (int64_t)p.tiles * kTokens<F8>) {
+        const int n = (int)min((int64_t)kTokens<F8>, len - t0);
         for (int x = threadIdx.x; x < n * per_token; x += kThreads) {
             const int t = x / per_token, y = x - t * per_token, h = y / p.half, i = y - h * p.half;
             uint32_t row = 0;
@@ -322,7 +328,8 @@ int kv_rope_shift(const kv_layout *layout, void *const *h_layer_ptrs, const int3
     auto kernel = cache_dtype == KV_F8E4M3 ? tkv::shift_kernel<tkv::Bf16, true>(inter, small)
                                            : (cache_dtype == KV_BF16 ? tkv::shift_kernel<tkv::Bf16, false>(inter, small)
                                                                      : tkv::shift_kernel<tkv::F16, false>(inter, small));
-    int64_t tiles = ((int64_t)max_len + tkv::kTokens - 1) / tkv::kTokens;
+    const int tokens = cache_dtype == KV_F8E4M3 ? tkv::kTokens<true> : tkv::kTokens<false>;
+    const int64_t tiles = ((int64_t)max_len + tokens - 1) / tokens;
     const int64_t most = tkv::kMaxBlocks / places;
     p.tiles = (int32_t)(tiles < 1 ? 1 : (tiles > most ? most : tiles));
     (void)hipGetLastError();
