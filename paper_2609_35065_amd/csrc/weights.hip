@@ -32,6 +32,7 @@ struct WeightParams {
     int32_t q_heads, kv_heads, group, head_dim;
     int32_t window, sink;
     bool causal;
+    bool steady;               // 64 rows are whole tokens, and 128 span less than 2^30 bytes: every step lies alike
     float *sums;               // [num_reqs * kv_heads][sink_tiles][parts][64], where a sink's rows are cut into parts
     int32_t sink_tiles, parts;
 };
@@ -119,15 +120,36 @@ __device__ __forceinline__ float weigh_tile(const WeightParams &p, const Span &s
     u32x4 qreg[VL];
     float base = 0.0f;
     int lo = 0, hi = 0;
-    const auto load = [&](int row0) {
+    // where this lane's vectors of a step lie behind the step's first token (which tokens start: see `steady`)
+    uint32_t off[VL];
 #pragma unroll
-        for (int i = 0; i < VL; ++i) {
-            const int x = i * kThreads + tid, vec = x % VPR;
-            const int row = row0 + x / VPR;
-            qreg[i] = u32x4{0, 0, 0, 0};
-            if (row < row_end && vec * 8 < p.head_dim) {
-                const int token = (int)divide(row, p.by_group), head = h * p.group + row - token * p.group;
-                qreg[i] = *(const u32x4 *)(p.q + (first + token) * p.q_ts + head * p.q_hs + vec * 16);
+    for (int i = 0; i < VL; ++i) {
+        const int x = i * kThreads + tid, row = x / VPR, token = (int)divide(row, p.by_group);
+        off[i] = (uint32_t)(token * (int)p.q_ts + (row - token * p.group) * (int)p.q_hs + x % VPR * 16);
+    }
+    const auto load = [&](int row0) {
+        if (p.steady && row0 + kRows <= row_end) {
+            const char *at = p.q + (first + divide((uint32_t)row0, p.by_group)) * p.q_ts + (int64_t)h * p.group * p.q_hs;
+            if (p.head_dim == DP) {
+#pragma unroll
+                for (int i = 0; i < VL; ++i) qreg[i] = *(const u32x4 *)(at + off[i]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < VL; ++i) {
+                    qreg[i] = u32x4{0, 0, 0, 0};
+                    if ((i * kThreads + tid) % VPR * 8 < p.head_dim) qreg[i] = *(const u32x4 *)(at + off[i]);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < VL; ++i) {
+                const int x = i * kThreads + tid, vec = x % VPR;
+                const int row = row0 + x / VPR;
+                qreg[i] = u32x4{0, 0, 0, 0};
+                if (row < row_end && vec * 8 < p.head_dim) {
+                    const int token = (int)divide(row, p.by_group), head = h * p.group + row - token * p.group;
+                    qreg[i] = *(const u32x4 *)(p.q + (first + token) * p.q_ts + head * p.q_hs + vec * 16);
+                }
             }
         }
         if (tid < kRows) {
@@ -504,6 +526,7 @@ int attention_weights(const kv_layout *layout, const void *d_layer, const kv_bat
     p.head_dim = layout->head_dim;
     p.window = window < kMaxLength ? window : 0;
     p.causal = causal != 0;
+    p.steady = 64 % p.group == 0 && p.q_ts < (int64_t(1) << 22) && p.q_hs < (int64_t(1) << 22);
     p.sink = sink < kMaxLength ? sink : kMaxLength;
     p.sums = (float *)d_workspace;
     p.sink_tiles = plan.sink_tiles;
