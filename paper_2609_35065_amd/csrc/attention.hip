@@ -116,6 +116,9 @@ __device__ __forceinline__ Run find_run(int sink, int first) { return {sink, max
 __device__ __forceinline__ int key_at(const Run &x, int place) { return place + (place < x.sink ? 0 : x.gap); }
 __device__ __forceinline__ int place_of(const Run &x, int key) { return max(key - x.gap, min(key, x.sink)); }
 
+// Columns that few_rows takes for a head of up to `dim`: of an 8-bit cache whole vectors of 16 elements for all lanes.
+template <bool F8> constexpr int few_dim(int dim) { return F8 && dim == 96 ? 128 : dim; }
+
 // Bytes of LDS that a body needs.
 template <int DP, int W> constexpr int kSplitLds = W * 32 * (DP * 2 + 32);
 
@@ -724,7 +727,8 @@ __global__ __launch_bounds__(kThreads) void attention_few_kernel(AttentionParams
 // keys); a request with no more than 16 rows in all takes the other body.
 template <class T, bool F8, int DP, int W, bool SINK>
 __global__ __launch_bounds__(64 * W, DP > 128 ? 1 : 2) void attention_many_kernel(AttentionParams p) {
-    __shared__ __align__(16) char lds[kTileLds<DP> > kSplitLds<DP, W> ? kTileLds<DP> : kSplitLds<DP, W>];
+    constexpr int kFew = few_dim<F8>(DP);
+    __shared__ __align__(16) char lds[kTileLds<DP> > kSplitLds<kFew, W> ? kTileLds<DP> : kSplitLds<kFew, W>];
     __shared__ float part[W][16][2];
     __shared__ int odd;                        // some value that not all rows see is not finite
     __shared__ Places places[4];
@@ -732,7 +736,7 @@ __global__ __launch_bounds__(64 * W, DP > 128 ? 1 : 2) void attention_many_kerne
     const int h = (int)(id % p.kv_heads), split = (int)(id / p.kv_heads % p.splits);
     const Tile tile = find_tile<32 * W>(p.cache, (int)p.tiles - 1 - (int)(id / p.kv_heads / p.splits), p.group);
     if (tile.row0 >= tile.rows) return;
-    if (tile.rows <= kSplitRows) few_rows<T, F8, DP, W, SINK>(p, tile, h, split, lds, part, &odd);
+    if (tile.rows <= kSplitRows) few_rows<T, F8, kFew, W, SINK>(p, tile, h, split, lds, part, &odd);
     else many_rows<T, F8, DP, W, SINK>(p, tile, h, split, lds, &odd, places);
 }
 
@@ -808,7 +812,7 @@ __global__ __launch_bounds__(kThreads) void attention_join_kernel(AttentionParam
 }
 
 template <class T, bool F8, bool SINK, int DP> void (*attention_kernel_for(int rows))(AttentionParams) {
-    if (rows == kSplitRows) return attention_few_kernel<T, F8, DP, SINK>;
+    if (rows == kSplitRows) return attention_few_kernel<T, F8, few_dim<F8>(DP), SINK>;
     if constexpr (DP <= 128) {
         if (rows == kLargeRows) return attention_many_kernel<T, F8, DP, kLargeRows / 32, SINK>;
     }
@@ -817,9 +821,7 @@ template <class T, bool F8, bool SINK, int DP> void (*attention_kernel_for(int r
 
 template <class T, bool F8, bool SINK> auto attention_kernel(int rows, int head_dim) {
     if (head_dim <= 64) return attention_kernel_for<T, F8, SINK, 64>(rows);
-    if constexpr (!F8) {
-        if (head_dim <= 96) return attention_kernel_for<T, F8, SINK, 96>(rows);
-    }
+    if (head_dim <= 96) return attention_kernel_for<T, F8, SINK, 96>(rows);
     if (head_dim <= 128) return attention_kernel_for<T, F8, SINK, 128>(rows);
     return attention_kernel_for<T, F8, SINK, 256>(rows);
 }

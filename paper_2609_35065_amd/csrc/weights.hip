@@ -32,16 +32,9 @@ struct WeightParams {
     int32_t q_heads, kv_heads, group, head_dim;
     int32_t window, sink;
     bool causal;
-    bool steady;               // 64 rows are whole tokens, and 128 span less than 2^30 bytes: every step lies alike
+    bool steady;               // 64 rows are whole tokens, and 128 span less than 2^30 bytes
     float *sums;               // [num_reqs * kv_heads][sink_tiles][parts][64], where a sink's rows are cut into parts
     int32_t sink_tiles, parts;
-};
-
-// What a staged row is to its keys: those it sees, lo <= j < hi, and its
-// lse in units of log 2.
-struct __align__(16) RowInfo {
-    float base[32];
-    int lo[32], hi[32];
 };
 
 template <int DP> constexpr int kQueryRow = DP * 2 + 16;     // bytes of an LDS row: 8 rows on different banks
@@ -67,7 +60,7 @@ template <int DP, int KW> struct Shape {
 };
 template <int DP, int KW> struct __align__(16) TileLds {
     char rows[2][Shape<DP, KW>::kRows * kQueryRow<DP>];
-    RowInfo info[2][Shape<DP, KW>::RW * Shape<DP, KW>::RT];
+    float base[2][Shape<DP, KW>::kRows];       // lse in units of log 2, infinity for a row that adds nothing
     float parts[kWaves][kWaveKeys];
 };
 
@@ -89,15 +82,17 @@ __device__ __forceinline__ float weigh_tile(const WeightParams &p, const Span &s
     const int t0 = tile0 + kw * kWaveKeys;     // t0 + 63 may pass 2^31 - 1: no key is there
     // this lane's two keys, as operands; the element order follows the rows'
     u32x4 kf[2][KS];
-    bool there[2];
-    uint64_t all = ~uint64_t(0);
+    int from[2], to[2];
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
         const int64_t t = (int64_t)t0 + x * 32 + col;
         uint32_t row = 0;
         const int32_t blk = t < len ? block_of(p.cache, r, (uint32_t)t, row) : -1;
-        there[x] = blk >= 0;
-        all &= __ballot(there[x]);
+        // the rows that see the key, causal from its own token on and up to the one whose window ends at it
+        const int64_t tok = t - ahead;
+        from[x] = blk < 0 ? 0 : (p.causal ? (int)min((int64_t)span.ntok, max((int64_t)0, tok)) * p.group : 0);
+        to[x] = blk < 0 ? 0 : span.ntok * p.group;
+        if (p.window > 0 && !(SINK && t < p.sink)) to[x] = min(to[x], (int)min((int64_t)span.ntok, max((int64_t)0, tok + p.window)) * p.group);
         const char *at = p.cache.layer + (int64_t)h * p.cache.head_bytes +
                          ((int64_t)(blk < 0 ? 0u : (uint32_t)blk * p.cache.block16 + row * p.cache.row16) << 4);
         if constexpr (F8) {
@@ -119,25 +114,29 @@ __device__ __forceinline__ float weigh_tile(const WeightParams &p, const Span &s
     }
     u32x4 qreg[VL];
     float base = 0.0f;
-    int lo = 0, hi = 0;
-    // where this lane's vectors of a step lie behind the step's first token (which tokens start: see `steady`)
-    uint32_t off[VL];
+    // Where this lane's vectors of a step lie behind the step's first token.  Where each pass of the lanes takes whole
+    // rows and those are whole tokens, a pass lies as far behind the one before for all; else each has a place of its own.
+    constexpr bool kWholeRows = kThreads % VPR == 0;
+    constexpr int kOffsets = kWholeRows ? 1 : VL;
+    const bool steady = p.steady && (!kWholeRows || kThreads / VPR % p.group == 0);
+    const int64_t apart = kWholeRows ? (int64_t)divide(kThreads / VPR, p.by_group) * p.q_ts : 0;
+    uint32_t off[kOffsets];
 #pragma unroll
-    for (int i = 0; i < VL; ++i) {
+    for (int i = 0; i < kOffsets; ++i) {
         const int x = i * kThreads + tid, row = x / VPR, token = (int)divide(row, p.by_group);
         off[i] = (uint32_t)(token * (int)p.q_ts + (row - token * p.group) * (int)p.q_hs + x % VPR * 16);
     }
     const auto load = [&](int row0) {
-        if (p.steady && row0 + kRows <= row_end) {
+        if (steady && row0 + kRows <= row_end) {
             const char *at = p.q + (first + divide((uint32_t)row0, p.by_group)) * p.q_ts + (int64_t)h * p.group * p.q_hs;
             if (p.head_dim == DP) {
 #pragma unroll
-                for (int i = 0; i < VL; ++i) qreg[i] = *(const u32x4 *)(at + off[i]);
+                for (int i = 0; i < VL; ++i) qreg[i] = *(const u32x4 *)(at + i * apart + off[i % kOffsets]);
             } else {
 #pragma unroll
                 for (int i = 0; i < VL; ++i) {
                     qreg[i] = u32x4{0, 0, 0, 0};
-                    if ((i * kThreads + tid) % VPR * 8 < p.head_dim) qreg[i] = *(const u32x4 *)(at + off[i]);
+                    if ((i * kThreads + tid) % VPR * 8 < p.head_dim) qreg[i] = *(const u32x4 *)(at + i * apart + off[i % kOffsets]);
                 }
             }
         } else {
@@ -154,14 +153,9 @@ __device__ __forceinline__ float weigh_tile(const WeightParams &p, const Span &s
         }
         if (tid < kRows) {
             const int row = row0 + tid, token = (int)divide(row, p.by_group);
-            base = lo = hi = 0;
-            if (row < row_end) {
-                base = p.lse[(first + token) * p.q_heads + h * p.group + row - token * p.group];
-                const int64_t pos = ahead + token;
-                if (base != -INFINITY) hi = (int)max((int64_t)0, p.causal ? min(len, pos + 1) : len);
-                else base = 0.0f;
-                lo = (int)(p.window > 0 ? max((int64_t)0, pos - p.window + 1) : 0);
-            }
+            base = -INFINITY;
+            if (row < row_end) base = p.lse[(first + token) * p.q_heads + h * p.group + row - token * p.group];
+            base = base == -INFINITY ? INFINITY : base * kLog2e;
         }
     };
     const auto stage = [&](int buf) {
@@ -170,69 +164,98 @@ __device__ __forceinline__ float weigh_tile(const WeightParams &p, const Span &s
             const int x = i * kThreads + tid;
             *(u32x4 *)(lds.rows[buf] + x / VPR * kQueryRow<DP> + x % VPR * 16) = qreg[i];
         }
-        if (tid < kRows) {
-            lds.info[buf][tid / 32].base[tid % 32] = base * kLog2e;
-            lds.info[buf][tid / 32].lo[tid % 32] = lo;
-            lds.info[buf][tid / 32].hi[tid % 32] = hi;
+        if (tid < kRows) lds.base[buf][tid] = base;
+    };
+    // Of 32 rows the operands are read while the exponentials of the 32 before are taken, and their lse after that: from
+    // the next step's buffer too, which is filled, with the step's one barrier, between the products and exponentials of
+    // its last rows.
+    u32x4 qf[KS];
+    f32x4 b[4];
+    float mark = 0.0f;                             // lse of row col: a row of infinity adds nothing
+    const auto read = [&](int buf, int at) {
+        const char *from = lds.rows[buf] + (at + col) * kQueryRow<DP>;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            const int d = F8 ? (ks / 2) * 32 + half * 16 + (ks & 1) * 8 : ks * 16 + half * 8;
+            qf[ks] = *(const u32x4 *)(from + d * 2);
         }
     };
+    const auto read_lse = [&](int buf, int at) {
+#pragma unroll
+        for (int g = 0; g < 4; ++g) b[g] = *(const f32x4 *)&lds.base[buf][at + g * 8 + half * 4];
+        mark = lds.base[buf][at + col];
+    };
+    const auto below = [](int n) { return n >= 32 ? ~0u : (1u << max(n, 0)) - 1; };
     float sum[2] = {0.0f, 0.0f};
-    if (row_begin < row_end) load(row_begin);
+    f32x16 s[2];
+    const auto products = [&]() {
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) s[x][e] = 0.0f;
+        __builtin_amdgcn_sched_barrier(0);         // all reads are on their way before the first product waits
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            s[0] = T::mfma32(qf[ks], kf[0][ks], s[0]);
+            s[1] = T::mfma32(qf[ks], kf[1][ks], s[1]);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    const auto exponentials = [&](int row0) {
+        __builtin_amdgcn_sched_barrier(0);
+        // which of the rows the lane's keys see
+        const uint32_t add = (uint32_t)__ballot(mark != INFINITY);
+        uint32_t bits[2];
+#pragma unroll
+        for (int x = 0; x < 2; ++x) bits[x] = below(to[x] - row0) & ~below(from[x] - row0) & add;
+        float part[2] = {0.0f, 0.0f};              // of these rows, so that long sums stay exact
+        if (__all((bits[0] & bits[1]) == ~0u)) {
+#pragma unroll
+            for (int g = 0; g < 16; ++g)
+#pragma unroll
+                for (int x = 0; x < 2; ++x) part[x] += exp2_(__builtin_fmaf(s[x][g], c, -b[g / 4][g % 4]));
+        } else if (__any((bits[0] | bits[1]) != 0u)) {
+            bits[0] >>= 4 * half;                  // element g has bit 8 (g / 4) + g % 4
+            bits[1] >>= 4 * half;
+#pragma unroll
+            for (int g = 0; g < 16; ++g)
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    const float v = exp2_(__builtin_fmaf(s[x][g], c, -b[g / 4][g % 4]));
+                    const uint32_t on = (uint32_t)((int)(bits[x] << (31 - (8 * (g / 4) + g % 4))) >> 31);
+                    part[x] += __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, v) & on);
+                }
+        }
+        sum[0] += part[0];
+        sum[1] += part[1];
+    };
+    const int mine = rw * RT * 32;
+    if (row_begin < row_end) {
+        load(row_begin);
+        stage(0);
+        __syncthreads();
+        if (row_begin + kRows < row_end) load(row_begin + kRows);
+        read(0, mine);
+        read_lse(0, mine);
+    }
     int buf = 0;
     for (int row0 = row_begin; row0 < row_end; row0 += kRows, buf ^= 1) {
-        stage(buf);
-        __syncthreads();
-        if (row0 + kRows < row_end) load(row0 + kRows);
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
-            const int rg = rw * RT + rt;
-            if (row0 + rg * 32 >= row_end) continue;
-            const char *at = lds.rows[buf] + (rg * 32 + col) * kQueryRow<DP>;
-            const RowInfo &y = lds.info[buf][rg];
-            u32x4 qf[KS];
-            f32x4 b[4];
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks) {
-                const int d = F8 ? (ks / 2) * 32 + half * 16 + (ks & 1) * 8 : ks * 16 + half * 8;
-                qf[ks] = *(const u32x4 *)(at + d * 2);
-            }
-#pragma unroll
-            for (int g = 0; g < 4; ++g) b[g] = *(const f32x4 *)&y.base[g * 8 + half * 4];
-            // whether every row sees every key of the wave
-            const bool whole = __all((y.lo[col] <= t0 || (SINK && t0 + kWaveKeys <= p.sink)) && y.hi[col] >= t0 + kWaveKeys) && all == ~uint64_t(0);
-            __builtin_amdgcn_sched_barrier(0);     // all reads are on their way before the first product waits
-            f32x16 s[2];
-#pragma unroll
-            for (int x = 0; x < 2; ++x)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) s[x][e] = 0.0f;
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks) {
-                s[0] = T::mfma32(qf[ks], kf[0][ks], s[0]);
-                s[1] = T::mfma32(qf[ks], kf[1][ks], s[1]);
-            }
-            float part[2] = {0.0f, 0.0f};          // of these rows, so that long sums stay exact
-            if (whole) {
-#pragma unroll
-                for (int g = 0; g < 16; ++g)
-#pragma unroll
-                    for (int x = 0; x < 2; ++x) part[x] += exp2_(__builtin_fmaf(s[x][g], c, -b[g / 4][g % 4]));
-            } else {
-#pragma unroll
-                for (int g = 0; g < 16; g += 4) {
-                    const i32x4 l = *(const i32x4 *)&y.lo[g * 2 + half * 4], u = *(const i32x4 *)&y.hi[g * 2 + half * 4];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-#pragma unroll
-                        for (int x = 0; x < 2; ++x) {
-                            const int t = t0 + x * 32 + col;
-                            const float v = exp2_(__builtin_fmaf(s[x][g + e], c, -b[g / 4][e]));
-                            part[x] += there[x] && (t >= l[e] || (SINK && t < p.sink)) && t < u[e] ? v : 0.0f;
-                        }
+            const int at = mine + rt * 32;
+            products();
+            int next = buf, next_at = at + 32;
+            if (rt + 1 == RT) {
+                next = buf ^ 1, next_at = mine;
+                if (row0 + kRows < row_end) {
+                    stage(next);
+                    __syncthreads();
+                    if (row0 + 2 * kRows < row_end) load(row0 + 2 * kRows);
                 }
             }
-            sum[0] += part[0];
-            sum[1] += part[1];
+            read(next, next_at);                   // (past the last step what an older one left, not used)
+            exponentials(row0 + at);
+            read_lse(next, next_at);
         }
     }
 #pragma unroll
