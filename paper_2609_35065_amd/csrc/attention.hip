@@ -10,6 +10,8 @@
 
 #include <math.h>
 
+#include <type_traits>
+
 #include "mfma.h"
 #include "paged.h"
 
@@ -407,6 +409,10 @@ template <int DP> constexpr int kKeyRow = DP * 2 + 16;     // bytes of an LDS ro
 template <int DP> constexpr int kValueRow = DP * 2 + (DP * 2 % 128 ? 0 : 64);   // of V: 4 rows, 64 bytes of each
 template <int DP> constexpr int kTileLds = 2 * kStep * (kKeyRow<DP> + kValueRow<DP>);
 
+// Steps that a tile's loads are ahead.  What is read once comes from memory, two steps away; where that takes too many
+// registers, one.
+template <bool F8, int DP, int W> constexpr int ahead_of = DP > 128 || (DP == 128 && !F8 && W == 4) ? 1 : 2;
+
 // Where a step's keys lie (16-byte units from a plane's start), and which of
 // them are in the cache.
 struct Places {
@@ -419,6 +425,7 @@ __device__ __forceinline__ void many_rows(const AttentionParams &p, const Tile &
                                           int *odd, Places *places) {
     constexpr int KS = DP / 16, DT = DP / 32, kThreads = 64 * W, kRows = 32 * W;
     constexpr int VEC = F8 ? 16 : 8, VPR = DP / VEC, kVecs = kStep * VPR, VL = (kVecs + kThreads - 1) / kThreads;
+    constexpr int kAhead = ahead_of<F8, DP, W>;
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), col = lane & 31, half = lane >> 5;
     char *const kbuf = lds, *const vbuf = lds + 2 * kStep * kKeyRow<DP>;
 
@@ -460,17 +467,17 @@ __device__ __forceinline__ void many_rows(const AttentionParams &p, const Tile &
     const char *kbase = p.cache.layer + (int64_t)h * p.cache.head_bytes;
     const char *vbase = kbase + p.cache.kv_stride;
 
-    uint64_t there = 0, there_next = 0;        // bit k: key k of the step is in the cache
+    uint64_t there = 0, there_next[kAhead];    // bit k: key k of the step is in the cache
     const auto is_mixed = [&](uint64_t there, int t0) {
         return there != ~uint64_t(0) || (t0 < tile_lo && !(SINK && t0 + kStep <= run.sink)) || t0 + kStep > tile_hi;
     };
     if (tid == 0) *odd = 0;
 
     // Staging.  One wave, in turn, looks up the keys of a step, a lane each, and leaves their places for all: the
-    // table's entries are asked for three steps ahead and looked at one step later.  One step ahead all load the
-    // vectors x = i kThreads + tid.
+    // table's entries are asked for kAhead + 2 steps ahead and looked at one step later.  kAhead steps ahead all load
+    // the vectors x = i kThreads + tid.
     const int32_t *const table = p.cache.bt + (int64_t)tile.req * p.cache.bt_stride;
-    u32x4 kreg[VL], vreg[VL];
+    u32x4 kregs[kAhead][VL], vregs[kAhead][VL];
     int32_t id = -1;
     uint32_t id_row = 0;
     const auto ask = [&](int step) {
@@ -485,9 +492,10 @@ __device__ __forceinline__ void many_rows(const AttentionParams &p, const Tile &
         places[step & 3].at[lane] = in ? (uint32_t)id * p.cache.block16 + id_row * p.cache.row16 : 0u;
         if (lane == 0) places[step & 3].there = mask;
     };
-    const auto load = [&](int step) {
+    const auto load = [&](int slot, int step) {
         const Places &from = places[step & 3];
-        there_next = uniform(from.there);
+        u32x4(&kreg)[VL] = kregs[slot], (&vreg)[VL] = vregs[slot];
+        there_next[slot] = uniform(from.there);
         uint32_t at[VL];
 #pragma unroll
         for (int i = 0; i < VL; ++i) at[i] = from.at[(i * kThreads + tid) / VPR % kStep];
@@ -502,8 +510,9 @@ __device__ __forceinline__ void many_rows(const AttentionParams &p, const Tile &
     };
     // A value that is not finite must reach only the rows that see its key: 0 times it is NaN.  In a step that some
     // row does not see whole, such values are staged as 0; below they are added to the results that do see them.
-    const auto stage = [&](int buf, int step) {
-        const bool mixed = is_mixed(there_next, begin + step * kStep);
+    const auto stage = [&](int buf, int slot, int step) {
+        u32x4(&kreg)[VL] = kregs[slot], (&vreg)[VL] = vregs[slot];
+        const bool mixed = is_mixed(there_next[slot], begin + step * kStep);
         if (p.head_dim < DP) {
 #pragma unroll
             for (int i = 0; i < VL; ++i)
@@ -540,21 +549,23 @@ __device__ __forceinline__ void many_rows(const AttentionParams &p, const Tile &
         for (int e = 0; e < 16; ++e) o[i][e] = 0.0f;
     float m = -INFINITY, base = 0.0f, l = 0.0f;
 
-    if (wave < 3) {
+    if (wave < kAhead + 2) {
         ask(step0 + wave);
         leave(step0 + wave);
     }
     __syncthreads();
-    if (step0 < step1) load(step0);
-    for (int step = step0; step < step1; ++step) {
-        const int buf = (step - step0) & 1, t0 = begin + step * kStep;
-        stage(buf, step);
-        there = there_next;
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i)
+        if (step0 + i < step1) load(i, step0 + i);
+    const auto take = [&](auto buf, int step) {
+        const int t0 = begin + step * kStep, slot = kAhead > 1 ? (int)buf : 0;
+        stage(buf, slot, step);
+        there = there_next[slot];
         __syncthreads();
-        if (step + 1 < step1) load(step + 1);
+        if (step + kAhead < step1) load(slot, step + kAhead);
         const int turn = (step - step0) % W;
-        if (wave == (turn + 2) % W && step > step0) leave(step + 2);
-        if (wave == (turn + 3) % W) ask(step + 3);
+        if (wave == (turn + kAhead + 1) % W && step > step0) leave(step + kAhead + 1);
+        if (wave == (turn + kAhead + 2) % W) ask(step + kAhead + 2);
 
         // S: the reads of K are ahead of the products, of the second half among those of the first
         f32x16 s[2];
@@ -647,6 +658,14 @@ __device__ __forceinline__ void many_rows(const AttentionParams &p, const Tile &
             if (kk < 3) exponentials(kk + 1);
         }
         l += (sums[0] + sums[1]) + (sums[2] + sums[3]);
+    };
+    if constexpr (kAhead > 1) {
+        for (int step = step0; step < step1; step += 2) {
+            take(std::integral_constant<int, 0>{}, step);
+            if (step + 1 < step1) take(std::integral_constant<int, 1>{}, step + 1);
+        }
+    } else {
+        for (int step = step0; step < step1; ++step) take((step - step0) & 1, step);
     }
     const f32x2 ls = both_halves(l);
     l = ls[0] + ls[1];
