@@ -137,6 +137,12 @@ int plan_weights(const kv_layout *lo, const kv_batch *b, int32_t q_heads, int32_
     int64_t span = b->max_kv_len;
     if (plan->windowed && span > (int64_t)window + b->max_q_len) span = (int64_t)window + b->max_q_len;
     plan->keys = !plan->few && heads * ((span + 255) / 256) < 512 ? 64 : 256;
+    // With a window, 128 in between: where the requests' mean gives five workgroups for two compute units (4 x 2,000 tokens
+    // over 6,000, a window of 1,024: 127 us, 138 with 64 keys and 168 with 256; one of 4,096 over 8,192: 112 against 80).
+    if (plan->windowed && plan->keys == 64 && heads > 0) {
+        const int64_t mean = (int64_t)window + b->num_q / b->num_reqs;
+        if (heads * ((mean < span ? mean : span) / 128) >= 640) plan->keys = 128;
+    }
     plan->sink_tiles = plan->parts = 0;
     if (plan->windowed && !plan->few) {
         // A sink's rows are all of a chunk's, a key's those of a window: as many parts as that is longer.  (Sums of
@@ -151,6 +157,9 @@ int plan_weights(const kv_layout *lo, const kv_batch *b, int32_t q_heads, int32_
     if (plan->windowed && plan->few) span += sink;
     if (span > b->max_kv_len) span = b->max_kv_len;
     int64_t tiles = (span + plan->keys - 1) / plan->keys;
+    // Few rows: a workgroup for each slot of the chip's, two on a compute unit, whose waves then pass tile after tile (64
+    // requests of 2,052 visible tokens: 63 us, 64 and 75 with 3 and 8 times as many).
+    if (plan->few && heads > 0 && tiles > 512 / heads) tiles = 512 / heads;
     plan->tiles = tiles < 1 ? 1 : (tiles > 32768 ? 32768 : tiles);
     return KV_OK;
 }

@@ -56,7 +56,7 @@ __device__ __forceinline__ Span find_span(const WeightParams &p, int r) {
 }
 
 template <int DP, int KW> struct Shape {
-    static constexpr int RW = kWaves / KW, RT = KW > 1 ? 2 : 1, kRows = 32 * RW * RT, kKeys = kWaveKeys * KW;
+    static constexpr int RW = kWaves / KW, RT = KW > 2 ? 2 : 1, kRows = 32 * RW * RT, kKeys = kWaveKeys * KW;
 };
 template <int DP, int KW> struct __align__(16) TileLds {
     char rows[2][Shape<DP, KW>::kRows * kQueryRow<DP>];
@@ -377,15 +377,16 @@ __global__ __launch_bounds__(64) void sink_weights_join_kernel(WeightParams p) {
 }
 
 // Few rows (a decoded token's heads): nothing to share, so that each wave works
-// alone on 64 keys, 16 rows at a time, and all its loads are on their way at
-// once.  A lane has one key (lane % 16) and 4 of 16 rows.  Bound by the reads of
-// K: 64 requests of 4,096 tokens, 8 KV heads of 128, 0.54 GB in 123 us (4.5
-// TB/s).  Keys loaded as half cache lines, without the exchange of columns,
-// take 31 against 28.7 us for 32 requests of 4,000 at head size 64, 48 against
-// 42 us at 80 and 96, 124.8 us where 128 takes 125.4.
+// alone on 64 keys, 16 rows at a time, with the next 64 on their way (where two
+// sets of them fit the registers) and their places looked up.  A lane has one
+// key (lane % 16) and 4 of 16 rows.  Bound by the reads of K: the last 2,048 and
+// first 4 tokens of 64 requests, 8 KV heads of 128, 0.28 GB in 63 us (4.4 TB/s;
+// 8 bits 32 us), where one tile a wave, none ahead, takes 68 (48).  Heads of one
+// block on one XCD, or more workgroups, are no faster.
 template <class T, bool F8, int DP, bool SINK>
-__global__ __launch_bounds__(kThreads) void attention_weights_few_kernel(WeightParams p) {
+__global__ __launch_bounds__(kThreads, DP > 128 ? 1 : 2) void attention_weights_few_kernel(WeightParams p) {
     constexpr int KS = DP / 32, LD = F8 ? KS / 2 : KS, KT = kWaveKeys / 16;
+    constexpr int kSets = LD <= 4 ? 2 : 1;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, quad = lane >> 4;
     const int h = (int)(blockIdx.x % p.kv_heads), r = (int)(blockIdx.x / p.kv_heads);
     const Span span = find_span(p, r);
@@ -396,53 +397,62 @@ __global__ __launch_bounds__(kThreads) void attention_weights_few_kernel(WeightP
 
     // with a window, tiles of places: the sinks and, next to them, the keys from `start` on
     const SinkKeys keys = SINK ? find_keys(p, span) : SinkKeys{0, 0};
-    const int64_t places = len - (keys.start - keys.sink);
+    const int places = (int)(len - (keys.start - keys.sink)), gap = (int)(keys.start - keys.sink);
     if constexpr (SINK) fade(p, out, keys, (int64_t)blockIdx.y * kThreads + threadIdx.x, (int64_t)gridDim.y * kThreads);
-    const auto key_at = [&](int place) { return SINK && place >= keys.sink ? place + (int)(keys.start - keys.sink) : place; };
-    for (int64_t tile = (int64_t)blockIdx.y * kWaves + wave; tile * kWaveKeys < places; tile += (int64_t)gridDim.y * kWaves) {
-        const int t0 = (int)tile * kWaveKeys, key = key_at(t0 + lane);
-        uint32_t row = 0;
-        const int32_t blk = t0 + lane < places ? block_of(p.cache, r, (uint32_t)key, row) : -1;
-        const uint64_t there = __ballot(blk >= 0);
-        const uint32_t off = blk < 0 ? 0u : (uint32_t)blk * p.cache.block16 + row * p.cache.row16;
-        const float old = p.decay != 0.0f && t0 + lane < places ? out[key] : 0.0f;
-        u32x4 kf[KT][LD];
+    const auto key_at = [&](int place) { return SINK && place >= (int)keys.sink ? place + gap : place; };
+    // (places are at most 2^30 and the grid's tiles 2^17 apart: 32 bits)
+    const int stride = (int)gridDim.y * kWaves * kWaveKeys, start = ((int)blockIdx.y * kWaves + wave) * kWaveKeys;
+
+    // 16 rows: operands, and for this lane's four rows of the result what they see
+    u32x4 qf[KS];
+    float base[4];
+    int lo[4], hi[4];
+    const auto rows = [&](int row0) {
+        const int mine = min(row0 + col, nrows - 1), token = (int)divide(mine, p.by_group);
+        const char *qat = p.q + (first + token) * p.q_ts + (int64_t)(h * p.group + mine - token * p.group) * p.q_hs;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            const int d = F8 ? (ks / 2) * 64 + quad * 16 + (ks & 1) * 8 : ks * 32 + quad * 8;
+            qf[ks] = d < p.head_dim ? *(const u32x4 *)(qat + d * 2) : u32x4{0, 0, 0, 0};
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int rr = row0 + quad * 4 + i, tok = (int)divide(min(rr, nrows - 1), p.by_group);
+            const float lse = p.lse[(first + tok) * p.q_heads + h * p.group + min(rr, nrows - 1) - tok * p.group];
+            const int64_t pos = ahead + tok;
+            const bool on = rr < nrows && lse != -INFINITY;
+            base[i] = on ? lse * kLog2e : 0.0f;
+            hi[i] = on ? (int)max((int64_t)0, p.causal ? min(len, pos + 1) : len) : 0;
+            lo[i] = (int)(p.window > 0 ? max((int64_t)0, pos - p.window + 1) : 0);
+        }
+    };
+    int32_t id = -1;
+    uint32_t id_row = 0;
+    const auto look_up = [&](int t0) {
+        id = t0 < places - lane ? block_of(p.cache, r, (uint32_t)key_at(t0 + lane), id_row) : -1;
+    };
+    u32x4 sets[kSets][KT][LD];
+    uint64_t there[kSets];
+    float old[kSets];
+    const auto fetch = [&](int set, int t0) {
+        there[set] = __ballot(id >= 0);
+        const uint32_t off = id < 0 ? 0u : (uint32_t)id * p.cache.block16 + id_row * p.cache.row16;
+        old[set] = p.decay != 0.0f && t0 < places - lane ? out[key_at(t0 + lane)] : 0.0f;
 #pragma unroll
         for (int x = 0; x < KT; ++x)
-            load_rows(kf[x], p.cache.head_bytes, [&](int row) {
+            load_rows(sets[set][x], p.cache.head_bytes, [&](int row) {
                 return p.cache.layer + (int64_t)h * p.cache.head_bytes + ((int64_t)(uint32_t)__shfl((int)off, x * 16 + row) << 4);
             });
-        bool arranged = false;
+    };
+    const auto weigh = [&](int set, int t0) {
+        u32x4(&kf)[KT][LD] = sets[set];
+#pragma unroll
+        for (int x = 0; x < KT; ++x) arrange_rows(kf[x]);
         float sum[KT];
 #pragma unroll
         for (int x = 0; x < KT; ++x) sum[x] = 0.0f;
         for (int row0 = 0; row0 < nrows; row0 += 16) {
-            const int mine = min(row0 + col, nrows - 1), token = (int)divide(mine, p.by_group);
-            const char *qat = p.q + (first + token) * p.q_ts + (int64_t)(h * p.group + mine - token * p.group) * p.q_hs;
-            u32x4 qf[KS];
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks) {
-                const int d = F8 ? (ks / 2) * 64 + quad * 16 + (ks & 1) * 8 : ks * 32 + quad * 8;
-                qf[ks] = d < p.head_dim ? *(const u32x4 *)(qat + d * 2) : u32x4{0, 0, 0, 0};
-            }
-            // this lane's four rows of the result
-            float base[4];
-            int lo[4], hi[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int rr = row0 + quad * 4 + i, tok = (int)divide(min(rr, nrows - 1), p.by_group);
-                const float lse = p.lse[(first + tok) * p.q_heads + h * p.group + min(rr, nrows - 1) - tok * p.group];
-                const int64_t pos = ahead + tok;
-                const bool on = rr < nrows && lse != -INFINITY;
-                base[i] = on ? lse * kLog2e : 0.0f;
-                hi[i] = on ? (int)max((int64_t)0, p.causal ? min(len, pos + 1) : len) : 0;
-                lo[i] = (int)(p.window > 0 ? max((int64_t)0, pos - p.window + 1) : 0);
-            }
-            if (!arranged) {                   // here, so that the rows above are on their way with the keys
-#pragma unroll
-                for (int x = 0; x < KT; ++x) arrange_rows(kf[x]);
-                arranged = true;
-            }
+            if (nrows > 16) rows(row0);
 #pragma unroll
             for (int x = 0; x < KT; ++x) {
                 f32x4 s = {0, 0, 0, 0};
@@ -452,7 +462,7 @@ __global__ __launch_bounds__(kThreads) void attention_weights_few_kernel(WeightP
                     else s = T::mfma16(qf[ks], kf[x][ks], s);
                 }
                 const int t = key_at(t0 + x * 16 + col);
-                const bool in = (there >> (x * 16 + col)) & 1;
+                const bool in = (there[set] >> (x * 16 + col)) & 1;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const float v = exp2_(__builtin_fmaf(s[i], c, -base[i]));
@@ -469,7 +479,29 @@ __global__ __launch_bounds__(kThreads) void attention_weights_few_kernel(WeightP
             const f32x2 z = both_halves(y);
             got = quad == x ? z[0] + z[1] : got;
         }
-        if (t0 + lane < places) out[key] = p.decay == 0.0f ? got : __builtin_fmaf(p.decay, old, got);
+        if (t0 < places - lane) out[key_at(t0 + lane)] = p.decay == 0.0f ? got : __builtin_fmaf(p.decay, old[set], got);
+    };
+    look_up(start);
+    if (nrows > 0) rows(0);
+    if constexpr (kSets == 1) {
+        for (int t0 = start; t0 < places; t0 += stride) {
+            fetch(0, t0);
+            look_up(t0 + stride);
+            weigh(0, t0);
+        }
+    } else {
+        if (start < places) fetch(0, start);
+        look_up(start + stride);
+        for (int t0 = start; t0 < places; t0 += 2 * stride) {
+            const int t1 = t0 + stride;
+            if (t1 < places) fetch(1, t1);
+            look_up(t1 + stride);
+            weigh(0, t0);
+            if (t1 >= places) break;
+            if (t1 + stride < places) fetch(0, t1 + stride);
+            look_up(t1 + 2 * stride);
+            weigh(1, t1);
+        }
     }
 }
 
@@ -506,7 +538,8 @@ template <int KW, bool SINK> auto weights_kernel(bool bf16, bool f8, int d) {
 
 template <bool SINK> auto weights_kernel(const WeightPlan &plan, bool bf16, bool f8, int d) {
     return plan.few ? weights_few_kernel<SINK>(bf16, f8, d)
-                    : (plan.keys == 64 ? weights_kernel<1, SINK>(bf16, f8, d) : weights_kernel<4, SINK>(bf16, f8, d));
+                    : (plan.keys == 64 ? weights_kernel<1, SINK>(bf16, f8, d)
+                                       : (plan.keys == 128 ? weights_kernel<2, SINK>(bf16, f8, d) : weights_kernel<4, SINK>(bf16, f8, d)));
 }
 
 int attention_weights(const kv_layout *layout, const void *d_layer, const kv_batch *batch, const kv_rows *q,
