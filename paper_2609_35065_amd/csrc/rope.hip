@@ -13,6 +13,7 @@ namespace tkv {
 namespace {
 
 constexpr int kThreads = 256, kMaxTokens = 4;
+constexpr int64_t kStream = int64_t(1) << 27;          // bytes from which rows pass the caches by
 
 struct RopeParams {
     Paged cache;
@@ -67,11 +68,24 @@ __device__ __forceinline__ uint32_t pack4_f8(float a, float b, float c, float d)
 // A row lies in one wave, which reads all of it before it writes, so q may be
 // rotated in place.  A lane's first unit is loaded before the angles.
 // Bound by memory: 32,768 tokens of 32 + 2 x 8 heads of 128, 0.81 GB read and
-// written in 154 us (5.2 TB/s); ragged, head size 80, an 8-bit cache: 0.25 GB in
-// 53 us (4.6 TB/s).
+// written in 143 us (5.6 TB/s); ragged, head size 80, an 8-bit cache: 0.25 GB in
+// 54 us (4.6 TB/s).  STREAM passes the caches by, which a large batch's rows do
+// not fit: 143 against 157 us (0.2 GB at head size 256: 38.7 against 45; but 0.1
+// GB 21 against 19).  That is for units of whole cache lines (64 pairs of 16
+// bits); the narrow rows of the 8-bit batch take 69 us that way.
 enum Pairing { HALF, INTERLEAVED, ODD };
 
-template <bool BF16, bool F8, Pairing PAIR, bool AXES>
+template <bool STREAM, class V> __device__ __forceinline__ V read_row(const V *at) {
+    if constexpr (STREAM) return __builtin_nontemporal_load(at);
+    return *at;
+}
+
+template <bool STREAM, class V> __device__ __forceinline__ void write_row(V x, V *at) {
+    if constexpr (STREAM) __builtin_nontemporal_store(x, at);
+    else *at = x;
+}
+
+template <bool BF16, bool F8, Pairing PAIR, bool AXES, bool STREAM>
 __global__ __launch_bounds__(kThreads) void rope_append_kernel(RopeParams p) {
     extern __shared__ __align__(16) float trig[];                       // [per_block][half4] cos, then sin
     __shared__ int32_t where_index[kMaxTokens];
@@ -115,8 +129,8 @@ __global__ __launch_bounds__(kThreads) void rope_append_kernel(RopeParams p) {
     const auto fetch = [&](const Unit &u, u32x4 &a, u32x4 &b) {
         if (!u.on) return;
         const char *src = source(u);
-        a = *(const u32x4 *)(src + u.a * 16);
-        if (u.b >= 0) b = *(const u32x4 *)(src + u.b * 16);
+        a = read_row<STREAM>((const u32x4 *)(src + u.a * 16));
+        if (u.b >= 0) b = read_row<STREAM>((const u32x4 *)(src + u.b * 16));
     };
     u32x4 ra = {0, 0, 0, 0}, rb = {0, 0, 0, 0};
     Unit u = unit_of(start);
@@ -249,7 +263,7 @@ __global__ __launch_bounds__(kThreads) void rope_append_kernel(RopeParams p) {
                 } else {
                     const u32x4 z = {pack2<BF16>(y[0], y[1]), pack2<BF16>(y[2], y[3]), pack2<BF16>(y[4], y[5]),
                                      pack2<BF16>(y[6], y[7])};
-                    *(u32x4 *)(dst + vec * 16) = is_q || is_k ? z : (v ? rb : ra);
+                    write_row<STREAM>(is_q || is_k ? z : (v ? rb : ra), (u32x4 *)(dst + vec * 16));
                 }
             }
         }
@@ -259,15 +273,18 @@ __global__ __launch_bounds__(kThreads) void rope_append_kernel(RopeParams p) {
     }
 }
 
-template <bool BF16, bool F8, bool AXES> auto rope_kernel(Pairing pair) {
-    return pair == HALF ? rope_append_kernel<BF16, F8, HALF, AXES>
-                        : (pair == INTERLEAVED ? rope_append_kernel<BF16, F8, INTERLEAVED, AXES>
-                                               : rope_append_kernel<BF16, F8, ODD, AXES>);
+template <bool BF16, bool F8, bool AXES> void (*rope_kernel(Pairing pair, bool stream))(RopeParams) {
+    if constexpr (!F8) {
+        if (stream) return rope_append_kernel<BF16, F8, HALF, AXES, true>;
+    }
+    return pair == HALF ? rope_append_kernel<BF16, F8, HALF, AXES, false>
+                        : (pair == INTERLEAVED ? rope_append_kernel<BF16, F8, INTERLEAVED, AXES, false>
+                                               : rope_append_kernel<BF16, F8, ODD, AXES, false>);
 }
 
-template <bool AXES> auto rope_kernel(bool bf16, bool f8, Pairing pair) {
-    return bf16 ? (f8 ? rope_kernel<true, true, AXES>(pair) : rope_kernel<true, false, AXES>(pair))
-                : (f8 ? rope_kernel<false, true, AXES>(pair) : rope_kernel<false, false, AXES>(pair));
+template <bool AXES> auto rope_kernel(bool bf16, bool f8, Pairing pair, bool stream) {
+    return bf16 ? (f8 ? rope_kernel<true, true, AXES>(pair, stream) : rope_kernel<true, false, AXES>(pair, stream))
+                : (f8 ? rope_kernel<false, true, AXES>(pair, stream) : rope_kernel<false, false, AXES>(pair, stream));
 }
 
 // The append with one position a row (num_axes 0), or several and the axis of each pair.
@@ -332,14 +349,18 @@ int rope_append(const kv_layout *layout, void *d_layer, const kv_batch *batch, c
     p.by_row = make_divider((uint32_t)p.row_units);
     p.by_token = make_divider((uint32_t)p.token_units);
     p.by_half = make_divider((uint32_t)(p.half ? p.half : 1));
-    // Four tokens share a workgroup's start where there are workgroups enough; few tokens take one each.
-    const int64_t share = batch->num_q / 1024;
-    p.per_block = share < 1 ? 1 : (share > kMaxTokens ? kMaxTokens : (int)share);
+    const bool f8 = cache_dtype == KV_F8E4M3;
+    // Rows of a batch that pass the caches by; and four tokens (of those two) that share a workgroup's start where there
+    // are workgroups enough, while few tokens take one each.
+    const int64_t moved = batch->num_q * 4 * d * (p.q_heads + (k ? 2 * p.kv_heads : 0));      // bytes
+    const bool stream_rows = !f8 && pair == HALF && p.half > 0 && p.half % 64 == 0 && 2 * p.half == d && moved >= kStream;
+    const int64_t share = batch->num_q / 1024, most = stream_rows ? 2 : kMaxTokens;
+    p.per_block = share < 1 ? 1 : (share > most ? (int)most : (int)share);
     const int64_t blocks = (batch->num_q + p.per_block - 1) / p.per_block;
     if (blocks >= (int64_t(1) << 31)) return KV_ELIMIT;
     const size_t lds = (size_t)p.per_block * ((p.half + 3) & ~3) * 2 * sizeof(float);
-    const bool f8 = cache_dtype == KV_F8E4M3;
-    auto kernel = num_axes > 0 ? rope_kernel<true>(dtype == KV_BF16, f8, pair) : rope_kernel<false>(dtype == KV_BF16, f8, pair);
+    auto kernel = num_axes > 0 ? rope_kernel<true>(dtype == KV_BF16, f8, pair, stream_rows)
+                               : rope_kernel<false>(dtype == KV_BF16, f8, pair, stream_rows);
     (void)hipGetLastError();
     hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(kThreads), lds, (hipStream_t)stream, p);
     return hipGetLastError() == hipSuccess ? KV_OK : KV_EHIP;

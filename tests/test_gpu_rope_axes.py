@@ -187,3 +187,32 @@ def test_graph_replays():
         g.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, want[0]) and torch.equal(c.d_pool[0], want[1]), x
+
+
+@pytest.mark.parametrize("kw", [dict(), dict(in_place=True, dtype=torch.float16), dict(inverse=True, gap=0, magnitude=1.3)], ids=str)
+def test_batches_that_pass_the_caches_by(kw):
+    """128 MiB and more of whole cache lines are read and written another way."""
+    new = [1000, 1, 0, 1050]
+    assert sum(new) * 4 * 128 * (120 + 2 * 4) >= 1 << 27
+    _case(new, [1003, 30, 5, 1050], [16, 24, 24], hq=120, heads=4, dim=128, seed=9, **kw)
+
+
+def test_large_batches_of_one_axis():
+    """kv_rope_append takes the same ways: the results of its own on parts of the batch, and on the whole."""
+    c = ref.Cache([1100, 1000], heads=4, dim=128, seed=2).device()
+    n = 2060
+    q, k, v = (ref.rows_of(n, h, 128, torch.bfloat16, c.gen).cuda() for h in (120, 4, 4))
+    freqs = torch.from_numpy(kv.kv_rope_frequencies(128)[0]).cuda()
+    whole, start = torch.empty_like(q), c.d_pool[0].clone()
+    kv.kv_rope_append(c.layout, c.d_pool[0], c.batch([1090, 970]), q, k, v, freqs, q_out=whole)
+    want = c.d_pool[0].clone()
+    c.d_pool[0].copy_(start)
+    parts = torch.empty_like(q)
+    at = 0
+    for r, m in enumerate([1090, 970]):
+        off = torch.tensor([0, m], device="cuda")
+        b = kv.make_batch(off, c.d_len[r:r + 1].clone(), c.d_bt[r:r + 1].contiguous(), m, m, 1100)
+        kv.kv_rope_append(c.layout, c.d_pool[0], b, q[at:at + m], k[at:at + m], v[at:at + m], freqs, q_out=parts[at:at + m])
+        at += m
+    torch.cuda.synchronize()
+    assert torch.equal(whole, parts) and torch.equal(c.d_pool[0], want)

@@ -194,3 +194,12 @@ def test_served_cache_refuses():
         with pytest.raises(ValueError, match="positions"):
             s.begin([1, 1], positions=bad)
     assert s.lengths.tolist() == [100, 3] and s.positions.tolist() == [100, 3]
+
+
+def test_workspaces_of_no_requests():
+    none = _batch(num_q=0, num_reqs=0, d_q_off=0, d_kv_len=0, d_block_tables=0)
+    for hint in (0, 5000):
+        empty = _batch(num_q=0, num_reqs=0, max_q_len=hint, max_kv_len=hint, d_q_off=0, d_kv_len=0, d_block_tables=0)
+        for b in (none, empty):
+            assert kv.kv_sink_attention_workspace(_layout(), b, 4, 20, 4) == 0
+            assert kv.kv_sink_weights_workspace(_layout(), b, 4, 20, 4) == 0
