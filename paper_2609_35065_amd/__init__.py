@@ -835,7 +835,7 @@ def kv_rope_append_axes(layout: KvLayout, layer, batch: KvBatch, q, k, v, d_freq
     torch = _torch()
     n, half = batch.num_q, d_freqs.numel()
     rq, ro, rk, rv, code = _append_rows(n, layout.head_dim, q, q_out, k, v)
-    if axes.dtype != np.uint8 or axes.shape != (half,) or not axes.flags.c_contiguous:
+    if not isinstance(axes, np.ndarray) or axes.dtype != np.uint8 or axes.shape != (half,) or not axes.flags.c_contiguous:
         raise ValueError("axes must hold the axis of each pair, uint8")
     shape = positions.shape
     if len(shape) != 2 or shape[1] != n:

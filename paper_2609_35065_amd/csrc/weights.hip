@@ -55,12 +55,14 @@ __device__ __forceinline__ Span find_span(const WeightParams &p, int r) {
     return x;
 }
 
+constexpr uint32_t kNothing = 0xffc0deadu;     // a NaN that no lse is
+
 template <int DP, int KW> struct Shape {
     static constexpr int RW = kWaves / KW, RT = KW > 2 ? 2 : 1, kRows = 32 * RW * RT, kKeys = kWaveKeys * KW;
 };
 template <int DP, int KW> struct __align__(16) TileLds {
     char rows[2][Shape<DP, KW>::kRows * kQueryRow<DP>];
-    float base[2][Shape<DP, KW>::kRows];       // lse in units of log 2, infinity for a row that adds nothing
+    float base[2][Shape<DP, KW>::kRows];       // lse in units of log 2; kNothing for a row that adds nothing
     float parts[kWaves][kWaveKeys];
 };
 
@@ -155,7 +157,7 @@ __device__ __forceinline__ float weigh_tile(const WeightParams &p, const Span &s
             const int row = row0 + tid, token = (int)divide(row, p.by_group);
             base = -INFINITY;
             if (row < row_end) base = p.lse[(first + token) * p.q_heads + h * p.group + row - token * p.group];
-            base = base == -INFINITY ? INFINITY : base * kLog2e;
+            base = base == -INFINITY ? __builtin_bit_cast(float, kNothing) : (base != base ? NAN : base * kLog2e);
         }
     };
     const auto stage = [&](int buf) {
@@ -171,7 +173,7 @@ __device__ __forceinline__ float weigh_tile(const WeightParams &p, const Span &s
     // its last rows.
     u32x4 qf[KS];
     f32x4 b[4];
-    float mark = 0.0f;                             // lse of row col: a row of infinity adds nothing
+    float mark = 0.0f;                             // lse of row col
     const auto read = [&](int buf, int at) {
         const char *from = lds.rows[buf] + (at + col) * kQueryRow<DP>;
 #pragma unroll
@@ -204,7 +206,7 @@ __device__ __forceinline__ float weigh_tile(const WeightParams &p, const Span &s
     const auto exponentials = [&](int row0) {
         __builtin_amdgcn_sched_barrier(0);
         // which of the rows the lane's keys see
-        const uint32_t add = (uint32_t)__ballot(mark != INFINITY);
+        const uint32_t add = (uint32_t)__ballot(__builtin_bit_cast(uint32_t, mark) != kNothing);
         uint32_t bits[2];
 #pragma unroll
         for (int x = 0; x < 2; ++x) bits[x] = below(to[x] - row0) & ~below(from[x] - row0) & add;

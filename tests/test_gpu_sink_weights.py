@@ -204,3 +204,23 @@ def test_graph_replays():
         torch.cuda.synchronize()
         assert torch.equal(w, want), x
         kept = want
+
+
+@pytest.mark.parametrize("value", [math.inf, math.nan], ids=["inf", "nan"])
+def test_rows_whose_sum_is_not_finite(value):
+    """A row of infinite lse adds 0 to finite scores, one of NaN adds NaN to what it sees; with and without sinks."""
+    c = ref.Cache([300], heads=1, dim=64, seed=7).device()
+    for n in (2, 60):
+        q = ref.rows_of(n, 2, 64, torch.bfloat16, c.gen).contiguous()
+
+        def edit(lse):
+            lse[n // 2] = value
+        w, _ = _check(c, [n], q, 0.125, 30, 4, lse_edit=edit)
+        assert bool(w.isnan().any()) == math.isnan(value)
+        lse = ref.attention(c, [n], q, 0.125)[2].float()
+        edit(lse)
+        old = torch.rand(1, 1, 300, generator=c.gen)
+        plain = old.cuda()
+        kv.kv_attention_weights(c.layout, c.d_pool[0], c.batch([n]), q.cuda(), lse.cuda(), plain, 0.125)
+        want, tol = stream_ref.weights(c, [n], q, lse, 0.125, old, 1.0)
+        ref.assert_within(plain, want, tol, "weights")
