@@ -135,7 +135,8 @@ template <int DP, int W> constexpr int kSplitLds = W * 32 * (DP * 2 + 32);
 // in the loop and each keeps the next step's K and V on their way.
 // Bound by the reads of the cache: 64 requests of 4,096 tokens, 8 KV heads of
 // 128, 1.07 GB in 207 us (5.2 TB/s); 8 of 32,768 in 8 bits, 0.54 GB in 128 us
-// (4.2 TB/s).  P is rounded to the type of the products, as the matrix units
+// (4.2 TB/s); the last 4,096 and first 4 of 64 requests of 8,192, 1.08 GB in 205
+// us (5.3 TB/s).  P is rounded to the type of the products, as the matrix units
 // take it: relative to the running maximum, after its sum.  That adds 12 to 19 %
 // to the error of results that are rounded to bf16 alone (0.0017 to 0.0020 of
 // their size; chunks 0.0023).  Sums and statistics stay in 32 bits.
@@ -387,16 +388,21 @@ __device__ __forceinline__ void few_rows(const AttentionParams &p, const Tile &t
 }
 
 // Tiles of 32 rows a wave over steps of 64 keys.  K and V of a step go
-// through LDS for all waves, one step ahead: loaded into registers while
-// the step before is computed, written to the other buffer, one barrier.
+// through LDS for all waves: loaded into registers two steps ahead (or one),
+// written to the other buffer, one barrier a step.
 // Again S^T = K Q^T and O^T = V^T P^T, with 32 x 32 products: a lane holds
 // one row's scores for half of the keys, so that a row's maximum and sum need
 // one exchange between lanes.  Steps are bound by the issue of exponentials,
 // LDS reads and products beside one another: 8 chunks of 2,048 tokens over
-// 4,096, 32 heads on 8 of 128, 825 GFLOP in 848 to 897 us (920 to 973 TFLOP/s,
+// 4,096, 32 heads on 8 of 128, 825 GFLOP in 840 to 890 us (930 to 980 TFLOP/s,
 // by card), the matrix units busy for 43 % of the time, the vector units for 45 %;
 // head size 80 with a window of 1,024, ragged, 61 to 65 us (330 to 350 TFLOP/s of
-// what the rows see).
+// what the rows see).  Four prompts of 4,096 with a window of 1,024 and 4 sinks,
+// 241 GFLOP in 326 to 340 us (710 to 740): of a workgroup's 47 us 4 go before its
+// first step and 2 behind its last, and its 18 steps hold 1,152 keys, of which a
+// row sees 1,028.  The scores of the next step beside the exponentials of this
+// one take 3 % longer, 64 rows a wave (half of the LDS reads, one wave on a SIMD)
+// half as long again.
 //
 // The running maximum may lag: o and l are only scaled when some row's
 // maximum has grown by more than 2^kLag since it was last taken.  Until then

@@ -68,10 +68,11 @@ template <int DP, int KW> struct __align__(16) TileLds {
 
 // What the keys tile0 .. tile0 + 64 KW - 1 receive from rows row_begin .. row_end - 1: of key t0 + lane of the wave's
 // 64 keys, in the waves of the first group of rows.  The four waves take KW groups of 64 keys and 4 / KW groups of 32
-// rows at a time; the rows go through LDS, one step ahead, for all of them.  Chunks of 1,000 tokens over 4,000 in 4
-// requests, 32 heads on 8 of 128, 115 GFLOP in 168 to 176 us (650 to 680 TFLOP/s).  A wave's products and exponentials
-// take turns, with two waves on each SIMD to overlap them: the matrix units are busy for 27 % of the time, the vector
-// units for 44 %.  And all 512 workgroups run at once, those of the last quarter of the keys with half the rows.
+// rows at a time; the rows go through LDS, one step ahead, for all of them.  A wave's products and exponentials take
+// turns, with two waves on each SIMD to overlap them.  Chunks of 1,000 tokens over 4,000 in 4 requests, 32 heads on 8 of
+// 128, 115 GFLOP in 154 to 156 us (740 TFLOP/s); of 2,000 over 6,000 with a window of 1,024 and 4 sinks, 67 GFLOP in 127
+// to 130 us (520): the matrix units busy for 24 % of the time, the vector units for 41 %.  Products of the next rows
+// beside the exponentials of these, with two sets of accumulators, need more registers than two waves on a SIMD leave.
 template <class T, bool F8, int DP, int KW, bool SINK>
 __device__ __forceinline__ float weigh_tile(const WeightParams &p, const Span &span, int r, int h, int tile0, int row_begin,
                                             int row_end, TileLds<DP, KW> &lds) {
