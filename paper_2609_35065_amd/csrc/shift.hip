@@ -6,7 +6,7 @@
 // memory: 32 layers of 8 requests of 2,048 tokens, 8 KV heads of 128, 2.15 GB read
 // and written in 376 to 385 us (5.6 to 5.7 TB/s); in 8 bits, where each head's
 // tokens have shifts of their own, by the vector units too (60 % of the time): 0.93
-// GB in 204 to 209 us (4.5 TB/s).
+// GB in 204 to 211 us (4.5 TB/s).
 
 #include "mfma.h"
 #include "paged.h"
@@ -59,31 +59,41 @@ __device__ __forceinline__ Place find_place(const ShiftParams &p) {
 typedef u32x4 __attribute__((aligned(1))) u32x4_any;
 typedef u32x2 __attribute__((aligned(1))) u32x2_any;
 
+template <bool STREAM, class V> __device__ __forceinline__ V read_some(const V *at) {
+    if constexpr (STREAM) return __builtin_nontemporal_load(at);
+    return *at;
+}
+
+template <bool STREAM, class V> __device__ __forceinline__ void write_some(V x, V *at) {
+    if constexpr (STREAM) __builtin_nontemporal_store(x, at);
+    else *at = x;
+}
+
 // N elements of the cache's type, and as 32-bit values.
 template <class T, bool F8, int N> struct Elements {
     uint32_t raw[F8 ? N / 4 : N / 2];
-    __device__ __forceinline__ void load(const char *at) {
+    template <bool STREAM> __device__ __forceinline__ void load(const char *at) {
         constexpr int kWords = F8 ? N / 4 : N / 2;
         if constexpr (kWords == 2) {
-            const u32x2 x = __builtin_nontemporal_load((const u32x2_any *)at);
+            const u32x2 x = read_some<STREAM>((const u32x2_any *)at);
             raw[0] = x[0], raw[1] = x[1];
         } else {
 #pragma unroll
             for (int i = 0; i < kWords; i += 4) {
-                const u32x4 x = __builtin_nontemporal_load((const u32x4_any *)(at + i * 4));
+                const u32x4 x = read_some<STREAM>((const u32x4_any *)(at + i * 4));
 #pragma unroll
                 for (int e = 0; e < 4; ++e) raw[i + e] = x[e];
             }
         }
     }
-    __device__ __forceinline__ void store(char *at) const {
+    template <bool STREAM> __device__ __forceinline__ void store(char *at) const {
         constexpr int kWords = F8 ? N / 4 : N / 2;
         if constexpr (kWords == 2) {
-            __builtin_nontemporal_store(u32x2{raw[0], raw[1]}, (u32x2_any *)at);
+            write_some<STREAM, u32x2_any>(u32x2{raw[0], raw[1]}, (u32x2_any *)at);
         } else {
 #pragma unroll
             for (int i = 0; i < kWords; i += 4)
-                __builtin_nontemporal_store(u32x4{raw[i], raw[i + 1], raw[i + 2], raw[i + 3]}, (u32x4_any *)(at + i * 4));
+                write_some<STREAM, u32x4_any>(u32x4{raw[i], raw[i + 1], raw[i + 2], raw[i + 3]}, (u32x4_any *)(at + i * 4));
         }
     }
     __device__ __forceinline__ void get(float (&x)[N]) const {
@@ -123,7 +133,7 @@ __device__ __forceinline__ void saturate_f8() { __builtin_amdgcn_s_setreg(1 | 23
 // turns stay below 2^19.  The sines of the unit are off by up to 1.3e-7 (2^-22.9) of their size-1 range.
 template <int N> __device__ __forceinline__ void sincos_turns(int s, const double (&f)[N], float (&c)[N], float (&si)[N]) {
     float u[N];
-    if (__any((uint32_t)(s + (1 << 20)) >= 1u << 21)) {
+    if (__any((uint32_t)s + (1u << 20) >= 1u << 21)) {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const double turns = s * f[i];
@@ -154,8 +164,10 @@ __device__ __forceinline__ double to_turns(const ShiftParams &p, int pair) {
 // tokens lie and their shifts go to LDS first.  A lane takes eight pairs of a
 // row, always the same ones, so that it holds their frequencies; a row's last
 // unit ends at its last pair and may overlap the one before.  A row lies in one
-// wave, which reads all of it before it writes.
-template <class T, bool F8, bool INTERLEAVED>
+// wave, which reads all of it before it writes.  STREAM passes the caches by:
+// for halves of a row that are whole cache lines (376 against 412 us for the
+// 16-bit keys above; halves of 16 and 48 bytes would take twice as long as they do).
+template <class T, bool F8, bool INTERLEAVED, bool STREAM>
 __global__ __launch_bounds__(kThreads) void rope_shift_kernel(ShiftParams p) {
     constexpr int kElem = F8 ? 1 : 2, kTok = kTokens<F8>, kNext = kAhead<F8>;
     __shared__ uint32_t where[kTok];            // 16-byte units from the plane's start
@@ -201,8 +213,8 @@ __global__ __launch_bounds__(kThreads) void rope_shift_kernel(ShiftParams p) {
                 s[i] = by[h][t];
                 at[i] = base + ((int64_t)where[t] << 4) + (int64_t)(head0 + h) * p.cache.head_bytes;
                 if (s[i] == 0) continue;
-                a[i].load(at[i] + first);
-                if constexpr (!INTERLEAVED) b[i].load(at[i] + second);
+                a[i].template load<STREAM>(at[i] + first);
+                if constexpr (!INTERLEAVED) b[i].template load<STREAM>(at[i] + second);
             }
             // units of a row overlap, in the same instructions of a wave: all are read here
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -222,10 +234,10 @@ __global__ __launch_bounds__(kThreads) void rope_shift_kernel(ShiftParams p) {
                     rb = __builtin_fmaf(va, si[e], vb * c[e]);
                 }
                 a[i].set(xa);
-                a[i].store(at[i] + first);
+                a[i].template store<STREAM>(at[i] + first);
                 if constexpr (!INTERLEAVED) {
                     b[i].set(xb);
-                    b[i].store(at[i] + second);
+                    b[i].template store<STREAM>(at[i] + second);
                 }
             }
         }
@@ -279,9 +291,10 @@ __global__ __launch_bounds__(kThreads) void rope_shift_short_kernel(ShiftParams 
     }
 }
 
-template <class T, bool F8> void (*shift_kernel(bool interleaved, bool small))(ShiftParams) {
+template <class T, bool F8> void (*shift_kernel(bool interleaved, bool small, bool stream))(ShiftParams) {
     if (small) return interleaved ? rope_shift_short_kernel<T, F8, true> : rope_shift_short_kernel<T, F8, false>;
-    return interleaved ? rope_shift_kernel<T, F8, true> : rope_shift_kernel<T, F8, false>;
+    if (interleaved) return rope_shift_kernel<T, F8, true, false>;
+    return stream ? rope_shift_kernel<T, F8, false, true> : rope_shift_kernel<T, F8, false, false>;
 }
 
 }  // namespace
@@ -329,9 +342,10 @@ int kv_rope_shift(const kv_layout *layout, void *const *h_layer_ptrs, const int3
     p.by_heads = tkv::make_divider((uint32_t)(layout->kv_heads % tkv::kHeads ? layout->kv_heads % tkv::kHeads : tkv::kHeads));
     p.sign = (flags & KV_ROPE_INVERSE) ? -1.0 : 1.0;
     const bool small = p.half < tkv::kPairs, inter = flags & KV_ROPE_INTERLEAVED;
-    auto kernel = cache_dtype == KV_F8E4M3 ? tkv::shift_kernel<tkv::Bf16, true>(inter, small)
-                                           : (cache_dtype == KV_BF16 ? tkv::shift_kernel<tkv::Bf16, false>(inter, small)
-                                                                     : tkv::shift_kernel<tkv::F16, false>(inter, small));
+    const bool lines = p.half * layout->elem_bytes % 128 == 0 && p.cache.head_bytes % 128 == 0;
+    auto kernel = cache_dtype == KV_F8E4M3 ? tkv::shift_kernel<tkv::Bf16, true>(inter, small, lines)
+                                           : (cache_dtype == KV_BF16 ? tkv::shift_kernel<tkv::Bf16, false>(inter, small, lines)
+                                                                     : tkv::shift_kernel<tkv::F16, false>(inter, small, lines));
     const int tokens = cache_dtype == KV_F8E4M3 ? tkv::kTokens<true> : tkv::kTokens<false>;
     const int64_t tiles = ((int64_t)max_len + tokens - 1) / tokens;
     const int64_t most = tkv::kMaxBlocks / places;

@@ -126,8 +126,8 @@ __device__ __forceinline__ float weigh_tile(const WeightParams &p, const Span &s
     uint32_t off[kOffsets];
 #pragma unroll
     for (int i = 0; i < kOffsets; ++i) {
-        const int x = i * kThreads + tid, row = x / VPR, token = (int)divide(row, p.by_group);
-        off[i] = (uint32_t)(token * (int)p.q_ts + (row - token * p.group) * (int)p.q_hs + x % VPR * 16);
+        const uint32_t x = i * kThreads + tid, row = x / VPR, token = divide(row, p.by_group);
+        off[i] = token * (uint32_t)p.q_ts + (row - token * p.group) * (uint32_t)p.q_hs + x % VPR * 16;
     }
     const auto load = [&](int row0) {
         if (steady && row0 + kRows <= row_end) {
