@@ -388,8 +388,8 @@ __device__ __forceinline__ void few_rows(const AttentionParams &p, const Tile &t
 }
 
 // Tiles of 32 rows a wave over steps of 64 keys.  K and V of a step go
-// through LDS for all waves: loaded into registers two steps ahead (or one),
-// written to the other buffer, one barrier a step.
+// through LDS for all waves: loaded into registers one step ahead (two of an
+// 8-bit cache), written to the other buffer, one barrier a step.
 // Again S^T = K Q^T and O^T = V^T P^T, with 32 x 32 products: a lane holds
 // one row's scores for half of the keys, so that a row's maximum and sum need
 // one exchange between lanes.  Steps are bound by the issue of exponentials,
@@ -398,7 +398,7 @@ __device__ __forceinline__ void few_rows(const AttentionParams &p, const Tile &t
 // by card), the matrix units busy for 43 % of the time, the vector units for 45 %;
 // head size 80 with a window of 1,024, ragged, 61 to 65 us (330 to 350 TFLOP/s of
 // what the rows see).  Four prompts of 4,096 with a window of 1,024 and 4 sinks,
-// 241 GFLOP in 326 to 340 us (710 to 740): of a workgroup's 47 us 4 go before its
+// 241 GFLOP in 324 to 340 us (710 to 745): of a workgroup's 47 us 4 go before its
 // first step and 2 behind its last, and its 18 steps hold 1,152 keys, of which a
 // row sees 1,028.  The scores of the next step beside the exponentials of this
 // one take 3 % longer, 64 rows a wave (half of the LDS reads, one wave on a SIMD)
@@ -415,9 +415,9 @@ template <int DP> constexpr int kKeyRow = DP * 2 + 16;     // bytes of an LDS ro
 template <int DP> constexpr int kValueRow = DP * 2 + (DP * 2 % 128 ? 0 : 64);   // of V: 4 rows, 64 bytes of each
 template <int DP> constexpr int kTileLds = 2 * kStep * (kKeyRow<DP> + kValueRow<DP>);
 
-// Steps that a tile's loads are ahead.  What is read once comes from memory, two steps away; where that takes too many
-// registers, one.
-template <bool F8, int DP, int W> constexpr int ahead_of = DP > 128 || (DP == 128 && !F8 && W == 4) ? 1 : 2;
+// Steps that a tile's loads are ahead: two of an 8-bit cache, whose steps are half the bytes (a ragged batch at head size
+// 80 56 against 57 us); one of a 16-bit cache, whose second set of registers costs as much as it gives.
+template <bool F8, int DP> constexpr int ahead_of = F8 && DP <= 128 ? 2 : 1;
 
 // Where a step's keys lie (16-byte units from a plane's start), and which of
 // them are in the cache.
@@ -431,7 +431,7 @@ __device__ __forceinline__ void many_rows(const AttentionParams &p, const Tile &
                                           int *odd, Places *places) {
     constexpr int KS = DP / 16, DT = DP / 32, kThreads = 64 * W, kRows = 32 * W;
     constexpr int VEC = F8 ? 16 : 8, VPR = DP / VEC, kVecs = kStep * VPR, VL = (kVecs + kThreads - 1) / kThreads;
-    constexpr int kAhead = ahead_of<F8, DP, W>;
+    constexpr int kAhead = ahead_of<F8, DP>;
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), col = lane & 31, half = lane >> 5;
     char *const kbuf = lds, *const vbuf = lds + 2 * kStep * kKeyRow<DP>;
 
