@@ -59,8 +59,8 @@ class ServedCache:
             raise ValueError("sink must not be negative")
         if renumber and axes is not None:
             raise ValueError("evictions renumber positions of one axis only")
-        self.axes, self.renumber = axes, renumber
-        self.num_axes = 1 if axes is None else int(np.max(axes, initial=0)) + 1
+        self.axes, self.renumber = None if axes is None else np.ascontiguousarray(axes, np.uint8), renumber
+        self.num_axes = 1 if axes is None else int(self.axes.max(initial=0)) + 1
         self.dev = block_tables.device
         self.capacity = block_tables.shape[1] * layout.block_size
         self.lengths = np.asarray(lengths, np.int64).copy()     # tokens that the cache holds
