@@ -118,8 +118,11 @@ class ServedCache:
             pos = given
             if pos.size:
                 after[new > 0] = np.maximum.reduceat(pos.max(0).astype(np.int64), off[:-1][new > 0]) + 1
-        elif self.axes is not None:
-            pos = np.tile(pos, (self.num_axes, 1))
+        else:
+            if (after[new > 0] > 1 << 31).any():
+                raise ValueError("positions must stay below 2^31")
+            if self.axes is not None:
+                pos = np.tile(pos, (self.num_axes, 1))
         self._follow()
         d_off, d_len, d_pos = self._upload(off, lengths.astype(np.int32), np.ascontiguousarray(pos, np.int32).ravel())
         if self.axes is not None:

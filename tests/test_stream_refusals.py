@@ -196,6 +196,15 @@ def test_served_cache_refuses():
     assert s.lengths.tolist() == [100, 3] and s.positions.tolist() == [100, 3]
 
 
+@pytest.mark.parametrize("axes", [None, kv.kv_rope_axes([8, 12, 12])])
+def test_served_cache_refuses_positions_beyond_31_bits(axes):
+    s = _host_cache([100, 3], axes=axes)
+    s.positions[1] = (1 << 31) - 1                     # the last one: it may still be taken, no request goes on after it
+    with pytest.raises(ValueError, match="2\\^31"):
+        s.begin([1, 2])
+    assert s.lengths.tolist() == [100, 3] and s.positions.tolist() == [100, (1 << 31) - 1]
+
+
 def test_workspaces_of_no_requests():
     none = _batch(num_q=0, num_reqs=0, d_q_off=0, d_kv_len=0, d_block_tables=0)
     for hint in (0, 5000):
