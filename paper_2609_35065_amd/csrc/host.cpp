@@ -146,9 +146,9 @@ int plan_weights(const kv_layout *lo, const kv_batch *b, int32_t q_heads, int32_
     plan->sink_tiles = plan->parts = 0;
     if (plan->windowed && !plan->few) {
         // A sink's rows are all of a chunk's, a key's those of a window: as many parts as that is longer.  (Sums of
-        // parts need memory for each sink: more than 1,024 are not cut.)
+        // parts need memory for each sink: more than 1,024 are not cut.  Without sinks there is nothing to cut, or to join.)
         int64_t tiles = ((int64_t)sink + 63) / 64, parts = (b->max_q_len + (int64_t)window + 255) / ((int64_t)window + 256);
-        parts = parts < 1 || tiles > 16 ? 1 : (parts > 64 ? 64 : parts);
+        parts = parts < 1 || tiles == 0 || tiles > 16 ? 1 : (parts > 64 ? 64 : parts);
         plan->sink_tiles = (int32_t)(tiles > 256 ? 256 : tiles);
         plan->parts = (int32_t)parts;
     }

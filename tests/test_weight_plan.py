@@ -1,0 +1,38 @@
+"""The launch plan of the accumulated weights, without a GPU: no launch is empty, and the batches that the GPU tests of
+its variants use take the variants that they are there for."""
+import random
+import shutil
+
+import pytest
+
+from weight_plan import weight_plan
+
+pytestmark = pytest.mark.skipif(shutil.which("g++") is None, reason="g++ missing")
+
+
+def _whole(p):
+    """Every launch of the plan has workgroups, and a workspace where sums are joined, for all of them."""
+    assert p.tiles > 0 and p.sink_tiles >= 0
+    assert p.workspace > 0 if p.parts > 1 else p.workspace == 0
+    assert p.sink_tiles > 0 or p.parts <= 1               # the join has a workgroup for each tile of sinks
+    assert p.tiles + p.sink_tiles * p.parts <= 65535
+
+
+@pytest.mark.parametrize("new", [1, 4, 5, 17, 272, 273, 700, 5000, 100000])
+@pytest.mark.parametrize("window", [1, 16, 100, 1024])
+@pytest.mark.parametrize("sink", [0, 1, 64, 65, 1024, 1025, 1 << 20])
+def test_no_launch_is_empty(new, window, sink):
+    p = weight_plan([new + 10, 10], [new, 1], 2, 4, window, sink)
+    _whole(p)
+    assert sink or p.parts <= 1
+
+
+def test_no_launch_is_empty_over_random_batches():
+    rng = random.Random(3)
+    for _ in range(3000):
+        log = lambda hi: int(hi ** rng.random())
+        reqs = log(200)
+        new = [log(20000) for _ in range(reqs)]
+        lengths = [n + log(40000) - 1 for n in new]
+        _whole(weight_plan(lengths, new, log(64), log(16), rng.choice([0, log(1 << 14), (1 << 31) - 1]),
+                           rng.choice([-1, 0, 1, 4, log(4096), (1 << 31) - 1])))
