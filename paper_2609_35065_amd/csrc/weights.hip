@@ -241,8 +241,15 @@ __device__ __forceinline__ float weigh_tile(const WeightParams &p, const Span &s
         read(0, mine);
         read_lse(0, mine);
     }
+    // Up to 32 rows, a request's that decodes in a batch of many rows, take one group: the others' products are left out (64
+    // requests of 20 rows over 4,000 tokens 166 us, 170 with them).
+    const bool one = row_end - row_begin <= 32;
+    if (one && row_begin < row_end && mine == 0) {
+        products();
+        exponentials(row_begin);
+    }
     int buf = 0;
-    for (int row0 = row_begin; row0 < row_end; row0 += kRows, buf ^= 1) {
+    for (int row0 = one ? row_end : row_begin; row0 < row_end; row0 += kRows, buf ^= 1) {
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
             const int at = mine + rt * 32;
