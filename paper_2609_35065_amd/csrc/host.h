@@ -30,7 +30,8 @@ struct AttentionPlan {
 struct WeightPlan {
     bool windowed;        // the kernels that know which keys a window leaves out
     bool few;             // no request has more than 16 rows a head
-    int32_t keys;         // of a workgroup's tile of many rows: 64 or 256
+    bool ahead;           // of these: a wave passes several tiles of 64 keys
+    int32_t keys;         // of a workgroup's tile of many rows: 64, 128 or 256
     int64_t tiles;        // workgroups for keys, each for every request and KV head
     int32_t sink_tiles;   // and for 64 sinks each,
     int32_t parts;        // times the parts that their rows are cut into

@@ -387,16 +387,24 @@ __global__ __launch_bounds__(64) void sink_weights_join_kernel(WeightParams p) {
 }
 
 // Few rows (a decoded token's heads): nothing to share, so that each wave works
-// alone on 64 keys, 16 rows at a time, with the next 64 on their way (where two
-// sets of them fit the registers) and their places looked up.  A lane has one
-// key (lane % 16) and 4 of 16 rows.  Bound by the reads of K: the last 2,048 and
-// first 4 tokens of 64 requests, 8 KV heads of 128, 0.28 GB in 63 us (4.4 TB/s;
-// 8 bits 32 us), where one tile a wave, none ahead, takes 68 (48).  Heads of one
-// block on one XCD, or more workgroups, are no faster.
-template <class T, bool F8, int DP, bool SINK>
-__global__ __launch_bounds__(kThreads, DP > 128 ? 1 : 2) void attention_weights_few_kernel(WeightParams p) {
+// alone on 64 keys, 16 rows at a time.  A lane has one key (lane % 16) and 4 of
+// 16 rows.  Bound by the reads of K: the last 2,048 and first 4 tokens of 64
+// requests, 8 KV heads of 128, 0.28 GB in 62 us (4.5 TB/s; 8 bits 32 us).
+// AHEAD: a wave passes several tiles, the next one in a second set of registers
+// on its way beside this one, its places looked up (above, 65 us without; 64
+// requests of 4,096 111 and 121).  Else most waves have one tile, and what
+// counts is how many waves there are, three on a SIMD where two sets leave two:
+// 512 requests of 64 tokens 18 us (35 with AHEAD), 8 of 2,100 10.7 (13.1).
+// 16-bit rows of up to 96 columns, of three pieces, are fastest with one tile a
+// wave and the rows read behind its keys: 64 requests of 4,096 at head size 80
+// 88 us, 91 with AHEAD and 97 with the rows first; ragged ones 94, 109 and 103.
+// 16-bit rows beyond 128 columns leave no room for two sets.  Heads of one block
+// on one XCD are no faster.
+template <class T, bool F8, int DP, bool SINK, bool AHEAD>
+__global__ __launch_bounds__(kThreads, AHEAD && DP <= 128 ? 2 : 1) void attention_weights_few_kernel(WeightParams p) {
     constexpr int KS = DP / 32, LD = F8 ? KS / 2 : KS, KT = kWaveKeys / 16;
-    constexpr int kSets = LD <= 4 ? 2 : 1;
+    constexpr int kSets = AHEAD ? 2 : 1;
+    constexpr bool kLate = DP == 96;           // rows behind the keys
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, quad = lane >> 4;
     const int h = (int)(blockIdx.x % p.kv_heads), r = (int)(blockIdx.x / p.kv_heads);
     const Span span = find_span(p, r);
@@ -410,7 +418,7 @@ __global__ __launch_bounds__(kThreads, DP > 128 ? 1 : 2) void attention_weights_
     const int places = (int)(len - (keys.start - keys.sink)), gap = (int)(keys.start - keys.sink);
     if constexpr (SINK) fade(p, out, keys, (int64_t)blockIdx.y * kThreads + threadIdx.x, (int64_t)gridDim.y * kThreads);
     const auto key_at = [&](int place) { return SINK && place >= (int)keys.sink ? place + gap : place; };
-    // (places are at most 2^30 and the grid's tiles 2^17 apart: 32 bits)
+    // (places are at most 2^30, and the grid's tiles 2^23 apart: 32 bits)
     const int stride = (int)gridDim.y * kWaves * kWaveKeys, start = ((int)blockIdx.y * kWaves + wave) * kWaveKeys;
 
     // 16 rows: operands, and for this lane's four rows of the result what they see
@@ -456,13 +464,21 @@ __global__ __launch_bounds__(kThreads, DP > 128 ? 1 : 2) void attention_weights_
     };
     const auto weigh = [&](int set, int t0) {
         u32x4(&kf)[KT][LD] = sets[set];
-#pragma unroll
-        for (int x = 0; x < KT; ++x) arrange_rows(kf[x]);
         float sum[KT];
 #pragma unroll
         for (int x = 0; x < KT; ++x) sum[x] = 0.0f;
+        if constexpr (!kLate) {
+#pragma unroll
+            for (int x = 0; x < KT; ++x) arrange_rows(kf[x]);
+        }
         for (int row0 = 0; row0 < nrows; row0 += 16) {
-            if (nrows > 16) rows(row0);
+            if (kLate || nrows > 16) rows(row0);
+            if constexpr (kLate) {
+                if (row0 == 0) {
+#pragma unroll
+                    for (int x = 0; x < KT; ++x) arrange_rows(kf[x]);
+                }
+            }
 #pragma unroll
             for (int x = 0; x < KT; ++x) {
                 f32x4 s = {0, 0, 0, 0};
@@ -491,15 +507,24 @@ __global__ __launch_bounds__(kThreads, DP > 128 ? 1 : 2) void attention_weights_
         }
         if (t0 < places - lane) out[key_at(t0 + lane)] = p.decay == 0.0f ? got : __builtin_fmaf(p.decay, old[set], got);
     };
-    look_up(start);
-    if (nrows > 0) rows(0);
-    if constexpr (kSets == 1) {
+    if constexpr (kLate) {
+        for (int t0 = start; t0 < places; t0 += stride) {
+            look_up(t0);
+            fetch(0, t0);
+            weigh(0, t0);
+        }
+    } else if constexpr (!AHEAD) {
+        if (start >= places) return;
+        look_up(start);
+        if (nrows > 0) rows(0);
         for (int t0 = start; t0 < places; t0 += stride) {
             fetch(0, t0);
             look_up(t0 + stride);
             weigh(0, t0);
         }
     } else {
+        look_up(start);
+        if (nrows > 0) rows(0);
         if (start < places) fetch(0, start);
         look_up(start + stride);
         for (int t0 = start; t0 < places; t0 += 2 * stride) {
@@ -515,18 +540,25 @@ __global__ __launch_bounds__(kThreads, DP > 128 ? 1 : 2) void attention_weights_
     }
 }
 
-template <class T, bool F8, bool SINK> void (*weights_few_kernel(int head_dim))(WeightParams) {
-    if (head_dim <= 64) return attention_weights_few_kernel<T, F8, 64, SINK>;
-    if constexpr (!F8) {
-        if (head_dim <= 96) return attention_weights_few_kernel<T, F8, 96, SINK>;
+template <class T, bool F8, bool SINK, int DP> void (*weights_few_kernel_for(bool ahead))(WeightParams) {
+    if constexpr (DP != 96 && (F8 || DP <= 128)) {
+        if (ahead) return attention_weights_few_kernel<T, F8, DP, SINK, true>;
     }
-    if (head_dim <= 128) return attention_weights_few_kernel<T, F8, 128, SINK>;
-    return attention_weights_few_kernel<T, F8, 256, SINK>;
+    return attention_weights_few_kernel<T, F8, DP, SINK, false>;
 }
 
-template <bool SINK> auto weights_few_kernel(bool bf16, bool f8, int d) {
-    return bf16 ? (f8 ? weights_few_kernel<Bf16, true, SINK>(d) : weights_few_kernel<Bf16, false, SINK>(d))
-                : (f8 ? weights_few_kernel<F16, true, SINK>(d) : weights_few_kernel<F16, false, SINK>(d));
+template <class T, bool F8, bool SINK> auto weights_few_kernel(int head_dim, bool ahead) {
+    if (head_dim <= 64) return weights_few_kernel_for<T, F8, SINK, 64>(ahead);
+    if constexpr (!F8) {
+        if (head_dim <= 96) return weights_few_kernel_for<T, F8, SINK, 96>(ahead);
+    }
+    if (head_dim <= 128) return weights_few_kernel_for<T, F8, SINK, 128>(ahead);
+    return weights_few_kernel_for<T, F8, SINK, 256>(ahead);
+}
+
+template <bool SINK> auto weights_few_kernel(bool bf16, bool f8, int d, bool ahead) {
+    return bf16 ? (f8 ? weights_few_kernel<Bf16, true, SINK>(d, ahead) : weights_few_kernel<Bf16, false, SINK>(d, ahead))
+                : (f8 ? weights_few_kernel<F16, true, SINK>(d, ahead) : weights_few_kernel<F16, false, SINK>(d, ahead));
 }
 
 template <class T, bool F8, int KW, bool SINK, int DP> void (*weights_kernel_for())(WeightParams) {
@@ -547,7 +579,7 @@ template <int KW, bool SINK> auto weights_kernel(bool bf16, bool f8, int d) {
 }
 
 template <bool SINK> auto weights_kernel(const WeightPlan &plan, bool bf16, bool f8, int d) {
-    return plan.few ? weights_few_kernel<SINK>(bf16, f8, d)
+    return plan.few ? weights_few_kernel<SINK>(bf16, f8, d, plan.ahead)
                     : (plan.keys == 64 ? weights_kernel<1, SINK>(bf16, f8, d)
                                        : (plan.keys == 128 ? weights_kernel<2, SINK>(bf16, f8, d) : weights_kernel<4, SINK>(bf16, f8, d)));
 }

@@ -16,6 +16,7 @@ def _whole(p):
     assert p.workspace > 0 if p.parts > 1 else p.workspace == 0
     assert p.sink_tiles > 0 or p.parts <= 1               # the join has a workgroup for each tile of sinks
     assert p.tiles + p.sink_tiles * p.parts <= 65535
+    assert p.few or not p.ahead
 
 
 @pytest.mark.parametrize("new", [1, 4, 5, 17, 272, 273, 700, 5000, 100000])
@@ -36,3 +37,18 @@ def test_no_launch_is_empty_over_random_batches():
         lengths = [n + log(40000) - 1 for n in new]
         _whole(weight_plan(lengths, new, log(64), log(16), rng.choice([0, log(1 << 14), (1 << 31) - 1]),
                            rng.choice([-1, 0, 1, 4, log(4096), (1 << 31) - 1])))
+
+
+def test_variants_of_few_rows():
+    from test_gpu_sink_weights_variants import TILES
+    t = dict(lengths=TILES["lengths"], new=TILES["new"], heads=TILES["heads"], group=2)
+    for dim in (64, 128, 256):
+        for window, sink in ((0, -1), (300, -1), (1200, 4), (300, 70), (1200, 0)):
+            p = weight_plan(window=window, sink=sink, dim=dim, **t)
+            assert p.few and p.ahead and p.tiles == 1, (dim, window, sink)
+    assert not weight_plan(dim=80, **t).ahead and weight_plan(dim=80, **t).tiles == 6
+    # where all run at once, and where a request has too few keys for it
+    assert weight_plan([9000] * 2, [1] * 2, 8, 4)[1:5] == (True, False, 256, 36)
+    assert weight_plan([511] * 1024, [1] * 1024, 8, 4)[1:5] == (True, False, 256, 2)
+    assert weight_plan([4096] * 8, [1] * 8, 8, 4, dim=128)[1:5] == (True, True, 256, 8)
+    assert weight_plan([16000] * 64, [1] * 64, 8, 4, dim=128).tiles == 4

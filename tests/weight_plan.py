@@ -10,7 +10,7 @@ import paper_2609_35065_amd as kv
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 CSRC = os.path.join(ROOT, "paper_2609_35065_amd", "csrc")
-Plan = collections.namedtuple("Plan", "windowed few keys tiles sink_tiles parts workspace")
+Plan = collections.namedtuple("Plan", "windowed few ahead keys tiles sink_tiles parts workspace")
 
 
 @functools.lru_cache(None)
@@ -28,7 +28,7 @@ def weight_plan(lengths, new, heads, group, window=0, sink=-1, dim=64, max_q=Non
     layout = kv.make_layout(1, heads, dim, 2, 16, 16, 64, 1, 64 * seg, seg)
     b = kv.KvBatch(len(lengths), 1, sum(new), max(new) if max_q is None else max_q, max(lengths) if max_kv is None else max_kv,
                    0, 0, 0)
-    out = (ct.c_int64 * 7)()
+    out = (ct.c_int64 * 8)()
     rc = _build().weight_plan(ct.byref(layout), ct.byref(b), heads * group, window, sink, out)
     assert rc == kv.KV_OK, rc
     return Plan(*out)
