@@ -579,9 +579,11 @@ template <int KW, bool SINK> auto weights_kernel(bool bf16, bool f8, int d) {
 }
 
 template <bool SINK> auto weights_kernel(const WeightPlan &plan, bool bf16, bool f8, int d) {
-    return plan.few ? weights_few_kernel<SINK>(bf16, f8, d, plan.ahead)
-                    : (plan.keys == 64 ? weights_kernel<1, SINK>(bf16, f8, d)
-                                       : (plan.keys == 128 ? weights_kernel<2, SINK>(bf16, f8, d) : weights_kernel<4, SINK>(bf16, f8, d)));
+    if (plan.few) return weights_few_kernel<SINK>(bf16, f8, d, plan.ahead);
+    if constexpr (SINK) {
+        if (plan.keys == 128) return weights_kernel<2, SINK>(bf16, f8, d);
+    }
+    return plan.keys == 64 ? weights_kernel<1, SINK>(bf16, f8, d) : weights_kernel<4, SINK>(bf16, f8, d);
 }
 
 int attention_weights(const kv_layout *layout, const void *d_layer, const kv_batch *batch, const kv_rows *q,

@@ -101,3 +101,17 @@ def test_missing_blocks_in_several_tiles(dtype):
     q = ref.rows_of(8, 128, 64, torch.bfloat16, c.gen, 1.5).contiguous()
     for window, sink in ((300, None), (700, 4), (300, 70)):
         _check_some(c, TILES["new"], q, 0.125, window, sink, 0.5)
+
+
+# tiles of 128 keys, each half of them two waves that share the rows; in the second the sinks' rows are cut into parts
+PAIRS = [dict(heads=64, lengths=[1000, 800], new=[200, 150], window=500), dict(heads=64, lengths=[900, 700], new=[660, 500], window=100)]
+
+
+@pytest.mark.parametrize("dim,dtype", [(64, "f16"), (80, "bf16"), (80, "f8"), (128, "bf16"), (128, "f8"), (256, "bf16"), (256, "f8")])
+@pytest.mark.parametrize("at", [0, 1])
+def test_tiles_of_128_keys(at, dim, dtype):
+    t = PAIRS[at]
+    c = ref.Cache(t["lengths"], heads=64, dim=dim, dtype=DTYPES[dtype], seed=dim).device()
+    q = ref.rows_of(sum(t["new"]), 128, dim, c.q_dtype, c.gen, 1.5).contiguous()
+    for sink, decay, causal in ((4, 1.0, True), (70, 0.5, True), (0, 0.0, True), (4, 0.5, False)):
+        _check_some(c, t["new"], q, dim ** -0.5, t["window"], sink, decay, causal)

@@ -52,3 +52,17 @@ def test_variants_of_few_rows():
     assert weight_plan([511] * 1024, [1] * 1024, 8, 4)[1:5] == (True, False, 256, 2)
     assert weight_plan([4096] * 8, [1] * 8, 8, 4, dim=128)[1:5] == (True, True, 256, 8)
     assert weight_plan([16000] * 64, [1] * 64, 8, 4, dim=128).tiles == 4
+
+
+def test_tiles_of_many_rows():
+    from test_gpu_sink_weights_variants import PAIRS
+    for t, parts in zip(PAIRS, (1, 2)):
+        for sink in (0, 4, 70):
+            p = weight_plan(group=2, sink=sink, dim=64, **t)
+            assert p.windowed and not p.few and p.keys == 128 and p.parts == (parts if sink else 1), (t, sink)
+        assert weight_plan(group=2, sink=-1, **t).keys != 128
+    rng = random.Random(4)
+    for _ in range(2000):                                  # 128 keys: with the windowed kernels alone
+        new = [rng.randint(1, 3000) for _ in range(rng.randint(1, 8))]
+        p = weight_plan([n + rng.randint(0, 3000) for n in new], new, rng.randint(1, 128), 4, rng.choice([0, 500, 1024]), rng.choice([-1, 0, 4]))
+        assert p.keys in (64, 256) or (p.keys == 128 and p.windowed)
