@@ -388,8 +388,8 @@ __device__ __forceinline__ void few_rows(const AttentionParams &p, const Tile &t
 }
 
 // Tiles of 32 rows a wave over steps of 64 keys.  K and V of a step go
-// through LDS for all waves: loaded into registers one step ahead (two of an
-// 8-bit cache), written to the other buffer, one barrier a step.
+// through LDS for all waves: loaded into registers one step ahead or two,
+// written to the other buffer, one barrier a step.
 // Again S^T = K Q^T and O^T = V^T P^T, with 32 x 32 products: a lane holds
 // one row's scores for half of the keys, so that a row's maximum and sum need
 // one exchange between lanes.  Steps are bound by the issue of exponentials,
@@ -415,9 +415,11 @@ template <int DP> constexpr int kKeyRow = DP * 2 + 16;     // bytes of an LDS ro
 template <int DP> constexpr int kValueRow = DP * 2 + (DP * 2 % 128 ? 0 : 64);   // of V: 4 rows, 64 bytes of each
 template <int DP> constexpr int kTileLds = 2 * kStep * (kKeyRow<DP> + kValueRow<DP>);
 
-// Steps that a tile's loads are ahead: two of an 8-bit cache, whose steps are half the bytes (a ragged batch at head size
-// 80 56 against 57 us); one of a 16-bit cache, whose second set of registers costs as much as it gives.
-template <bool F8, int DP> constexpr int ahead_of = F8 && DP <= 128 ? 2 : 1;
+// Steps that a tile's loads are ahead: two of an 8-bit cache in 96 columns (a ragged batch at head size 80 with a window 52
+// against 54 us, 4 chunks of 1,000 tokens over 4,000 at 96 213 and 217, though 8 of 2,048 over 4,096 692 and 688), else one:
+// the second set of registers costs more than it gives (8 bits at 64 columns, 4 chunks of 1,000 over 4,000 165 against 158
+// us; at 128, 64 chunks of 20 over 2,020 123 and 113, 8 of 2,048 over 4,096 813 and 806).
+template <bool F8, int DP> constexpr int ahead_of = F8 && DP == 96 ? 2 : 1;
 
 // Where a step's keys lie (16-byte units from a plane's start), and which of
 // them are in the cache.
