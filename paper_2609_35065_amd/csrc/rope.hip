@@ -13,7 +13,7 @@ namespace tkv {
 namespace {
 
 constexpr int kThreads = 256, kMaxTokens = 4;
-constexpr int64_t kStream = int64_t(1) << 27;          // bytes from which rows pass the caches by
+constexpr int64_t kStream = int64_t(1) << 28;          // bytes from which rows pass the caches by
 
 struct RopeParams {
     Paged cache;
@@ -70,9 +70,13 @@ __device__ __forceinline__ uint32_t pack4_f8(float a, float b, float c, float d)
 // Bound by memory: 32,768 tokens of 32 + 2 x 8 heads of 128, 0.81 GB read and
 // written in 143 us (5.6 TB/s); ragged, head size 80, an 8-bit cache: 0.25 GB in
 // 54 us (4.6 TB/s).  STREAM passes the caches by, which a large batch's rows do
-// not fit: 143 against 157 us (0.2 GB at head size 256: 38.7 against 45; but 0.1
-// GB 21 against 19).  That is for units of whole cache lines (64 pairs of 16
-// bits); the narrow rows of the 8-bit batch take 69 us that way.
+// not fit: 143 against 157 us by itself.  What follows an append is attention,
+// which reads its rows.  The two together, into rows of their own, take 273
+// against 283 us at 403 MB (32 prompts of 512 tokens) and 226 against 238 at 270
+// MB (11 of 1,000), in place the same within 1 %; but at 201 MB (16 of 512) in
+// place 144 against 138, as much of it is still in the memory-side cache of 256
+// MB.  That is for units of whole cache lines (64 pairs of 16 bits); the narrow
+// rows of the 8-bit batch take 69 us that way.
 enum Pairing { HALF, INTERLEAVED, ODD };
 
 template <bool STREAM, class V> __device__ __forceinline__ V read_row(const V *at) {
