@@ -100,7 +100,9 @@ class ServedCache:
 
     def begin(self, new, positions=None) -> None:
         """Start a step: ``new`` tokens of each request (0, 1 or many).  With several axes, ``positions`` [axes, rows]
-        are those of the new tokens (text, the same on all axes: None); a request goes on after its largest."""
+        are those of the new tokens (text, the same on all axes: None); a request goes on after its largest, of this
+        step and of those before.  Tokens held at the start have positions 0, 1, ...; where they have others, set the
+        request's next one, ``positions[r]``, first."""
         new = np.asarray(new, np.int64)
         if new.shape != self.lengths.shape or (new < 0).any() or (self.lengths + new > self.capacity).any():
             raise ValueError("new must hold one count per request, and leave every request within its block table")
@@ -117,7 +119,8 @@ class ServedCache:
                                  f"with axes")
             pos = given
             if pos.size:
-                after[new > 0] = np.maximum.reduceat(pos.max(0).astype(np.int64), off[:-1][new > 0]) + 1
+                largest = np.maximum.reduceat(pos.max(0).astype(np.int64), off[:-1][new > 0])
+                after[new > 0] = np.maximum(self.positions[new > 0], largest + 1)
         else:
             if (after[new > 0] > 1 << 31).any():
                 raise ValueError("positions must stay below 2^31")
