@@ -26,7 +26,7 @@ from typing import List, Optional, Sequence
 import numpy as np
 import torch
 
-from . import (KvLayout, kv_attention_weights, kv_evict_compact, kv_evict_select, kv_paged_attention,
+from . import (KV_MAX_AXES, KvLayout, kv_attention_weights, kv_evict_compact, kv_evict_select, kv_paged_attention,
                kv_rope_append, kv_rope_append_axes, kv_rope_shift, kv_sink_attention, kv_sink_attention_workspace,
                kv_sink_weights, kv_sink_weights_workspace, make_batch)
 
@@ -113,10 +113,12 @@ class ServedCache:
         after = self.positions + new
         if positions is not None:
             given = np.asarray(positions)
-            if self.axes is None or given.shape != (self.num_axes, pos.size) or given.dtype.kind not in "iu" \
+            # (there may be axes that no pair takes)
+            if self.axes is None or given.ndim != 2 or not self.num_axes <= given.shape[0] <= KV_MAX_AXES \
+                    or given.shape[1] != pos.size or given.dtype.kind not in "iu" \
                     or (given.size and (given.min() < -1 << 31 or given.max() >= 1 << 31)):
-                raise ValueError(f"positions must be [{self.num_axes}, {pos.size}] whole numbers of 32 bits, for a cache "
-                                 f"with axes")
+                raise ValueError(f"positions must be [axes, {pos.size}] whole numbers of 32 bits, of {self.num_axes} to "
+                                 f"{KV_MAX_AXES} axes, for a cache with axes")
             pos = given
             if pos.size:
                 largest = np.maximum.reduceat(pos.max(0).astype(np.int64), off[:-1][new > 0])
@@ -129,7 +131,7 @@ class ServedCache:
         self._follow()
         d_off, d_len, d_pos = self._upload(off, lengths.astype(np.int32), np.ascontiguousarray(pos, np.int32).ravel())
         if self.axes is not None:
-            d_pos = d_pos.view(self.num_axes, -1)
+            d_pos = d_pos.view(pos.shape)
         batch = make_batch(d_off, d_len, self.block_tables, int(off[-1]), int(new.max(initial=0)),
                            int(lengths.max(initial=0)))
         size = kv_sink_attention_workspace(self.layout, batch, self.q_heads, self.window, self.sink)

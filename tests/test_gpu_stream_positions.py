@@ -34,3 +34,21 @@ def test_a_request_goes_on_after_its_largest_position():
     s.positions[0] = 12
     s.begin([1], np.array([[12], [20], [14]]))
     assert s.positions.tolist() == [21]
+
+
+@pytest.mark.parametrize("sections", [[16, 16, 0], [0, 32, 0, 0], [32, 0]])
+def test_axes_that_no_pair_takes(sections):
+    c, s = _served([0, 4], seed=1, axes=kv.kv_rope_axes(sections), decay=None)
+    new, n = [20, 3], 23
+    given = np.random.default_rng(0).integers(0, 500, (len(sections), n))
+    s.begin(new, given)
+    assert s.positions.tolist() == [max(0, given[:, :20].max() + 1), max(4, given[:, 20:].max() + 1)]
+    q, k, v = (ref.rows_of(n, h, 64, torch.bfloat16, c.gen) for h in (4, 2, 2))
+    dq, out = q.cuda(), torch.empty(n, 4, 64, dtype=torch.bfloat16, device="cuda")
+    s.attend(0, dq, k.cuda(), v.cuda(), out)
+    torch.cuda.synchronize()
+    want, err = stream_ref.turn(q, given[kv.kv_rope_axes(sections)].T[:, None], FREQS, False)
+    ref.assert_within(dq, want, 2.0 ** -8 * want.abs() * 1.001 + err + 2.0 ** -24, "q")
+    for more in (0, kv.KV_MAX_AXES + 1):
+        with pytest.raises(ValueError, match="positions"):
+            s.begin([1, 1], np.zeros((more, 2), int))
