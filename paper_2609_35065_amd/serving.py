@@ -187,7 +187,8 @@ class ServedCache:
         if windowed and cut and recent < self.window - 1 and not self.renumber:
             raise ValueError(f"an eviction has to leave the last {self.window - 1} tokens, which the window reaches, "
                              f"not {recent}")
-        dtype = next((t.dtype for t in self.layers if t.is_floating_point()), self._dtype)
+        held = [t.dtype for t in self.layers if isinstance(t, torch.Tensor) and t.is_floating_point()]
+        dtype = held[0] if held else self._dtype
         if self.renumber and self.layout.elem_bytes == 2 and dtype is None:
             raise ValueError("the type of the keys is not known before a layer is attended")
         self._follow()

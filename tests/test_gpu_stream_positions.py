@@ -52,3 +52,22 @@ def test_axes_that_no_pair_takes(sections):
     for more in (0, kv.KV_MAX_AXES + 1):
         with pytest.raises(ValueError, match="positions"):
             s.begin([1, 1], np.zeros((more, 2), int))
+
+
+@pytest.mark.parametrize("renumber", [False, True])
+def test_layers_given_by_their_addresses(renumber):
+    got = []
+    for by_address in (False, True):
+        c = ref.Cache([300, 90], heads=2, dim=64, layers=2, seed=5).device()
+        s = ServedCache(c.layout, [t.data_ptr() for t in c.d_pool] if by_address else c.d_pool, c.d_bt, [0, 0], 4,
+                        torch.from_numpy(FREQS).cuda(), renumber=renumber)
+        for new in ([200, 60], [1, 1]):
+            s.begin(new)
+            for l in range(2):
+                q, k, v = (ref.rows_of(sum(new), h, 64, torch.bfloat16, c.gen).cuda() for h in (4, 2, 2))
+                s.attend(l, q, k, v, torch.empty_like(q))
+            s.evict(50, sink=2, recent=4)
+        torch.cuda.synchronize()
+        got.append([t.cpu() for t in (s.weights, *c.d_pool)])
+    for a, b in zip(*got):
+        assert torch.equal(a, b)
