@@ -157,22 +157,22 @@ int plan_weights(const kv_layout *lo, const kv_batch *b, int32_t q_heads, int32_
     if (plan->windowed && plan->few) span += sink;
     if (span > b->max_kv_len) span = b->max_kv_len;
     int64_t tiles = (span + plan->keys - 1) / plan->keys;
-    // Few rows: where all workgroups run at once, or a request has less than two tiles for each wave of one, a wave for each
-    // tile (2 requests of 9,000 tokens 12.2 us, 14.2 with the next tile on its way; 1,024 of 100 61 and 98).  Else a
-    // workgroup for each slot of the chip's, two on a compute unit (three at head sizes up to 64), whose waves pass tile
-    // after tile (8 requests of 4,096: 16.3 us, 16.8 a wave for each; 64 of 2,052 visible tokens 62 us, 64 and 75 with 3 and
-    // 8 times as many).  Several requests may be ragged, unless a window cuts them to one length: up to four times as many,
-    // of at least 1,024 keys (64 lognormal ones around 4,000 tokens 133 us, 232 without; 8 of them 16.7, 21.3 with keys for
-    // 512).  16-bit rows of 72 to 96 columns always have a wave for each tile (the kernel's comment has the times).
+    // Few rows: a wave for each tile, or a workgroup for each slot of the chip's, two on a compute unit (three at head sizes up
+    // to 64), whose waves pass tile after tile with the next one on its way.  The second where one request, or a window that
+    // cuts all to one length, leaves several tiles to a wave (one of 100,000 tokens 47 us, 51 a wave for each; 64 of 2,052
+    // visible ones 62, 65).  Several requests may be ragged, and then some waves pass far more than others (16 lognormal ones
+    // around 940 tokens 9.0 us a wave for each, 11 tile after tile): only where there are heads or keys enough for four
+    // workgroups a slot, of 1,024 keys or more and up to 2,048 of the longest request's (64 of 4,096 111 us, 122 a wave for
+    // each; 64 lognormal ones around 4,000 129 and 136).  16-bit rows of 72 to 96 columns always have a wave for each tile.
     plan->ahead = false;
     const bool pieces = lo->elem_bytes == 2 && lo->head_dim > 64 && lo->head_dim <= 96;
-    if (plan->few && !pieces && heads * tiles > 768 && (heads <= 512 || span >= 512)) {
+    if (plan->few && !pieces && heads > 0 && (heads <= 512 || span >= 512)) {
         const bool ragged = b->num_reqs > 1 && !(plan->windowed && (int64_t)window + b->max_q_len < b->max_kv_len);
         const int64_t slots = lo->head_dim <= 64 ? 768 : 512;
         int64_t most = slots / heads;
-        if (ragged) most = std::max(most, std::min(4 * slots / heads, span / 1024));
+        if (ragged) most = std::max({most, std::min(4 * slots / heads, span / 1024), span / 2048});
         most = std::max(most, int64_t(1));
-        plan->ahead = tiles > most;
+        plan->ahead = tiles > most && !(ragged && heads < 512 && heads * (span / 1024) < 4 * slots);
         if (plan->ahead) tiles = most;
     }
     plan->tiles = tiles < 1 ? 1 : (tiles > 32768 ? 32768 : tiles);

@@ -306,7 +306,8 @@ __global__ __launch_bounds__(kThreads, DP > 128 ? 1 : 2) void attention_weights_
         int tok0 = 0, tok1 = ntok;
         if (p.causal) tok0 = (int)min((int64_t)ntok, max((int64_t)0, (int64_t)tile0 - ahead));
         if (p.window > 0) tok1 = (int)max((int64_t)0, min((int64_t)ntok, (int64_t)tile0 + kKeys - 1 + p.window - ahead));
-        const float got = weigh_tile<T, F8, DP, KW, false>(p, span, r, h, tile0, tok0 * p.group, tok1 * p.group, lds);
+        float got = 0.0f;                          // (a window may have left all of them behind)
+        if (tok0 < tok1) got = weigh_tile<T, F8, DP, KW, false>(p, span, r, h, tile0, tok0 * p.group, tok1 * p.group, lds);
         const int64_t key = (int64_t)tile0 + wave % KW * kWaveKeys + lane;
         if (wave / KW == 0 && key < len) out[key] = p.decay == 0.0f ? got : __builtin_fmaf(p.decay, out[key], got);
     }
@@ -391,20 +392,17 @@ __global__ __launch_bounds__(64) void sink_weights_join_kernel(WeightParams p) {
 // 16 rows.  Bound by the reads of K: the last 2,048 and first 4 tokens of 64
 // requests, 8 KV heads of 128, 0.28 GB in 62 us (4.5 TB/s; 8 bits 32 us).
 // AHEAD: a wave passes several tiles, the next one in a second set of registers
-// on its way beside this one, its places looked up (above, 65 us without; 64
-// requests of 4,096 111 and 121).  Else most waves have one tile, and what
-// counts is how many waves there are, three on a SIMD where two sets leave two:
-// 512 requests of 64 tokens 18 us (35 with AHEAD), 8 of 2,100 10.7 (13.1).
-// 16-bit rows of up to 96 columns, of three pieces, are fastest with one tile a
-// wave and the rows read behind its keys: 64 requests of 4,096 at head size 80
-// 88 us, 91 with AHEAD and 97 with the rows first; ragged ones 94, 109 and 103.
-// 16-bit rows beyond 128 columns leave no room for two sets.  Heads of one block
-// on one XCD are no faster.
+// on its way beside this one (where two fit: not 16-bit rows beyond 128 columns),
+// its places looked up (64 requests of 4,096 tokens 111 us, 122 without).  Else
+// most waves have one tile, whose keys are asked for before the rows: 512
+// requests of 64 tokens 19 us, 35 with AHEAD; 1,024 of 100 72 and 98.  16-bit rows
+// of up to 96 columns, of three pieces, are fastest that way also in long caches:
+// 64 requests of 4,096 at head size 80 87 us, 91 with AHEAD, ragged ones around
+// 4,000 93 and 109.  Heads of one block on one XCD are no faster.
 template <class T, bool F8, int DP, bool SINK, bool AHEAD>
 __global__ __launch_bounds__(kThreads, AHEAD && DP <= 128 ? 2 : 1) void attention_weights_few_kernel(WeightParams p) {
     constexpr int KS = DP / 32, LD = F8 ? KS / 2 : KS, KT = kWaveKeys / 16;
-    constexpr int kSets = AHEAD ? 2 : 1;
-    constexpr bool kLate = DP == 96;           // rows behind the keys
+    constexpr int kSets = AHEAD && LD <= 4 ? 2 : 1;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, quad = lane >> 4;
     const int h = (int)(blockIdx.x % p.kv_heads), r = (int)(blockIdx.x / p.kv_heads);
     const Span span = find_span(p, r);
@@ -467,14 +465,14 @@ __global__ __launch_bounds__(kThreads, AHEAD && DP <= 128 ? 2 : 1) void attentio
         float sum[KT];
 #pragma unroll
         for (int x = 0; x < KT; ++x) sum[x] = 0.0f;
-        if constexpr (!kLate) {
+        if constexpr (AHEAD) {
 #pragma unroll
             for (int x = 0; x < KT; ++x) arrange_rows(kf[x]);
         }
         for (int row0 = 0; row0 < nrows; row0 += 16) {
-            if (kLate || nrows > 16) rows(row0);
-            if constexpr (kLate) {
-                if (row0 == 0) {
+            if (!AHEAD || nrows > 16) rows(row0);
+            if constexpr (!AHEAD) {
+                if (row0 == 0) {                   // here, so that the rows above are on their way with the keys
 #pragma unroll
                     for (int x = 0; x < KT; ++x) arrange_rows(kf[x]);
                 }
@@ -507,14 +505,13 @@ __global__ __launch_bounds__(kThreads, AHEAD && DP <= 128 ? 2 : 1) void attentio
         }
         if (t0 < places - lane) out[key_at(t0 + lane)] = p.decay == 0.0f ? got : __builtin_fmaf(p.decay, old[set], got);
     };
-    if constexpr (kLate) {
+    if constexpr (!AHEAD) {
         for (int t0 = start; t0 < places; t0 += stride) {
             look_up(t0);
             fetch(0, t0);
             weigh(0, t0);
         }
-    } else if constexpr (!AHEAD) {
-        if (start >= places) return;
+    } else if constexpr (kSets == 1) {
         look_up(start);
         if (nrows > 0) rows(0);
         for (int t0 = start; t0 < places; t0 += stride) {
@@ -541,7 +538,7 @@ __global__ __launch_bounds__(kThreads, AHEAD && DP <= 128 ? 2 : 1) void attentio
 }
 
 template <class T, bool F8, bool SINK, int DP> void (*weights_few_kernel_for(bool ahead))(WeightParams) {
-    if constexpr (DP != 96 && (F8 || DP <= 128)) {
+    if constexpr (F8 || DP != 96) {
         if (ahead) return attention_weights_few_kernel<T, F8, DP, SINK, true>;
     }
     return attention_weights_few_kernel<T, F8, DP, SINK, false>;

@@ -47,11 +47,15 @@ def test_variants_of_few_rows():
             p = weight_plan(window=window, sink=sink, dim=dim, **t)
             assert p.few and p.ahead and p.tiles == 1, (dim, window, sink)
     assert not weight_plan(dim=80, **t).ahead and weight_plan(dim=80, **t).tiles == 6
-    # where all run at once, and where a request has too few keys for it
+    # a wave for each tile where requests may be ragged and there are few heads, or keys; else up to 2,048 keys a workgroup
     assert weight_plan([9000] * 2, [1] * 2, 8, 4)[1:5] == (True, False, 256, 36)
     assert weight_plan([511] * 1024, [1] * 1024, 8, 4)[1:5] == (True, False, 256, 2)
-    assert weight_plan([4096] * 8, [1] * 8, 8, 4, dim=128)[1:5] == (True, True, 256, 8)
-    assert weight_plan([16000] * 64, [1] * 64, 8, 4, dim=128).tiles == 4
+    assert weight_plan([4096] * 8, [1] * 8, 8, 4, dim=128)[1:5] == (True, False, 256, 16)
+    assert weight_plan([32768] * 8, [1] * 8, 8, 4, dim=128)[1:5] == (True, True, 256, 32)
+    assert weight_plan([16384] * 64, [1] * 64, 8, 4, dim=128)[1:5] == (True, True, 256, 8)
+    assert weight_plan([32768], [1], 8, 4, dim=128)[1:5] == (True, True, 256, 64)
+    assert weight_plan([32768], [1], 8, 4, dim=80)[1:5] == (True, False, 256, 128)
+    assert weight_plan([8192] * 64, [1] * 64, 8, 4, window=2048, sink=4, dim=128)[1:5] == (True, True, 256, 1)
 
 
 def test_tiles_of_many_rows():
