@@ -409,7 +409,10 @@ __device__ __forceinline__ void few_rows(const AttentionParams &p, const Tile &t
 // maximum has grown by more than 2^kLag since it was last taken.  Until then
 // exponentials reach 2^kLag instead of 1, which costs no precision, neither in
 // l and o (32 bits) nor in P (a rounding relative to its size; 2^8 is far
-// below the 16-bit types' ends).
+// below the 16-bit types' ends).  P is rounded to the type of the products, as
+// the matrix units take it, which adds about a third to the error of results that
+// are rounded alone: 0.0022 against 0.0016 of their size in bf16, 0.00029 against
+// 0.00021 in f16; l sums what was not rounded.
 constexpr float kLag = 8.0f;
 constexpr int kStep = kTileStep;
 template <int DP> constexpr int kKeyRow = DP * 2 + 16;     // bytes of an LDS row of K: 8 rows on different banks

@@ -113,7 +113,9 @@ int plan_attention(const kv_layout *lo, const kv_batch *b, int32_t q_heads, int3
     int64_t span = b->max_kv_len;
     if (window > 0 && span > (int64_t)window + b->max_q_len + sink) span = (int64_t)window + b->max_q_len + sink;
     // Tiles of 256 rows read K and V half as often as those of 128, but take a compute unit each: where there are four
-    // rounds of them (8 x 2,048 tokens of 32 heads: 859 against 917 us; a mixed batch of fewer: 77 against 61 us).
+    // rounds of them (8 x 2,048 tokens of 32 heads: 859 against 917 us; a mixed batch of fewer: 77 against 61 us).  That is
+    // without a window, at head size 128: with one of 1,024 or less, and at head size 64, 128 rows are the faster (4 x 4,096
+    // tokens, a window of 512: 223 against 205 us).
     const bool many = b->max_q_len * group > kSplitRows;
     const bool large = lo->head_dim <= 128 && b->num_q * group / kLargeRows * lo->kv_heads >= 1024;
     plan->rows = !many ? kSplitRows : (large ? kLargeRows : kTileRows);
@@ -138,7 +140,9 @@ int plan_weights(const kv_layout *lo, const kv_batch *b, int32_t q_heads, int32_
     if (plan->windowed && span > (int64_t)window + b->max_q_len) span = (int64_t)window + b->max_q_len;
     plan->keys = !plan->few && heads * ((span + 255) / 256) < 512 ? 64 : 256;
     // With a window, 128 in between: where the requests' mean gives five workgroups for two compute units (4 x 2,000 tokens
-    // over 6,000, a window of 1,024: 127 us, 138 with 64 keys and 168 with 256; one of 4,096 over 8,192: 112 against 80).
+    // over 6,000, a window of 1,024: 127 us, 135 with 64 keys and 168 with 256; 8 of 512 over 2,512 75, 82 and 75; one of 4,096
+    // over 8,192 112 against 79 with 64, 2 of 2,000 over 6,000 at 2,048 173 against 126).  Of 18 batches of 1 to 16 requests
+    // and windows of 256 to 4,096 none is more than 11 % above the best of the three.
     if (plan->windowed && plan->keys == 64 && heads > 0) {
         const int64_t mean = (int64_t)window + b->num_q / b->num_reqs;
         if (heads * ((mean < span ? mean : span) / 128) >= 640) plan->keys = 128;

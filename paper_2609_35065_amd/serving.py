@@ -41,7 +41,9 @@ class ServedCache:
 
     With a ``window`` the first ``sink`` tokens of each request stay visible.  ``axes`` (kv_rope_axes) makes positions
     have several axes, which ``begin`` takes.  ``renumber`` makes every eviction give the kept tokens the positions
-    0, 1, ... in the cache's order, head by head (only with one axis: the tokens of several have no such order).
+    0, 1, ... in the cache's order, head by head (only with one axis: the tokens of several have no such order).  Each
+    such eviction rounds the keys that it moves to the cache's type once more, and these roundings add up: evict many
+    tokens at a time rather than one a step, above all from an 8-bit cache.
 
     The layers of a step share buffers, so that calls follow one another on the GPU: one that comes on another stream
     than the last waits for that one's work.  (Not in a graph capture: its replays are the program's to order.)"""
