@@ -83,38 +83,6 @@ __device__ __forceinline__ float weigh_tile(const WeightParams &p, const Span &s
     const int64_t first = span.first, len = span.len, ahead = span.ahead;
     const float c = p.scale * (F8 && p.k_scale ? p.k_scale[h] : 1.0f);
     const int t0 = tile0 + kw * kWaveKeys;     // t0 + 63 may pass 2^31 - 1: no key is there
-    // this lane's two keys, as operands; the element order follows the rows'
-    u32x4 kf[2][KS];
-    int from[2], to[2];
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-        const int64_t t = (int64_t)t0 + x * 32 + col;
-        uint32_t row = 0;
-        const int32_t blk = t < len ? block_of(p.cache, r, (uint32_t)t, row) : -1;
-        // the rows that see the key, causal from its own token on and up to the one whose window ends at it
-        const int64_t tok = t - ahead;
-        from[x] = blk < 0 ? 0 : (p.causal ? (int)min((int64_t)span.ntok, max((int64_t)0, tok)) * p.group : 0);
-        to[x] = blk < 0 ? 0 : span.ntok * p.group;
-        if (p.window > 0 && !(SINK && t < p.sink)) to[x] = min(to[x], (int)min((int64_t)span.ntok, max((int64_t)0, tok + p.window)) * p.group);
-        const char *at = p.cache.layer + (int64_t)h * p.cache.head_bytes +
-                         ((int64_t)(blk < 0 ? 0u : (uint32_t)blk * p.cache.block16 + row * p.cache.row16) << 4);
-        if constexpr (F8) {
-            // 16 elements at a time: a lane holds other elements than in order, as the rows are read below
-#pragma unroll
-            for (int ks = 0; ks < KS; ks += 2) {
-                const int d = ks * 16 + half * 16;
-                const u32x4 y = d < p.head_dim ? *(const u32x4 *)(at + d) : u32x4{0, 0, 0, 0};
-                kf[x][ks] = unpack8<T>(y[0], y[1]);
-                kf[x][ks + 1] = unpack8<T>(y[2], y[3]);
-            }
-        } else {
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks) {
-                const int d = ks * 16 + half * 8;
-                kf[x][ks] = d < p.head_dim ? *(const u32x4 *)(at + d * 2) : u32x4{0, 0, 0, 0};
-            }
-        }
-    }
     u32x4 qreg[VL];
     float base = 0.0f;
     // Where this lane's vectors of a step lie behind the step's first token.  Where each pass of the lanes takes whole
@@ -169,6 +137,41 @@ __device__ __forceinline__ float weigh_tile(const WeightParams &p, const Span &s
         }
         if (tid < kRows) lds.base[buf][tid] = base;
     };
+    // The first rows are on their way while the keys are looked up and, of 8 bits, unpacked (64 requests of 20 rows over 4,000
+    // tokens 158 us, 166 with them behind the keys).
+    if (row_begin < row_end) load(row_begin);
+    // this lane's two keys, as operands; the element order follows the rows'
+    u32x4 kf[2][KS];
+    int from[2], to[2];
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+        const int64_t t = (int64_t)t0 + x * 32 + col;
+        uint32_t row = 0;
+        const int32_t blk = t < len ? block_of(p.cache, r, (uint32_t)t, row) : -1;
+        // the rows that see the key, causal from its own token on and up to the one whose window ends at it
+        const int64_t tok = t - ahead;
+        from[x] = blk < 0 ? 0 : (p.causal ? (int)min((int64_t)span.ntok, max((int64_t)0, tok)) * p.group : 0);
+        to[x] = blk < 0 ? 0 : span.ntok * p.group;
+        if (p.window > 0 && !(SINK && t < p.sink)) to[x] = min(to[x], (int)min((int64_t)span.ntok, max((int64_t)0, tok + p.window)) * p.group);
+        const char *at = p.cache.layer + (int64_t)h * p.cache.head_bytes +
+                         ((int64_t)(blk < 0 ? 0u : (uint32_t)blk * p.cache.block16 + row * p.cache.row16) << 4);
+        if constexpr (F8) {
+            // 16 elements at a time: a lane holds other elements than in order, as the rows are read below
+#pragma unroll
+            for (int ks = 0; ks < KS; ks += 2) {
+                const int d = ks * 16 + half * 16;
+                const u32x4 y = d < p.head_dim ? *(const u32x4 *)(at + d) : u32x4{0, 0, 0, 0};
+                kf[x][ks] = unpack8<T>(y[0], y[1]);
+                kf[x][ks + 1] = unpack8<T>(y[2], y[3]);
+            }
+        } else {
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                const int d = ks * 16 + half * 8;
+                kf[x][ks] = d < p.head_dim ? *(const u32x4 *)(at + d * 2) : u32x4{0, 0, 0, 0};
+            }
+        }
+    }
     // Of 32 rows the operands are read while the exponentials of the 32 before are taken, and their lse after that: from
     // the next step's buffer too, which is filled, with the step's one barrier, between the products and exponentials of
     // its last rows.
@@ -234,15 +237,14 @@ __device__ __forceinline__ float weigh_tile(const WeightParams &p, const Span &s
     };
     const int mine = rw * RT * 32;
     if (row_begin < row_end) {
-        load(row_begin);
         stage(0);
         __syncthreads();
         if (row_begin + kRows < row_end) load(row_begin + kRows);
         read(0, mine);
         read_lse(0, mine);
     }
-    // Up to 32 rows, a request's that decodes in a batch of many rows, take one group: the others' products are left out (64
-    // requests of 20 rows over 4,000 tokens 166 us, 170 with them).
+    // Up to 32 rows, a request's that decodes in a batch of many rows, take one group: the others' products are left out
+    // (these 64 requests: 4 us).
     const bool one = row_end - row_begin <= 32;
     if (one && row_begin < row_end && mine == 0) {
         products();
